@@ -311,3 +311,16 @@ def mm_bf16_f32(A, B, out=None):
     if _mm_bf16_f32 is None:
         _mm_bf16_f32 = _helper("gemm_bf16_f32", "bfloat16", "float32")
     return _mm_bf16_f32(A, B, out)
+
+
+# ---------------------------------------------------------------- block-scaled operands
+_MX = ("MxMatrix", "linear_mx4", "linear_mx4_dx", "linear_mx8_dw", "pack_mx4", "pack_mx8", "unpack_mx")
+
+
+def __getattr__(name):
+    # The helpers of mx.py, which builds on this module, by the same names here.
+    if name in _MX:
+        from . import mx
+        globals().update((n, getattr(mx, n)) for n in _MX)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,0 +1,139 @@
+// mx_api.cpp -- the C ABI entry points of the block-scaled products (host side): argument
+// checks before any HIP call, then the launch.
+#include <stdint.h>
+
+#include "../../include/mx_mi355x.h"
+#include "mx.h"
+
+namespace {
+
+constexpr int64_t kMaxSize = int64_t(1) << 55;      // sizes and stride products stay in 64-bit byte offsets
+
+// One operand: rows of `used` bytes at a stride of `stride` bytes from `p`.
+struct Region {
+    uintptr_t p;
+    int64_t rows, used, stride;
+    int64_t align;
+    bool empty() const { return rows <= 0 || used <= 0; }
+    bool valid() const {
+        if (empty()) return true;
+        if (p == 0 || p % uintptr_t(align) != 0 || stride < used) return false;
+        return rows <= kMaxSize && stride <= kMaxSize / rows;
+    }
+    uint64_t span() const { return empty() ? 0 : uint64_t((rows - 1) * stride + used); }
+    bool overlaps(const Region &o) const {
+        return !empty() && !o.empty() && p < o.p + o.span() && o.p < p + span();
+    }
+};
+
+Region region(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
+    // Strides past the limit are left as they are: valid() refuses them.
+    const bool big = ld > kMaxSize || cols > kMaxSize;
+    return Region{reinterpret_cast<uintptr_t>(p), rows, big ? kMaxSize : cols * esize, big ? kMaxSize + 1 : ld * esize, esize};
+}
+
+int64_t code_bytes(int64_t cols, int bits) { return bits == 4 ? cols / 2 + cols % 2 : cols; }
+int64_t blocks(int64_t cols) { return cols / gemm::kMxBlock + (cols % gemm::kMxBlock != 0); }
+
+int status(int launched) {
+    switch (launched) {
+        case gemm::LAUNCH_OK: return GEMM_OK;
+        case gemm::LAUNCH_NO_MEMORY: return GEMM_ERR_NO_MEMORY;
+        default: return GEMM_ERR_HIP;
+    }
+}
+
+int convert(bool pack, int bits, int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *codes, int64_t ldq,
+            const uint8_t *scales, int64_t lds, void *stream) {
+    if (rows < 0 || cols < 0) return GEMM_ERR_INVALID_VALUE;
+    const Region rx = region(x, rows, cols, ldx, 2);
+    const Region rq = region(codes, rows, code_bytes(cols, bits), ldq, 1);
+    const Region rs = region(scales, rows, blocks(cols), lds, 1);
+    if (!rx.valid() || !rq.valid() || !rs.valid()) return GEMM_ERR_INVALID_VALUE;
+    if (rx.overlaps(rq) || rx.overlaps(rs) || (pack && rq.overlaps(rs))) return GEMM_ERR_INVALID_VALUE;
+    if (rows == 0 || cols == 0) return GEMM_OK;
+    const gemm::MxMatrixArgs a{rows, cols, const_cast<void *>(x), ldx, const_cast<void *>(codes), ldq,
+                               const_cast<uint8_t *>(scales), lds};
+    return status(pack ? gemm::launch_mx_pack(a, bits, stream) : gemm::launch_mx_unpack(a, bits, stream));
+}
+
+int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const void *codes,
+            int64_t ldq, const uint8_t *scales, int64_t lds, void *C, int64_t ldc, bool bf16_out, void *stream) {
+    if (M < 0 || N < 0 || K < 0) return GEMM_ERR_INVALID_VALUE;
+    const int bits = op == gemm::MX_DW ? 8 : 4;
+    const Region ra = op == gemm::MX_DW ? region(A, K, M, lda, 2) : region(A, M, K, lda, 2);
+    const int64_t b_rows = op == gemm::MX_FWD ? N : K, b_cols = op == gemm::MX_FWD ? K : N;
+    const Region rq = region(codes, b_rows, code_bytes(b_cols, bits), ldq, 1);
+    const Region rs = region(scales, b_rows, blocks(b_cols), lds, 1);
+    const Region rc = region(C, M, N, ldc, bf16_out ? 2 : 4);
+    if (!ra.valid() || !rq.valid() || !rs.valid() || !rc.valid()) return GEMM_ERR_INVALID_VALUE;
+    if (rc.overlaps(ra) || rc.overlaps(rq) || rc.overlaps(rs)) return GEMM_ERR_INVALID_VALUE;
+    if (M == 0 || N == 0) return GEMM_OK;
+    gemm::MxArgs a{};
+    a.g.dtype = 1;      // bf16 operands on the MFMAs
+    a.g.A = A;
+    a.g.B = codes;
+    a.g.C = C;
+    a.g.M = M; a.g.N = N; a.g.K = K;
+    a.g.lda = lda; a.g.ldb = ldq; a.g.ldc = ldc;
+    a.g.epilogue = bf16_out ? gemm::EPI_BF16 : gemm::EPI_NONE;
+    a.scales = scales;
+    a.ld_scales = lds;
+    return status(gemm::launch_mx_gemm(a, op, stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int mx_pack4(int64_t rows, int64_t cols, const uint16_t *X, int64_t ldx, uint8_t *codes, int64_t ldq, uint8_t *scales,
+             int64_t lds, void *stream) {
+    return convert(true, 4, rows, cols, X, ldx, codes, ldq, scales, lds, stream);
+}
+
+int mx_pack8(int64_t rows, int64_t cols, const uint16_t *X, int64_t ldx, int8_t *codes, int64_t ldq, uint8_t *scales,
+             int64_t lds, void *stream) {
+    return convert(true, 8, rows, cols, X, ldx, codes, ldq, scales, lds, stream);
+}
+
+int mx_unpack4(int64_t rows, int64_t cols, const uint8_t *codes, int64_t ldq, const uint8_t *scales, int64_t lds,
+               uint16_t *X, int64_t ldx, void *stream) {
+    return convert(false, 4, rows, cols, X, ldx, codes, ldq, scales, lds, stream);
+}
+
+int mx_unpack8(int64_t rows, int64_t cols, const int8_t *codes, int64_t ldq, const uint8_t *scales, int64_t lds,
+               uint16_t *X, int64_t ldx, void *stream) {
+    return convert(false, 8, rows, cols, X, ldx, codes, ldq, scales, lds, stream);
+}
+
+int mx_gemm_bf16_mx4_f32_bt(int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const uint8_t *codes,
+                            int64_t ldq, const uint8_t *scales, int64_t lds, float *C, int64_t ldc, void *stream) {
+    return product(gemm::MX_FWD, M, N, K, A, lda, codes, ldq, scales, lds, C, ldc, false, stream);
+}
+
+int mx_gemm_bf16_mx4_bf16_bt(int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const uint8_t *codes,
+                             int64_t ldq, const uint8_t *scales, int64_t lds, uint16_t *C, int64_t ldc, void *stream) {
+    return product(gemm::MX_FWD, M, N, K, A, lda, codes, ldq, scales, lds, C, ldc, true, stream);
+}
+
+int mx_gemm_bf16_mx4_f32(int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const uint8_t *codes,
+                         int64_t ldq, const uint8_t *scales, int64_t lds, float *C, int64_t ldc, void *stream) {
+    return product(gemm::MX_DX, M, N, K, A, lda, codes, ldq, scales, lds, C, ldc, false, stream);
+}
+
+int mx_gemm_bf16_mx4_bf16(int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const uint8_t *codes,
+                          int64_t ldq, const uint8_t *scales, int64_t lds, uint16_t *C, int64_t ldc, void *stream) {
+    return product(gemm::MX_DX, M, N, K, A, lda, codes, ldq, scales, lds, C, ldc, true, stream);
+}
+
+int mx_gemm_bf16_mx8_f32_at(int64_t M, int64_t N, int64_t K, const uint16_t *At, int64_t ldat, const int8_t *codes,
+                            int64_t ldq, const uint8_t *scales, int64_t lds, float *C, int64_t ldc, void *stream) {
+    return product(gemm::MX_DW, M, N, K, At, ldat, codes, ldq, scales, lds, C, ldc, false, stream);
+}
+
+int mx_gemm_bf16_mx8_bf16_at(int64_t M, int64_t N, int64_t K, const uint16_t *At, int64_t ldat, const int8_t *codes,
+                             int64_t ldq, const uint8_t *scales, int64_t lds, uint16_t *C, int64_t ldc, void *stream) {
+    return product(gemm::MX_DW, M, N, K, At, ldat, codes, ldq, scales, lds, C, ldc, true, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,368 @@
+"""The block-scaled kernels against their definitions in 64 bits: packing and unpacking bit for
+bit, the products within the bound of their fp32 sums."""
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as ref
+from paper_2512_13282_amd import binding as b
+from paper_2512_13282_amd import inputs, mx
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def place(x: np.ndarray, pad=0, offset=0, fill=0):
+    """A 2-D array in a larger GPU buffer: rows `pad` elements apart from contiguous, starting
+    `offset` elements in, everything else `fill`.  Returns (buffer, address, row stride)."""
+    rows, cols = x.shape
+    host = x.view(np.int16) if x.dtype == np.uint16 else x
+    ld = cols + pad
+    flat = np.full(offset + rows * ld + 64, fill, dtype=host.dtype)
+    if rows and cols:
+        flat[offset:offset + rows * ld].reshape(rows, ld)[:, :cols] = host
+    buf = torch.from_numpy(flat).to(DEV)
+    return buf, buf.data_ptr() + offset * buf.element_size(), ld
+
+
+# ---------------------------------------------------------------- packing
+
+def all_bf16():
+    """Every bf16 bit pattern, 32 of one kind in a block: 2048 rows of one block."""
+    return np.arange(65536, dtype=np.uint32).astype(np.uint16).reshape(2048, 32)
+
+
+def odd_matrix(rows, cols, seed):
+    """Values over many powers of two, with zeros, ties, subnormals, blocks of zeros and (for every
+    seventh row) infinities and NaN."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-140, 127, size=(rows, 1)))
+    x *= np.exp2(rng.integers(-12, 1, size=(rows, cols)))
+    ties = rng.random((rows, cols)) < 0.3
+    x = np.where(ties, np.exp2(np.floor(np.log2(np.abs(x) + 1e-300))) * (1 + rng.integers(0, 128, size=x.shape) / 128), x)
+    x = np.where(rng.random((rows, cols)) < 0.1, 0.0, x) * rng.choice([-1, 1], size=x.shape)
+    with np.errstate(over="ignore"):
+        bits = inputs.bf16_bits_from_f32(x.astype(np.float32))
+    bits = np.where((bits & 0x7fff) >= 0x7f80, bits & 0x8000 | 0x7f00, bits).astype(np.uint16)
+    for r in range(0, rows, 5):
+        bits[r, :32] &= 0x8000
+    for r in range(3, rows, 7):
+        bits[r, rng.integers(0, cols)] = rng.choice(np.array([0x7f80, 0xff80, 0x7fc0, 0xffff, 0x7f81], np.uint16))
+    return bits
+
+
+def run_pack(bits, width, pads=(0, 0, 0), offsets=(0, 0, 0)):
+    rows, cols = bits.shape
+    nbytes = (cols + 1) // 2 if width == 4 else cols
+    xb, xa, ldx = place(bits, pads[0], offsets[0], -1)
+    qb, qa, ldq = place(np.full((rows, nbytes), 0x55, np.uint8), pads[1], offsets[1], 0x55)
+    sb, sa, lds = place(np.full((rows, -(-cols // 32)), 0x77, np.uint8), pads[2], offsets[2], 0x77)
+    rc = (mx.mx_pack4 if width == 4 else mx.mx_pack8)(rows, cols, xa, ldx, qa, ldq, sa, lds, stream())
+    assert rc == b.GEMM_OK
+    torch.cuda.synchronize()
+    q, s = qb.cpu().numpy(), sb.cpu().numpy()
+    codes = q[offsets[1]:offsets[1] + rows * ldq].reshape(rows, ldq)
+    scales = s[offsets[2]:offsets[2] + rows * lds].reshape(rows, lds)
+    assert np.all(codes[:, nbytes:] == 0x55) and np.all(q[offsets[1] + rows * ldq:] == 0x55) and np.all(q[:offsets[1]] == 0x55)
+    assert np.all(scales[:, -(-cols // 32):] == 0x77) and np.all(s[:offsets[2]] == 0x77)
+    codes = codes[:, :nbytes]
+    return (codes.view(np.int8) if width == 8 else codes), scales[:, :-(-cols // 32)]
+
+
+@pytest.mark.parametrize("width", [4, 8])
+def test_every_bf16_pattern_packs(width):
+    bits = all_bf16()
+    codes, scales = run_pack(bits, width)
+    want_codes, want_scales = ref.pack(bits, width)
+    assert np.array_equal(scales, want_scales)
+    if width == 4:      # a zero's sign is free
+        v, w = ref.values(codes, scales, 32), ref.values(want_codes, want_scales, 32)
+        assert np.array_equal(v, w, equal_nan=True)
+        assert np.all(codes[scales[:, 0] == 255] == 0)
+    else:
+        assert np.array_equal(codes, want_codes)
+
+
+@pytest.mark.parametrize("width", [4, 8])
+@pytest.mark.parametrize("rows,cols,pads,offsets", [
+    (1, 1, (0, 0, 0), (0, 0, 0)), (3, 7, (0, 0, 0), (0, 0, 0)), (5, 31, (1, 2, 3), (1, 1, 1)),
+    (9, 32, (0, 0, 0), (0, 0, 0)), (7, 33, (3, 5, 0), (3, 3, 2)), (40, 63, (1, 0, 0), (0, 1, 0)),
+    (17, 1000, (8, 12, 3), (8, 16, 0)), (33, 1027, (0, 0, 0), (0, 0, 0)), (2, 5003, (5, 1, 1), (1, 7, 3)),
+    (700, 40, (0, 12, 0), (0, 0, 0)),
+])
+def test_packing_any_shape(width, rows, cols, pads, offsets):
+    bits = odd_matrix(rows, cols, 100 * rows + cols)
+    codes, scales = run_pack(bits, width, pads, offsets)
+    want_codes, want_scales = ref.pack(bits, width)
+    assert np.array_equal(scales, want_scales)
+    assert np.array_equal(ref.values(codes, scales, cols), ref.values(want_codes, want_scales, cols), equal_nan=True)
+    if width == 4 and cols % 2:
+        assert np.all(codes[:, -1] < 16)
+    if width == 8:
+        assert np.array_equal(codes, want_codes)
+
+
+@pytest.mark.parametrize("width", [4, 8])
+@pytest.mark.parametrize("rows,cols,pads,offsets", [
+    (256, 64, (0, 0, 0), (0, 0, 0)), (3, 33, (1, 1, 1), (1, 3, 5)), (1, 1, (0, 0, 0), (0, 0, 0)),
+    (19, 2049, (0, 15, 0), (0, 0, 0)),
+])
+def test_unpacking_every_code_and_scale(width, rows, cols, pads, offsets):
+    rng = np.random.default_rng(rows + cols)
+    if width == 4:
+        codes = rng.integers(0, 256, size=(rows, (cols + 1) // 2)).astype(np.uint8)
+    else:
+        codes = rng.integers(-128, 128, size=(rows, cols)).astype(np.int8)
+    scales = rng.integers(0, 256, size=(rows, -(-cols // 32))).astype(np.uint8)
+    if (rows, cols) == (256, 64):       # every scale byte against many codes
+        scales[:, 0] = scales[:, 1] = np.arange(256)
+    qb, qa, ldq = place(codes, pads[1], offsets[1], -1 if width == 8 else 255)
+    sb, sa, lds = place(scales, pads[2], offsets[2], 255)
+    xb, xa, ldx = place(np.zeros((rows, cols), np.uint16), pads[0], offsets[0], 0x5a5a)
+    rc = (mx.mx_unpack4 if width == 4 else mx.mx_unpack8)(rows, cols, qa, ldq, sa, lds, xa, ldx, stream())
+    assert rc == b.GEMM_OK
+    torch.cuda.synchronize()
+    flat = xb.cpu().numpy().view(np.uint16)
+    got = flat[offsets[0]:offsets[0] + rows * ldx].reshape(rows, ldx)
+    assert np.all(got[:, cols:] == 0x5a5a)
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = ref.values(codes, scales, cols).astype(np.float32).astype(np.float64)     # past fp32's range: infinite
+    assert np.array_equal(ref.widen(got[:, :cols]), want, equal_nan=True)
+
+
+# ---------------------------------------------------------------- products
+
+OPS = ("fwd", "dx", "dw")
+
+
+def run_product(op, M, N, K, a_bits, codes, scales, bf16_out, pads=(0, 0, 0, 0), offsets=(0, 0, 0, 0)):
+    """C through the C ABI; everything around A is NaN, around the codes 0xff, around the scales 255."""
+    ab, aa, lda = place(a_bits, pads[0], offsets[0], -1)
+    qb, qa, ldq = place(codes.view(np.uint8), pads[1], offsets[1], 255)
+    sb, sa, lds = place(scales, pads[2], offsets[2], 255)
+    ldc = N + pads[3]
+    cb = torch.full((offsets[3] + M * ldc + 64,), 12.0, dtype=torch.bfloat16 if bf16_out else torch.float32, device=DEV)
+    name = {"fwd": "mx_gemm_bf16_mx4_{}_bt", "dx": "mx_gemm_bf16_mx4_{}", "dw": "mx_gemm_bf16_mx8_{}_at"}[op]
+    fn = getattr(mx, name.format("bf16" if bf16_out else "f32"))
+    rc = fn(M, N, K, aa, lda, qa, ldq, sa, lds, cb.data_ptr() + offsets[3] * cb.element_size(), ldc, stream())
+    assert rc == b.GEMM_OK, b.gemm_status_string(rc)
+    torch.cuda.synchronize()
+    flat = cb.float().cpu().numpy().astype(np.float64)
+    C = flat[offsets[3]:offsets[3] + M * ldc].reshape(M, ldc)
+    assert np.all(C[:, N:] == 12.0) and np.all(flat[:offsets[3]] == 12.0) and np.all(flat[offsets[3] + M * ldc:] == 12.0)
+    return C[:, :N]
+
+
+def operands(op, M, N, K, seed):
+    a = inputs.bf16_matrix(*((K, M) if op == "dw" else (M, K)), seed)
+    rows, cols = (N, K) if op == "fwd" else (K, N)
+    codes, scales = ref.random_packed(rows, cols, 8 if op == "dw" else 4, seed + 1)
+    return a, codes, scales, cols
+
+
+def check_product(op, M, N, K, bf16_out, seed=0, **kw):
+    a, codes, scales, cols = operands(op, M, N, K, seed)
+    C = run_product(op, M, N, K, a, codes, scales, bf16_out, **kw)
+    want, magnitude = ref.product(op, ref.widen(a), ref.values(codes, scales, cols))
+    off = np.abs(C - want)
+    lim = ref.bound(K, magnitude, want, bf16_out)
+    assert np.all(off <= lim), (op, M, N, K, float((off / lim).max()), np.argwhere(~(off <= lim))[:4].tolist())
+
+
+SIZES = [(1, 1, 1), (1, 16, 32), (1, 33, 31), (2, 64, 64), (3, 17, 129), (5, 130, 95), (8, 100, 600), (15, 257, 127),
+         (16, 256, 256), (17, 48, 1000), (31, 65, 33), (33, 129, 2049), (48, 515, 321), (64, 320, 512), (65, 64, 96),
+         (100, 256, 1024), (127, 300, 40), (129, 511, 700), (200, 264, 1040), (256, 512, 64), (257, 130, 513), (300, 1024, 256)]
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("bf16_out", [False, True], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_products(op, size, bf16_out):
+    check_product(op, *size, bf16_out, seed=sum(size))
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("size", [(1, 96, 160), (7, 65, 97), (40, 200, 131), (70, 129, 260), (150, 300, 515)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("pads,offsets", [((8, 16, 3, 4), (8, 16, 5, 4)), ((1, 1, 1, 1), (1, 1, 1, 1)),
+                                          ((0, 3, 0, 0), (4, 4, 0, 3)), ((3, 0, 0, 5), (0, 0, 1, 0))])
+def test_products_with_strides_and_offsets(op, size, pads, offsets):
+    check_product(op, *size, False, seed=sum(size), pads=pads, offsets=offsets)
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 70), (130, 257)])
+def test_empty_sum_writes_zeros(op, M, N):
+    a, codes, scales, _ = operands(op, M, N, 0, 1)
+    for bf16_out in (False, True):
+        assert np.all(run_product(op, M, N, 0, a, codes, scales, bf16_out, pads=(0, 0, 0, 3)) == 0.0)
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("size", [(1, 128, 320), (20, 96, 200), (140, 260, 300)], ids=lambda s: "x".join(map(str, s)))
+def test_not_a_number_stays_in_its_row_and_column(op, size):
+    """A NaN block of B, a NaN and an infinity of A reach the results that use them, and no others."""
+    M, N, K = size
+    a, codes, scales, cols = operands(op, M, N, K, 3)
+    scales = scales.copy()
+    scales[scales.shape[0] // 2, -1] = 255              # the last block of a row, a short one where cols is odd
+    av = a if op != "dw" else a.T
+    av[M - 1, K // 3] = 0x7f80
+    C = run_product(op, M, N, K, a, codes, scales, False)
+    with np.errstate(invalid="ignore"):
+        bv = ref.values(codes, scales, cols)
+        left, right = ref.widen(a), bv
+        if op == "dw":
+            left = left.T
+        if op == "fwd":
+            right = right.T
+        finite = np.where(np.isfinite(left), left, 0.0) @ np.where(np.isfinite(right), right, 0.0)
+    bad = (~np.isfinite(left)).any(1)[:, None] | (~np.isfinite(right)).any(0)[None, :]
+    assert np.all(np.isfinite(C) == ~bad)
+    lim = ref.bound(K, np.abs(np.nan_to_num(left, posinf=0, neginf=0)) @ np.abs(np.nan_to_num(right)), finite, False)
+    assert np.all(np.abs(C - finite)[~bad] <= lim[~bad])
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("size", [(1, 512, 2048), (40, 512, 4096), (300, 512, 1024)], ids=lambda s: "x".join(map(str, s)))
+def test_same_bits_on_every_run_and_stream(op, size):
+    M, N, K = size
+    a, codes, scales, _ = operands(op, M, N, K, 9)
+    first = run_product(op, M, N, K, a, codes, scales, False)
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        for _ in range(3):
+            assert np.array_equal(run_product(op, M, N, K, a, codes, scales, False), first)
+
+
+# ---------------------------------------------------------------- the torch helpers
+
+def packed(rows, cols, width, seed):
+    x = torch.from_numpy(inputs.bf16_matrix(rows, cols, seed).view(np.int16)).to(DEV).view(torch.bfloat16)
+    return x, (mx.pack_mx4 if width == 4 else mx.pack_mx8)(x)
+
+
+def numbers(Q):
+    return ref.values(Q.codes.cpu().numpy(), Q.scales.cpu().numpy(), Q.cols)
+
+
+def test_helpers_pack_as_the_definition_says():
+    for width in (4, 8):
+        x, Q = packed(37, 131, width, 5)
+        codes, scales = ref.pack(x.view(torch.int16).cpu().numpy().view(np.uint16), width)
+        assert np.array_equal(Q.scales.cpu().numpy(), scales)
+        assert np.array_equal(numbers(Q), ref.values(codes, scales, 131))
+        assert np.array_equal(mx.unpack_mx(Q).double().cpu().numpy(), numbers(Q))
+        # A strided source, and a single column.
+        wide = torch.zeros(37, 200, dtype=torch.bfloat16, device=DEV)
+        wide[:, 60:191] = x
+        assert torch.equal(mx.unpack_mx((mx.pack_mx4 if width == 4 else mx.pack_mx8)(wide[:, 60:191])), mx.unpack_mx(Q))
+        one = (mx.pack_mx4 if width == 4 else mx.pack_mx8)(x[:, :1])
+        assert one.codes.shape == (37, 1) and mx.unpack_mx(one).shape == (37, 1)
+
+
+def test_a_layer_forward_and_backward():
+    """y = x W^T, dx = dy W and dW = dy^T x^ of one layer, x^ its input as packed."""
+    T, n_in, n_out = 70, 288, 130
+    _, W = packed(n_out, n_in, 4, 1)
+    x, X = packed(T, n_in, 8, 2)
+    dy, _ = packed(T, n_out, 8, 3)
+    w, xh = numbers(W), numbers(X)
+    for got, want, mag, K, wide in (
+            (mx.linear_mx4(x, W), *ref.product("fwd", x.double().cpu().numpy(), w), n_in, False),
+            (mx.linear_mx4(x, W, out_dtype=torch.float32), *ref.product("fwd", x.double().cpu().numpy(), w), n_in, True),
+            (mx.linear_mx4_dx(dy, W), *ref.product("dx", dy.double().cpu().numpy(), w), n_out, False),
+            (mx.linear_mx8_dw(dy, X), *ref.product("dw", dy.double().cpu().numpy(), xh), T, True),
+            (mx.linear_mx8_dw(dy, X, out_dtype=torch.bfloat16), *ref.product("dw", dy.double().cpu().numpy(), xh), T, False)):
+        assert got.dtype == (torch.float32 if wide else torch.bfloat16)
+        assert np.all(np.abs(got.double().cpu().numpy() - want) <= ref.bound(K, mag, want, not wide))
+
+
+def test_gradients_against_differences():
+    """The layer is linear in x and in W: a step along any direction changes sum(G * y) by exactly the
+    gradient times the step, up to the rounding of the sums."""
+    T, n_in, n_out = 24, 96, 64
+    _, W = packed(n_out, n_in, 4, 11)
+    x, X = packed(T, n_in, 8, 12)
+    g, _ = packed(T, n_out, 8, 13)
+    xh = mx.unpack_mx(X)
+    y = mx.linear_mx4(xh, W, out_dtype=torch.float32).double()
+    dx = mx.linear_mx4_dx(g, W, out_dtype=torch.float32).double()
+    dw = mx.linear_mx8_dw(g, X).double()
+    w, gd, xd = torch.from_numpy(numbers(W)).to(DEV), g.double(), xh.double()
+    step, _ = packed(T, n_in, 8, 14)
+    moved = mx.linear_mx4((xd + step.double()).to(torch.bfloat16), W, out_dtype=torch.float32).double()
+    real = (xd + step.double()).to(torch.bfloat16).double() - xd
+    size = (gd.abs() @ (w.abs())).mul(2 * xd.abs() + 2 * real.abs()).sum()
+    assert abs((gd * (moved - y)).sum() - (dx * real).sum()) <= (n_in + n_out + 200) * 2.0 ** -23 * size
+    # sum(G * (x (W + D)^T)) - sum(G * x W^T) = sum(dW * D), with D a packed matrix of its own.
+    _, D = packed(n_out, n_in, 4, 15)
+    d = torch.from_numpy(numbers(D)).to(DEV)
+    change = (gd * mx.linear_mx4(xh, D, out_dtype=torch.float32).double()).sum()
+    size = ((gd.abs().T @ xd.abs()) * d.abs()).sum()
+    assert abs(change - (dw * d).sum()) <= (T + n_in + 200) * 2.0 ** -23 * size
+
+
+def test_helpers_take_strided_operands_and_outputs():
+    x, X = packed(50, 200, 8, 21)
+    _, W = packed(90, 200, 4, 22)
+    wide = torch.zeros(50, 333, dtype=torch.bfloat16, device=DEV)
+    wide[:, 33:233] = x
+    out = torch.zeros(50, 100, device=DEV)
+    got = mx.linear_mx4(wide[:, 33:233], W, out=out[:, 5:95])
+    assert got.data_ptr() == out.data_ptr() + 20 and torch.equal(got, mx.linear_mx4(x, W, out_dtype=torch.float32))
+    assert torch.all(out[:, :5] == 0) and torch.all(out[:, 95:] == 0)
+    # Codes whose rows follow each other, and one row of a packed weight.
+    tight = mx.MxMatrix(W.codes.contiguous(), W.scales, W.cols)
+    assert torch.equal(mx.linear_mx4(x, tight), mx.linear_mx4(x, W))
+    row = mx.MxMatrix(W.codes[7:8], W.scales[7:8], W.cols)
+    lim = torch.from_numpy(ref.bound(200, *ref.product("fwd", x.double().cpu().numpy(), numbers(row))[::-1], True)).to(DEV)
+    assert torch.all((mx.linear_mx4(x, row).double() - mx.linear_mx4(x, W)[:, 7:8].double()).abs() <= 2 * lim)
+
+
+def test_helpers_refuse():
+    x, X = packed(8, 64, 8, 31)
+    _, W = packed(16, 64, 4, 32)
+    with pytest.raises(TypeError):
+        mx.linear_mx4(x, X)                     # 8-bit codes as a weight
+    with pytest.raises(TypeError):
+        mx.linear_mx8_dw(x, W)
+    with pytest.raises(TypeError):
+        mx.linear_mx4(x, W, out_dtype=torch.float16)
+    with pytest.raises(ValueError):
+        mx.linear_mx4_dx(x, W)                  # 64 columns against 16 rows
+    with pytest.raises(ValueError):
+        mx.linear_mx4(x, mx.MxMatrix(W.codes, W.scales[:, :1], 64))
+    with pytest.raises(ValueError):
+        mx.linear_mx4(x, W, out=torch.empty(8, 15, device=DEV))
+    with pytest.raises(ValueError):
+        mx.linear_mx4(x.t()[:8, :8], mx.MxMatrix(W.codes[:, :4], W.scales[:, :1], 8))   # strided elements
+    with pytest.raises(b.GemmError):
+        mx.linear_mx4(x, W, out=x[:, :16])      # the output in the input
+
+
+@pytest.mark.parametrize("op", OPS)
+def test_captured_calls_replay(op):
+    """Replays, with eager work between them, give the eager result of the inputs they find."""
+    M, N, K = {"fwd": (48, 520, 1056), "dx": (40, 544, 2048), "dw": (48, 544, 2000)}[op]
+    a, codes, scales, cols = operands(op, M, N, K, 41)
+    A = torch.from_numpy(a.view(np.int16)).to(DEV).view(torch.bfloat16)
+    Q = mx.MxMatrix(torch.from_numpy(codes).to(DEV), torch.from_numpy(scales).to(DEV), cols)
+    fn = {"fwd": mx.linear_mx4, "dx": mx.linear_mx4_dx, "dw": mx.linear_mx8_dw}[op]
+    out = torch.empty(M, N, device=DEV)
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        fn(A, Q, out=out)
+    for i in range(4):
+        A.normal_()
+        want = fn(A, Q, out_dtype=torch.float32)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        out.fill_(7.0)
