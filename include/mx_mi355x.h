@@ -29,7 +29,8 @@
  * read, without using, the bytes up to the next multiple of 16.
  * GEMM_ERR_INVALID_VALUE is returned for a negative size, a stride that is too small,
  * a NULL pointer whose operand is non-empty, a bf16 or fp32 pointer that is not
- * aligned to its element size, and an output that overlaps an input or another output.
+ * aligned to its element size, and an output that overlaps an input or another output;
+ * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more.
  */
 #ifndef MX_MI355X_H
 #define MX_MI355X_H
@@ -88,6 +89,26 @@ int mx_gemm_bf16_mx8_f32_at(int64_t M, int64_t N, int64_t K, const uint16_t *At,
 int mx_gemm_bf16_mx8_bf16_at(int64_t M, int64_t N, int64_t K, const uint16_t *At, int64_t ldat,
                              const int8_t *codes, int64_t ldq, const uint8_t *scales, int64_t lds,
                              uint16_t *C, int64_t ldc, void *stream);
+
+/* Pure host: the plan that a product of these sizes would use: the kernel's
+ * configuration (-1: nothing to do), its output tile, the number of K slices and the K
+ * of each.  GEMM_ERR_INVALID_VALUE: an unknown op, a negative size, a NULL out. */
+typedef struct mx_plan_info {
+    int32_t config;
+    int32_t bm, bn;
+    int32_t split_k;
+    int64_t k_chunk;
+    char    name[48];
+} mx_plan_info;
+
+enum { MX_OP_FORWARD = 0, MX_OP_INPUT_GRADIENT = 1, MX_OP_WEIGHT_GRADIENT = 2 };
+
+int mx_plan(int op, int64_t M, int64_t N, int64_t K, mx_plan_info *out);
+
+/* Test and benchmark hook: the configuration (-1: the library's choice) and the number of
+ * K slices (0: its choice) of every later product of `op`.  A product that the
+ * configuration cannot run returns GEMM_ERR_UNSUPPORTED. */
+int mx_force_plan(int op, int config, int split_k);
 
 #ifdef __cplusplus
 }

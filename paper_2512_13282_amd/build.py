@@ -23,7 +23,7 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libgemm_mi355x.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-HOST_SOURCES = ["gemm_api.cpp", "selector.cpp", "mx_api.cpp"]
+HOST_SOURCES = ["gemm_api.cpp", "selector.cpp", "mx_api.cpp", "mx_plan.cpp"]
 DEVICE_SOURCES = sorted(os.path.basename(p) for p in glob.glob(os.path.join(CSRC, "*.hip")))
 
 # Packed-fp32 instructions are disabled for all device code (the hipcc host

@@ -101,8 +101,9 @@ static void *malloc_in_capture(size_t bytes) {
 // Partials and counters for a call on `stream`, grown where they are too small.  In a capture
 // the counters do not grow (what zeroes them would run at each replay, not now), and the call
 // gets LAUNCH_NO_COUNTERS, before anything is queued.
-static int acquire_workspace(hipStream_t stream, size_t partial_bytes, int64_t counter_words, void **partials,
-                             uint32_t **counters) {
+int acquire_workspace(void *stream_ptr, size_t partial_bytes, int64_t counter_words, void **partials,
+                      uint32_t **counters) {
+    hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return LAUNCH_HIP_ERROR;
     std::lock_guard<std::mutex> lk(g_ws_mu);

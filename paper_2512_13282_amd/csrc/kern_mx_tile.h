@@ -1,0 +1,437 @@
+// kern_mx_tile.h -- the products over block-scaled operands on output tiles.
+#pragma once
+
+#include "mx_common.h"
+
+namespace gemm {
+
+// ---------------------------------------------------------------------------
+// C = A . W^T, W 4-bit N x K.  Both operands go from memory straight into a ring of NS LDS
+// stages of KS k: A as BM rows of 128 bytes per 64 k (16-byte chunks XOR-swizzled by swz), W
+// packed as it is, BN rows of KS / 2 bytes.  A lane reads the 16 bytes of one W block once
+// (32 k: its share of four MFMA k-steps) and converts eight codes at a time in registers,
+// so W costs a quarter of bf16's LDS and load-path traffic and the conversions (four
+// instructions per 32 x 16 fragment) are repeated only by the WM waves that share its rows.
+// k-step t of a 64-k part takes, for lanes of half h, k = 32 h + 8 t + 0..7 of both operands.
+//
+// The block scales of the tile's rows sit in LDS for PANEL k at a time, loaded through
+// registers between two stages: their bytes are too few and too scattered to ride along in
+// each stage.
+// ---------------------------------------------------------------------------
+template <int BM, int BN, int WM, int WN, int WAVES_PER_EU, int KS, int NS, int PANEL>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN),
+                          amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU)))
+void mx_fwd_kernel(MxArgs a) {
+    constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+    constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int PARTS = KS / 64;                            // 64-k parts of a stage
+    constexpr int A_PART = BM * 128, A_STAGE = A_PART * PARTS;
+    constexpr int PITCH = KS / 2, CPR = PITCH / 16;           // bytes and chunks of a W row
+    constexpr int B_STAGE = BN * PITCH;
+    constexpr int A_INSTR = A_STAGE / 1024 / WAVES, B_INSTR = B_STAGE / 1024 / WAVES;
+    constexpr int LPS = A_INSTR + B_INSTR;
+    static_assert(A_INSTR >= 1 && A_INSTR * 1024 * WAVES == A_STAGE, "A stage split");
+    static_assert(B_INSTR >= 1 && B_INSTR * 1024 * WAVES == B_STAGE, "W stage split");
+    static_assert(NS >= 2 && (NS - 1) * LPS < 64, "loads in flight must fit vmcnt");
+    // A panel row is an odd number of dwords: 32 rows lie on 32 banks.
+    constexpr int PANEL_PITCH = PANEL / kMxBlock + 4;
+    static_assert(PANEL % KS == 0 && PANEL % 256 == 0, "a stage has one panel, of whole odd rows");
+
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NS][A_STAGE + B_STAGE];
+    __shared__ uint8_t panel[BN * PANEL_PITCH];
+
+    const int tid = int(threadIdx.x), lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave_m = wave / WN, wave_n = wave % WN;
+    int tm, tn, slice;
+    map_tile(a.g, tm, tn, slice);
+    const int64_t M = a.g.M, N = a.g.N;
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+    const int64_t k_begin = int64_t(slice) * a.g.k_chunk;
+    const int64_t k_end = k_begin + a.g.k_chunk < a.g.K ? k_begin + a.g.k_chunk : a.g.K;
+    const int k_len = k_end > k_begin ? int(k_end - k_begin) : 0;
+    const int nk = (k_len + KS - 1) / KS;
+    const int64_t lda_b = a.g.lda * 2, ldq = a.g.ldb;
+
+    // Where this lane's pieces of a stage come from.  A: load i fills part (i W + wave) KiB / A_PART.
+    const uint32_t a_bytes = uint32_t(((M - m0) < BM ? (M - m0) : BM) * lda_b);
+    uint32_t a_voff[A_INSTR];
+    int a_k[A_INSTR];
+#pragma unroll
+    for (int i = 0; i < A_INSTR; ++i) {
+        const int row = ((i * WAVES + wave) * 8 + (lane >> 3)) % BM, part = ((i * WAVES + wave) * 8) / BM;
+        const int c = swz(lane & 7, row);
+        a_k[i] = 64 * part + 8 * c;
+        a_voff[i] = uint32_t(row * lda_b + 128 * part + 16 * c);
+    }
+    // W: chunk c of row r sits at chunk c ^ w_swz(r), which spreads 32 rows' reads over the banks.
+    auto w_swz = [](int row) { return CPR == 8 ? (row ^ (row >> 3)) & 7 : CPR == 4 ? ring_swz(row) : (row >> 3) & 1; };
+    const uint32_t b_bytes = uint32_t(((N - n0) < BN ? (N - n0) : BN) * ldq);
+    uint32_t b_voff[B_INSTR];
+    int b_k[B_INSTR];
+#pragma unroll
+    for (int i = 0; i < B_INSTR; ++i) {
+        const int row = (i * WAVES + wave) * (64 / CPR) + lane / CPR;
+        const int c = (lane % CPR) ^ w_swz(row);
+        b_k[i] = 32 * c;
+        b_voff[i] = uint32_t(row * ldq + 16 * c);
+    }
+    const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + m0 * lda_b + k_begin * 2;
+    const uint8_t *const b_base = static_cast<const uint8_t *>(a.g.B) + n0 * ldq + k_begin / 2;
+
+    auto load_stage = [&](int kt, auto buf_c) {
+        constexpr int BUF = decltype(buf_c)::value;
+        const int rem = k_len - kt * KS;
+        const uint32_t dst = lds_addr(lds[BUF]) + uint32_t(wave) * 1024u;
+        const i32x4_t ra = ring_rsrc(a_base + int64_t(kt) * (KS * 2), rem > 0 ? a_bytes : 0u);
+        const i32x4_t rb = ring_rsrc(b_base + int64_t(kt) * PITCH, rem > 0 ? b_bytes : 0u);
+#pragma unroll
+        for (int i = 0; i < B_INSTR; ++i)
+            ring_load16(rb, dst + A_STAGE + i * (WAVES * 1024), b_k[i] < rem ? b_voff[i] : kOOB);
+#pragma unroll
+        for (int i = 0; i < A_INSTR; ++i) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
+    };
+    // The scales of rows n0.. from k0 (of this slice) on; rows and blocks past the end take 0.
+    auto load_panel = [&](int k0) {
+        const int64_t b0 = (k_begin + k0) / kMxBlock, nb = (a.g.K + kMxBlock - 1) / kMxBlock;
+        constexpr int DW = PANEL / kMxBlock / 4;          // dwords of a panel row
+        for (int p = tid; p < BN * DW; p += THREADS) {
+            const int r = p / DW, d = p % DW;
+            if (k0 + d * 4 * kMxBlock >= nk * KS) continue;      // no stage reads them
+            const uint8_t *const src = a.scales + (n0 + r) * a.ld_scales + b0 + 4 * d;
+            const int64_t left = n0 + r < N ? nb - (b0 + 4 * d) : 0;
+            uint32_t v = 0;
+            if (left >= 4) {
+                v = *reinterpret_cast<const u32_any_mx *>(src);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) v |= uint32_t(src[e]) << (8 * e);
+            }
+            *reinterpret_cast<uint32_t *>(&panel[r * PANEL_PITCH + 4 * d]) = v;
+        }
+    };
+
+    const int frag_row = lane & 31, half = lane >> 5;
+    const int r0 = wave_m * (BM / WM) + frag_row, c0 = wave_n * (BN / WN) + frag_row;
+    int a_fo[2][4];                                           // k-step t of the wave's 32-row tiles (even, odd)
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) a_fo[p][t] = r0 * 128 + 16 * (swz(4 * half + t, r0) ^ (4 * p));
+    int b_fo[TN][PARTS];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q)
+            b_fo[j][q] = A_STAGE + (c0 + 32 * j) * PITCH + 16 * ((2 * q + half) ^ w_swz(c0 + 32 * j));
+
+    f32x16_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
+
+    auto iteration = [&](int kt, auto buf_c) {
+        constexpr int BUF = decltype(buf_c)::value;
+        ring_barrier<(NS - 2) * LPS>();
+        uint8_t *const st = lds[BUF];
+        if (kt == nk - 1 && (k_len & 7) != 0) {
+            // K ends inside a chunk: what follows it in A's row is not part of the sum.
+            const int kl = k_len - kt * KS, part = kl / 64, c = (kl % 64) / 8;
+            for (int r = tid; r < BM; r += THREADS)
+                for (int e = kl & 7; e < 8; ++e)
+                    reinterpret_cast<uint16_t *>(st + part * A_PART + r * 128 + 16 * swz(c, r))[e] = 0;
+            phase_barrier();
+        }
+        load_stage(kt + NS - 1, std::integral_constant<int, (BUF + NS - 1) % NS>{});
+        const int block0 = (kt * KS % PANEL) / kMxBlock + half;
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            u32x4_t w[TN];
+            float s[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                w[j] = *reinterpret_cast<const u32x4_t *>(st + b_fo[j][q]);
+                s[j] = mx4_scale(panel[(c0 + 32 * j) * PANEL_PITCH + block0 + 2 * q]);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                u32x4_t fa[TM], fb[TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+                    fa[i] = *reinterpret_cast<const u32x4_t *>(st + q * A_PART + a_fo[i & 1][t] + 4096 * i);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[j] = mx4_to_bf16(w[j][t], s[j]);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma32<DT_BF16>(fa[i], fb[j], acc[i][j]);
+            }
+        }
+    };
+
+    if (nk > 0) {
+        static_for<0, NS - 1>([&](auto u) { load_stage(decltype(u)::value, u); });
+        for (int kt = 0; kt < nk; kt += NS) {
+            static_for<0, NS>([&](auto u) {
+                constexpr int U = decltype(u)::value;
+                if (kt + U < nk) {
+                    if ((kt + U) % (PANEL / KS) == 0) {
+                        if (kt + U > 0) phase_barrier();      // every wave is done with the panel before
+                        load_panel((kt + U) * KS);
+                    }
+                    iteration(kt + U, u);
+                }
+            });
+        }
+    }
+    stage_barrier();
+    store_tile<DT_BF16, BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wave_m * (BM / WM), n0 + wave_n * (BN / WN), lane,
+                                        *reinterpret_cast<int *>(lds[0]));
+}
+
+// ---------------------------------------------------------------------------
+// C = A . W (MX_DX: A bf16 M x K, W 4-bit K x N) and C = A^T . X (MX_DW: A bf16 K x M, X 8-bit
+// K x N): the blocks lie along N, across the sum, so every k of a column has another scale
+// and no scale can be applied after the matrix instruction.  B is converted to bf16 (exactly)
+// once per workgroup, on its way into LDS: a thread takes one block of 32 codes of one row k
+// through registers per stage of 64 k.  A goes straight from memory into LDS.
+//
+// LDS, two stages each: A as BM rows of 128 bytes (DX), or as 64 rows (k) of BM elements read
+// back transposed (DW), both as gemm_lds_kernel lays them out.  B in one region per block column:
+// 64 rows (k) of 32 bf16, the 64-byte rows back to back, the regions 64 bytes further apart.
+// A transpose read then covers two runs of 256 bytes, and the eight lanes that write one row's
+// chunks hit different banks (the regions of blocks 0-3 by their offset, 4-7 by a flipped chunk).
+//
+// B's codes are loaded two stages ahead into registers, A one stage ahead.
+// ---------------------------------------------------------------------------
+template <int OP, int BM, int BN, int WM, int WN, int WAVES_PER_EU>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN),
+                          amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU)))
+void mx_grad_kernel(MxArgs a) {
+    constexpr bool DW = OP == MX_DW;
+    constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+    constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int BK = 64;
+    constexpr int A_STAGE = BM * 128;
+    constexpr int A_PITCH = DW ? BM * 2 : 128, A_CPR = A_PITCH / 16;
+    constexpr int A_INSTR = A_STAGE / 1024 / WAVES;
+    constexpr int BLOCKS = BN / kMxBlock, REGION = BK * 64 + 64;
+    constexpr int CODES = DW ? 32 : 16;                      // bytes of a block's codes
+    constexpr int RAW = CODES / 16 + 1;                      // loads per thread and stage: codes and a scale
+    static_assert(A_INSTR >= 1 && A_INSTR * 1024 * WAVES == A_STAGE, "A stage split");
+    static_assert(BK * BLOCKS == THREADS, "one block of one row per thread");
+
+    __shared__ __attribute__((aligned(1024))) uint8_t a_lds0[A_STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t a_lds1[A_STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t b_lds0[BLOCKS * REGION];
+    __shared__ __attribute__((aligned(1024))) uint8_t b_lds1[BLOCKS * REGION];
+
+    const int tid = int(threadIdx.x), lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave_m = wave / WN, wave_n = wave % WN;
+    int tm, tn, slice;
+    map_tile(a.g, tm, tn, slice);
+    const int64_t M = a.g.M, N = a.g.N;
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+    const int64_t k_begin = int64_t(slice) * a.g.k_chunk;
+    const int64_t k_end = k_begin + a.g.k_chunk < a.g.K ? k_begin + a.g.k_chunk : a.g.K;
+    const int k_len = k_end > k_begin ? int(k_end - k_begin) : 0;
+    const int nk = (k_len + BK - 1) / BK;
+    const int64_t lda_b = a.g.lda * 2, ldq = a.g.ldb, lds_ = a.ld_scales;
+
+    // ---- A: this lane's pieces of a stage.
+    const uint32_t a_bytes = uint32_t(((M - m0) < BM ? (M - m0) : BM) * lda_b);     // DX: rows past M read zeros
+    uint32_t a_voff[A_INSTR];
+    int a_k[A_INSTR];
+#pragma unroll
+    for (int i = 0; i < A_INSTR; ++i) {
+        if constexpr (DW) {
+            const int row = (i * WAVES + wave) * (64 / A_CPR) + lane / A_CPR;
+            const int c = (lane % A_CPR) ^ ring_bswz<DT_BF16, A_CPR>(row);
+            a_k[i] = row;
+            a_voff[i] = m0 + 8 * c < M ? uint32_t(row * lda_b + 16 * c) : kOOB;
+        } else {
+            const int row = (i * WAVES + wave) * 8 + (lane >> 3);
+            const int c = swz(lane & 7, row);
+            a_k[i] = 8 * c;
+            a_voff[i] = uint32_t(row * lda_b + 16 * c);
+        }
+    }
+    const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + (DW ? k_begin * lda_b + m0 * 2 : m0 * lda_b + k_begin * 2);
+    auto load_a = [&](int kt, auto buf_c) {
+        constexpr int BUF = decltype(buf_c)::value;
+        const int rem = k_len - kt * BK;
+        const uint32_t dst = lds_addr(BUF ? a_lds1 : a_lds0) + uint32_t(wave) * 1024u;
+        const i32x4_t ra = DW ? ring_rsrc(a_base + int64_t(kt) * BK * lda_b,
+                                          uint32_t(__builtin_amdgcn_readfirstlane(int((rem <= 0 ? 0 : rem < BK ? rem : BK) * lda_b))))
+                              : ring_rsrc(a_base + int64_t(kt) * 128, rem > 0 ? a_bytes : 0u);
+#pragma unroll
+        for (int i = 0; i < A_INSTR; ++i)
+            ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
+    };
+
+    // ---- B: this thread's block of row b_row of each stage.
+    const int b_row = tid / BLOCKS, b_blk = tid % BLOCKS;
+    const bool b_in = n0 + b_blk * kMxBlock < N;
+    const uint32_t q_off = uint32_t(b_row * ldq + b_blk * CODES), s_off = uint32_t(b_row * lds_ + b_blk);
+    const uint8_t *const q_base = static_cast<const uint8_t *>(a.g.B) + k_begin * ldq + (DW ? n0 : n0 / 2);
+    const uint8_t *const s_base = a.scales + k_begin * lds_ + n0 / kMxBlock;
+    // The second half of a block's 8-bit codes may lie past N.
+    const bool b_in2 = n0 + b_blk * kMxBlock + 16 < N;
+    u32x4_t raw[2][CODES / 16];
+    uint32_t raw_scale[2];
+    auto load_b = [&](int kt, auto set_c) {
+        constexpr int SET = decltype(set_c)::value;
+        const bool in = b_in && kt * BK + b_row < k_len;
+        const __amdgpu_buffer_rsrc_t rq = make_rsrc(q_base + int64_t(kt) * BK * ldq, kOOB);
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(s_base + int64_t(kt) * BK * lds_, kOOB);
+        raw[SET][0] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rq, int(in ? q_off : kOOB), 0, 0));
+        if constexpr (DW)
+            raw[SET][1] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rq, int(in && b_in2 ? q_off + 16 : kOOB), 0, 0));
+        raw_scale[SET] = __builtin_amdgcn_raw_buffer_load_b8(rs, int(in ? s_off : kOOB), 0, 0);
+    };
+    const int b_wo = b_blk * REGION + b_row * 64, b_flip = (b_blk >> 2) & 1;
+    // Chunk t (eight columns) of the thread's block, converted and written.
+    auto write_b = [&](auto set_c, auto buf_c, auto t_c) {
+        constexpr int SET = decltype(set_c)::value, T = decltype(t_c)::value;
+        uint8_t *const dst = decltype(buf_c)::value ? b_lds1 : b_lds0;
+        u32x4_t v;
+        if constexpr (DW) {
+            const float s = mx_scale(raw_scale[SET]);
+            const u32x2_t lo = mx8_to_bf16(raw[SET][T / 2][2 * (T & 1)], s), hi = mx8_to_bf16(raw[SET][T / 2][2 * (T & 1) + 1], s);
+            v = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            v = mx4_to_bf16(raw[SET][0][T], mx4_scale(raw_scale[SET]));
+        }
+        *reinterpret_cast<u32x4_t *>(dst + b_wo + 16 * (T ^ b_flip)) = v;
+    };
+
+    // ---- fragments
+    const int frag_row = lane & 31, half = lane >> 5;
+    const int wrow0 = wave_m * (BM / WM), wcol0 = wave_n * (BN / WN);
+    const int r0 = wrow0 + frag_row;
+    const int grp = lane >> 4, g16 = lane & 15;
+    const int tr_row = g16 >> 2, tr_k = (grp >> 1) * 8 + tr_row;      // row of a transpose read, in the k-step
+    int a_fo[DW ? TM : 2][4];
+    if constexpr (DW) {
+        const int bz = ring_bswz<DT_BF16, A_CPR>(tr_row);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int colb = (wrow0 + 32 * i) * 2 + (g16 & 3) * 8 + (grp & 1) * 32;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) a_fo[i][s] = (16 * s + tr_k) * A_PITCH + (((colb >> 4) ^ bz) << 4) + (colb & 15);
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) a_fo[p][s] = r0 * 128 + 16 * (swz(2 * s + half, r0) ^ (4 * p));
+    }
+    int b_fo[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int blk = wcol0 / 32 + j;
+        b_fo[j] = blk * REGION + tr_k * 64 + 16 * ((2 * (grp & 1) + ((g16 & 3) >> 1)) ^ ((blk >> 2) & 1)) + 8 * (g16 & 1);
+    }
+    u32x4_t fa[2][TM], fb[2][TN];
+    auto load_frags = [&](auto buf_c, auto s_c, auto slot_c) {
+        constexpr int S = decltype(s_c)::value, SLOT = decltype(slot_c)::value;
+        const uint8_t *const as = decltype(buf_c)::value ? a_lds1 : a_lds0;
+        const uint8_t *const bs = decltype(buf_c)::value ? b_lds1 : b_lds0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            if constexpr (DW) {
+                const u32x2_t lo = lds_read_tr<DT_BF16>(as + a_fo[i][S]), hi = lds_read_tr<DT_BF16>(as + a_fo[i][S] + 4 * A_PITCH);
+                fa[SLOT][i] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+            } else {
+                fa[SLOT][i] = *reinterpret_cast<const u32x4_t *>(as + a_fo[i & 1][S] + 4096 * i);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const u32x2_t lo = lds_read_tr<DT_BF16>(bs + b_fo[j] + S * 1024), hi = lds_read_tr<DT_BF16>(bs + b_fo[j] + S * 1024 + 256);
+            fb[SLOT][j] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+        }
+    };
+    f32x16_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[1][i] = u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[1][j] = u32x4_t{0u, 0u, 0u, 0u};
+    auto multiply = [&](auto slot_c) {
+        constexpr int SLOT = decltype(slot_c)::value;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma32<DT_BF16>(fa[SLOT][i], fb[SLOT][j], acc[i][j]);
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+
+    // K ends inside a chunk of A's rows: what follows it is not part of the sum.
+    auto cut_a = [&](int kt, auto buf_c) {
+        if constexpr (!DW) {
+            if (kt != nk - 1 || (k_len & 7) == 0) return;
+            uint8_t *const as = decltype(buf_c)::value ? a_lds1 : a_lds0;
+            const int kl = k_len - kt * BK;
+            for (int r = tid; r < BM; r += THREADS)
+                for (int e = kl & 7; e < 8; ++e) reinterpret_cast<uint16_t *>(as + r * 128 + 16 * swz(kl / 8, r))[e] = 0;
+            phase_barrier();
+        }
+    };
+    // One stage: buffer BUF holds stage kt, set 1 - BUF the codes of stage kt + 1.  On entry
+    // slot 1 holds the fragments of the stage before's last k-step, whose MFMAs run under the
+    // latency of this stage's first reads.
+    auto stage = [&](int kt, auto buf_c) {
+        constexpr int BUF = decltype(buf_c)::value;
+        using OTHER = std::integral_constant<int, 1 - BUF>;
+        cut_a(kt, buf_c);
+        // The codes of stage kt + 1 have arrived (loaded a stage ago): said here, before the
+        // loads below, so that their use does not wait for those.
+#pragma unroll
+        for (int i = 0; i < CODES / 16; ++i) asm volatile("" : "+v"(raw[1 - BUF][i]));
+        asm volatile("" : "+v"(raw_scale[1 - BUF]));
+        load_a(kt + 1, OTHER{});
+        load_b(kt + 2, buf_c);
+        load_frags(buf_c, I0{}, I0{});
+        write_b(OTHER{}, OTHER{}, I0{});
+        multiply(I1{});
+        load_frags(buf_c, I1{}, I1{});
+        write_b(OTHER{}, OTHER{}, I1{});
+        multiply(I0{});
+        load_frags(buf_c, I2{}, I0{});
+        write_b(OTHER{}, OTHER{}, I2{});
+        multiply(I1{});
+        load_frags(buf_c, I3{}, I1{});
+        write_b(OTHER{}, OTHER{}, I3{});
+        multiply(I0{});
+        ring_barrier<RAW>();              // A of stage kt + 1 is in LDS; the codes of kt + 2 may be on their way
+    };
+
+    if (nk > 0) {
+        load_b(0, I0{});
+        load_b(1, I1{});
+        load_a(0, I0{});
+        static_for<0, 4>([&](auto t) { write_b(I0{}, I0{}, t); });
+        stage_barrier();
+        int kt = 0;
+        for (; kt + 1 < nk; kt += 2) {
+            stage(kt, I0{});
+            stage(kt + 1, I1{});
+        }
+        if (kt < nk) stage(kt, I0{});
+        multiply(I1{});
+    }
+    stage_barrier();
+    store_tile<DT_BF16, BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, *reinterpret_cast<int *>(a_lds0));
+}
+
+}  // namespace gemm

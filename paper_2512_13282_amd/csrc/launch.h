@@ -2,6 +2,7 @@
 // Pure C++: no HIP types, so the API file builds without HIP headers.
 #pragma once
 
+#include <stddef.h>
 #include <stdint.h>
 
 namespace gemm {
@@ -49,7 +50,7 @@ enum { REDUCE_SEPARATE = 0, REDUCE_LAST_SLICE = 1, REDUCE_ATOMIC = 2, REDUCE_ATO
 // atomics behind each other (a GEMV with 32 slices per tile ran 1.9x slower).
 constexpr int kFlagCounterStride = 32;
 
-enum { LAUNCH_OK = 0, LAUNCH_HIP_ERROR = 1, LAUNCH_NO_MEMORY = 2, LAUNCH_SCRATCH_LIMIT = 3, LAUNCH_NO_COUNTERS = 4 };
+enum { LAUNCH_OK = 0, LAUNCH_HIP_ERROR = 1, LAUNCH_NO_MEMORY = 2, LAUNCH_SCRATCH_LIMIT = 3, LAUNCH_NO_COUNTERS = 4, LAUNCH_UNSUPPORTED = 5 };
 
 // The fixed split-K scratch of the entry point that allocates nothing: per device,
 // kScratchCounterBytes of per-tile arrival counters followed by the partial planes.
@@ -63,6 +64,12 @@ constexpr int64_t kScratchCounterBytes = int64_t(64) << 10;
 // `stream` is being captured and its workspace holds too few counters, the reductions that
 // need none take the place of those that do.
 int launch_gemm(const KernelArgs &a, int32_t config, int64_t grid, void *stream, bool static_scratch = false);
+
+// The workspace of `stream` on the current device, grown where it is too small: at least
+// partial_bytes of scratch and counter_words arrival counters, zero between launches.
+// LAUNCH_NO_COUNTERS, and nothing queued, where the counters would have to grow while the
+// stream is being captured.
+int acquire_workspace(void *stream, size_t partial_bytes, int64_t counter_words, void **partials, uint32_t **counters);
 
 // Frees every cached split-K workspace (all devices and streams) after
 // synchronising each device that holds one.

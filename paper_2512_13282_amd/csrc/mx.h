@@ -33,9 +33,30 @@ struct MxMatrixArgs {          // packing and unpacking
     int64_t ld_scales;         // bytes
 };
 
+// How a product runs: a row of kMxConfigs and the number of K slices.
+struct MxPlan {
+    int32_t config;
+    int32_t split_k;
+    int64_t k_chunk;           // K of a slice, a multiple of 256
+};
+
+struct MxConfig {
+    MxOp op;
+    int32_t bm, bn;            // output tile
+    int32_t waves;             // per workgroup
+    int32_t occupancy;         // workgroups a compute unit holds
+    const char *name;
+};
+extern const MxConfig kMxConfigs[];
+extern const int32_t kMxNumConfigs;
+
+// The plan for a product.  config >= 0 and split > 0 say which one to evaluate instead.
+// False where that configuration is not the operator's, or cannot hold the rows.
+bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, MxPlan *out);
+
 // Each queues its kernels on `stream` (a hipStream_t) and returns a LAUNCH_* value.
 int launch_mx_pack(const MxMatrixArgs &a, int bits, void *stream);
 int launch_mx_unpack(const MxMatrixArgs &a, int bits, void *stream);
-int launch_mx_gemm(const MxArgs &a, MxOp op, void *stream);
+int launch_mx_gemm(const MxArgs &a, MxOp op, const MxPlan &plan, void *stream);
 
 }  // namespace gemm

@@ -1,6 +1,9 @@
 // mx_api.cpp -- the C ABI entry points of the block-scaled products (host side): argument
 // checks before any HIP call, then the launch.
 #include <stdint.h>
+#include <string.h>
+
+#include <atomic>
 
 #include "../../include/mx_mi355x.h"
 #include "mx.h"
@@ -39,6 +42,7 @@ int status(int launched) {
     switch (launched) {
         case gemm::LAUNCH_OK: return GEMM_OK;
         case gemm::LAUNCH_NO_MEMORY: return GEMM_ERR_NO_MEMORY;
+        case gemm::LAUNCH_UNSUPPORTED: return GEMM_ERR_UNSUPPORTED;
         default: return GEMM_ERR_HIP;
     }
 }
@@ -57,6 +61,16 @@ int convert(bool pack, int bits, int64_t rows, int64_t cols, const void *x, int6
     return status(pack ? gemm::launch_mx_pack(a, bits, stream) : gemm::launch_mx_unpack(a, bits, stream));
 }
 
+struct Forced {
+    std::atomic<int32_t> config{-1}, split{0};
+};
+Forced g_forced[3];
+
+int plan_for(gemm::MxOp op, int64_t M, int64_t N, int64_t K, gemm::MxPlan *plan) {
+    if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX - 4096) return GEMM_ERR_UNSUPPORTED;    // 32-bit indices
+    return gemm::mx_select(op, M, N, K, g_forced[op].config, g_forced[op].split, plan) ? GEMM_OK : GEMM_ERR_UNSUPPORTED;
+}
+
 int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const void *codes,
             int64_t ldq, const uint8_t *scales, int64_t lds, void *C, int64_t ldc, bool bf16_out, void *stream) {
     if (M < 0 || N < 0 || K < 0) return GEMM_ERR_INVALID_VALUE;
@@ -69,6 +83,9 @@ int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, i
     if (!ra.valid() || !rq.valid() || !rs.valid() || !rc.valid()) return GEMM_ERR_INVALID_VALUE;
     if (rc.overlaps(ra) || rc.overlaps(rq) || rc.overlaps(rs)) return GEMM_ERR_INVALID_VALUE;
     if (M == 0 || N == 0) return GEMM_OK;
+    gemm::MxPlan plan;
+    const int planned = plan_for(op, M, N, K, &plan);
+    if (planned != GEMM_OK) return planned;
     gemm::MxArgs a{};
     a.g.dtype = 1;      // bf16 operands on the MFMAs
     a.g.A = A;
@@ -79,7 +96,7 @@ int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, i
     a.g.epilogue = bf16_out ? gemm::EPI_BF16 : gemm::EPI_NONE;
     a.scales = scales;
     a.ld_scales = lds;
-    return status(gemm::launch_mx_gemm(a, op, stream));
+    return status(gemm::launch_mx_gemm(a, op, plan, stream));
 }
 
 }  // namespace
@@ -134,6 +151,34 @@ int mx_gemm_bf16_mx8_f32_at(int64_t M, int64_t N, int64_t K, const uint16_t *At,
 int mx_gemm_bf16_mx8_bf16_at(int64_t M, int64_t N, int64_t K, const uint16_t *At, int64_t ldat, const int8_t *codes,
                              int64_t ldq, const uint8_t *scales, int64_t lds, uint16_t *C, int64_t ldc, void *stream) {
     return product(gemm::MX_DW, M, N, K, At, ldat, codes, ldq, scales, lds, C, ldc, true, stream);
+}
+
+int mx_plan(int op, int64_t M, int64_t N, int64_t K, mx_plan_info *out) {
+    if (out == nullptr || op < MX_OP_FORWARD || op > MX_OP_WEIGHT_GRADIENT || M < 0 || N < 0 || K < 0)
+        return GEMM_ERR_INVALID_VALUE;
+    memset(out, 0, sizeof(*out));
+    out->config = -1;
+    if (M == 0 || N == 0) return GEMM_OK;
+    gemm::MxPlan plan;
+    const int rc = plan_for(gemm::MxOp(op), M, N, K, &plan);
+    if (rc != GEMM_OK) return rc;
+    const gemm::MxConfig &c = gemm::kMxConfigs[plan.config];
+    out->config = plan.config;
+    out->bm = c.bm;
+    out->bn = c.bn;
+    out->split_k = plan.split_k;
+    out->k_chunk = plan.k_chunk;
+    strncpy(out->name, c.name, sizeof(out->name) - 1);
+    return GEMM_OK;
+}
+
+int mx_force_plan(int op, int config, int split_k) {
+    if (op < MX_OP_FORWARD || op > MX_OP_WEIGHT_GRADIENT || config < -1 || config >= gemm::kMxNumConfigs || split_k < 0 ||
+        (config >= 0 && gemm::kMxConfigs[config].op != op))
+        return GEMM_ERR_INVALID_VALUE;
+    g_forced[op].config = config;
+    g_forced[op].split = split_k;
+    return GEMM_OK;
 }
 
 }  // extern "C"

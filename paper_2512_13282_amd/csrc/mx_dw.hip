@@ -1,0 +1,18 @@
+// mx_dw.hip -- instances of the gradient kernel, weight gradients over 8-bit checkpoints.
+#include "kern_mx_tile.h"
+#include "mx_launch.h"
+
+namespace gemm {
+
+hipError_t launch_mx_dw(int32_t cfg, const MxArgs &a, int64_t grid, hipStream_t s) {
+    const dim3 g{unsigned(grid)};
+    switch (cfg) {
+        case 10: return launch_mx(mx_grad_kernel<MX_DW, 32, 128, 1, 4, 3>, a, g, 256, 0, s);
+        case 11: return launch_mx(mx_grad_kernel<MX_DW, 64, 128, 2, 2, 3>, a, g, 256, 0, s);
+        case 12: return launch_mx(mx_grad_kernel<MX_DW, 128, 128, 2, 2, 2>, a, g, 256, 0, s);
+        case 13: return launch_mx(mx_grad_kernel<MX_DW, 256, 256, 2, 4, 2>, a, g, 512, 0, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace gemm

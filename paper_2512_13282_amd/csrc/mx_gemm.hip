@@ -1,41 +1,103 @@
-// mx_gemm.hip -- the products over block-scaled operands.
-#include "mx_common.h"
+// mx_gemm.hip -- launches the products over block-scaled operands.
+#include "families.h"
+#include "mx_launch.h"
 
 namespace gemm {
 
-__device__ __forceinline__ float mx_element(const MxArgs &a, MxOp op, int64_t row, int64_t col) {
-    const uint32_t e = a.scales[row * a.ld_scales + col / kMxBlock];
-    const uint8_t *const codes = static_cast<const uint8_t *>(a.g.B) + row * a.g.ldb;
-    if (op == MX_DW) return float(int8_t(codes[col])) * mx_scale(e);
-    const uint32_t pair = codes[col / 2];
-    const uint32_t v = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(pair, mx4_scale(e), 0));
-    return bf16_to_f32(col & 1 ? v >> 16 : v & 0xffffu);
-}
-
-// One thread per element of C.
-template <int OP>
-__global__ __launch_bounds__(256) void mx_element_kernel(MxArgs a) {
-    const int64_t total = a.g.M * a.g.N, stride = int64_t(gridDim.x) * 256;
-    const uint16_t *const A = static_cast<const uint16_t *>(a.g.A);
-    for (int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x; id < total; id += stride) {
-        const int64_t i = id / a.g.N, j = id - i * a.g.N;
-        float sum = 0.0f;
-        for (int64_t k = 0; k < a.g.K; ++k) {
-            const float x = bf16_to_f32(OP == MX_DW ? A[k * a.g.lda + i] : A[i * a.g.lda + k]);
-            sum = fmaf(x, OP == MX_FWD ? mx_element(a, MX_FWD, j, k) : mx_element(a, MxOp(OP), k, j), sum);
+// Rows of `used` bytes at any address and stride, copied to rows of `pitch` bytes (a multiple
+// of 16) on 16-byte addresses, zeros behind each row: what the tile kernels load straight into
+// LDS, 16 aligned bytes at a time.
+__global__ __launch_bounds__(256) void mx_realign_kernel(const uint8_t *src, int64_t stride, int64_t used, uint8_t *dst,
+                                                         int64_t pitch, int64_t rows) {
+    const int64_t pieces = pitch / 16, total = rows * pieces, step = int64_t(gridDim.x) * 256;
+    for (int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x; id < total; id += step) {
+        const int64_t r = id / pieces, c = id - r * pieces;
+        const uint8_t *const p = src + r * stride + 16 * c;
+        const int64_t left = used - 16 * c;
+        u32x4_t v{0u, 0u, 0u, 0u};
+        if (left >= 16) {
+            v = *reinterpret_cast<const u32x4_any_mx *>(p);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (e < left) v[e / 4] |= uint32_t(p[e]) << (8 * (e & 3));
         }
-        write_c<DT_BF16>(a.g, i * a.g.ldc + j, sum);
+        *reinterpret_cast<u32x4_t *>(dst + r * pitch + 16 * c) = v;
     }
 }
 
-int launch_mx_gemm(const MxArgs &a, MxOp op, void *stream_ptr) {
+namespace {
+// An operand as the tile kernels need it: rows on 16-byte addresses, no further apart than
+// 32-bit offsets within a tile allow.
+bool loadable(const void *p, int64_t stride) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0 && stride <= (int64_t(1) << 22);
+}
+int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+bool realign(const void *src, int64_t stride, int64_t used, void *dst, int64_t rows, hipStream_t stream) {
+    const int64_t n = (rows * (padded(used) / 16) + 255) / 256;
+    hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream,
+                       static_cast<const uint8_t *>(src), stride, used, static_cast<uint8_t *>(dst), padded(used), rows);
+    return hipGetLastError() == hipSuccess;
+}
+}  // namespace
+
+int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_ptr) {
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
-    const int64_t n = (a.g.M * a.g.N + 255) / 256;
-    const dim3 grid(unsigned(n < (int64_t(1) << 20) ? n : (int64_t(1) << 20)));
-    if (op == MX_FWD) hipLaunchKernelGGL(mx_element_kernel<MX_FWD>, grid, dim3(256), 0, stream, a);
-    else if (op == MX_DX) hipLaunchKernelGGL(mx_element_kernel<MX_DX>, grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(mx_element_kernel<MX_DW>, grid, dim3(256), 0, stream, a);
-    return hipGetLastError() == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
+    MxArgs a = a0;
+    const MxConfig &c = kMxConfigs[plan.config];
+    const bool decode = plan.config < 2;
+    const int64_t tm = decode ? 1 : (a.g.M + c.bm - 1) / c.bm, tn = (a.g.N + c.bn - 1) / c.bn;
+    const int64_t grid = tm * tn * plan.split_k;
+    if (grid > 0x7fffffff) return LAUNCH_HIP_ERROR;
+    a.g.k_chunk = plan.k_chunk;
+    a.g.split_k = plan.split_k;
+    a.g.tiles_m = int32_t(tm);
+    a.g.tiles_n = int32_t(tn);
+    a.g.group_m = 4;
+    a.g.reduce_in_kernel = REDUCE_LAST_SLICE;
+
+    // Scratch: the K slices' partial sums, and aligned copies of operands that need one.
+    const int64_t a_rows = op == MX_DW ? a.g.K : a.g.M, a_used = (op == MX_DW ? a.g.M : a.g.K) * 2;
+    const int64_t b_rows = op == MX_FWD ? a.g.N : a.g.K, b_cols = op == MX_FWD ? a.g.K : a.g.N;
+    const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2;
+    const bool copy_a = !decode && a.g.K > 0 && !loadable(a.g.A, a.g.lda * 2);
+    const bool copy_b = !decode && a.g.K > 0 && !loadable(a.g.B, a.g.ldb);
+    const int64_t partial = a.g.split_k > 1 ? padded(a.g.split_k * a.g.M * a.g.N * 4) : 0;
+    const int64_t a_bytes = copy_a ? a_rows * padded(a_used) : 0, b_bytes = copy_b ? b_rows * padded(b_used) : 0;
+    if ((copy_a && padded(a_used) > (int64_t(1) << 22)) || (copy_b && padded(b_used) > (int64_t(1) << 22)))
+        return LAUNCH_UNSUPPORTED;
+    if (partial + a_bytes + b_bytes > 0) {
+        void *ws = nullptr;
+        uint32_t *counters = nullptr;
+        const size_t bytes = size_t(partial + a_bytes + b_bytes);
+        int rc = acquire_workspace(stream_ptr, bytes, a.g.split_k > 1 ? tm * tn : 0, &ws, &counters);
+        if (rc == LAUNCH_NO_COUNTERS) {
+            a.g.reduce_in_kernel = REDUCE_SEPARATE;     // the same sums in the same order
+            rc = acquire_workspace(stream_ptr, bytes, 0, &ws, &counters);
+        }
+        if (rc != LAUNCH_OK) return rc;
+        a.g.workspace = ws;
+        a.g.counters = counters;
+        uint8_t *const copies = static_cast<uint8_t *>(ws) + partial;
+        if (copy_a) {
+            if (!realign(a.g.A, a.g.lda * 2, a_used, copies, a_rows, stream)) return LAUNCH_HIP_ERROR;
+            a.g.A = copies;
+            a.g.lda = padded(a_used) / 2;
+        }
+        if (copy_b) {
+            if (!realign(a.g.B, a.g.ldb, b_used, copies + a_bytes, b_rows, stream)) return LAUNCH_HIP_ERROR;
+            a.g.B = copies + a_bytes;
+            a.g.ldb = padded(b_used);
+        }
+    }
+    hipError_t e = op == MX_FWD ? launch_mx_fwd(plan.config, a, grid, stream)
+                 : op == MX_DX ? launch_mx_dx(plan.config, a, grid, stream) : launch_mx_dw(plan.config, a, grid, stream);
+    if (e == hipSuccess && a.g.split_k > 1 && a.g.reduce_in_kernel == REDUCE_SEPARATE) {
+        int64_t blocks = (a.g.M * a.g.N + 255) / 256;
+        e = launch_splitk_reduce<DT_BF16>(a.g, blocks < 8192 ? blocks : 8192, stream);
+    }
+    return e == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
 }
 
 }  // namespace gemm

@@ -1,0 +1,57 @@
+// mx_plan.cpp -- how the block-scaled products choose their kernel, tile and K slices (host).
+#include "mx.h"
+
+namespace gemm {
+
+// Rows 0 and 1 are the decode kernels (at most kMxDecodeRows rows of A), the rest output tiles.
+const MxConfig kMxConfigs[] = {
+    {MX_FWD, 16, 16, 4, 8, "mx_decode_16_w4"},
+    {MX_FWD, 16, 16, 8, 4, "mx_decode_16_w8"},
+    {MX_FWD, 32, 128, 4, 2, "mx_fwd_32x128"},
+    {MX_FWD, 64, 128, 4, 2, "mx_fwd_64x128"},
+    {MX_FWD, 128, 128, 4, 2, "mx_fwd_128x128"},
+    {MX_FWD, 256, 256, 8, 1, "mx_fwd_256x256"},
+    {MX_DX, 32, 128, 4, 3, "mx_dx_32x128"},
+    {MX_DX, 64, 128, 4, 2, "mx_dx_64x128"},
+    {MX_DX, 128, 128, 4, 2, "mx_dx_128x128"},
+    {MX_DX, 256, 256, 8, 1, "mx_dx_256x256"},
+    {MX_DW, 32, 128, 4, 3, "mx_dw_32x128"},
+    {MX_DW, 64, 128, 4, 2, "mx_dw_64x128"},
+    {MX_DW, 128, 128, 4, 2, "mx_dw_128x128"},
+    {MX_DW, 256, 256, 8, 1, "mx_dw_256x256"},
+};
+const int32_t kMxNumConfigs = sizeof(kMxConfigs) / sizeof(kMxConfigs[0]);
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+static bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPlan *out) {
+    if (config < 0 || config >= kMxNumConfigs || kMxConfigs[config].op != op) return false;
+    const bool decode = config < 2;
+    if (decode) {
+        // A's slice has to fit 64 KiB of LDS.
+        if (M > 16 || K == 0) return false;
+        const int64_t most = (65536 / M - 16) / 256 * 128;
+        const int64_t least = ceil_div(K, most);
+        if (split < least) split = int32_t(least);
+    }
+    const int64_t unit = decode ? 128 : 256;
+    const int64_t chunk = K > 0 ? ceil_div(ceil_div(K, unit), split) * unit : unit;
+    out->config = config;
+    out->k_chunk = chunk;
+    out->split_k = int32_t(K > 0 ? ceil_div(K, chunk) : 1);
+    return true;
+}
+
+bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, MxPlan *out) {
+    if (config >= 0) return evaluate(op, M, K, config, split > 0 ? split : 1, out);
+    if (op == MX_FWD && M <= 4 && K > 0) return evaluate(op, M, K, N >= 8192 ? 0 : 1, 1, out);
+    const int first = op == MX_FWD ? 2 : op == MX_DX ? 6 : 10;
+    const int at = M <= 32 ? 0 : M <= 64 ? 1 : M <= 512 || N <= 1024 ? 2 : 3;
+    const MxConfig &c = kMxConfigs[first + at];
+    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(N, c.bn);
+    int64_t s = 256 * c.occupancy / tiles;
+    if (s > ceil_div(K, 512)) s = ceil_div(K, 512);
+    return evaluate(op, M, K, first + at, int32_t(split > 0 ? split : s < 1 ? 1 : s > 32 ? 32 : s), out);
+}
+
+}  // namespace gemm

@@ -20,8 +20,16 @@ from . import binding as _b
 
 EXPORTED = ("mx_pack4", "mx_pack8", "mx_unpack4", "mx_unpack8",
             "mx_gemm_bf16_mx4_f32_bt", "mx_gemm_bf16_mx4_bf16_bt", "mx_gemm_bf16_mx4_f32",
-            "mx_gemm_bf16_mx4_bf16", "mx_gemm_bf16_mx8_f32_at", "mx_gemm_bf16_mx8_bf16_at")
+            "mx_gemm_bf16_mx4_bf16", "mx_gemm_bf16_mx8_f32_at", "mx_gemm_bf16_mx8_bf16_at",
+            "mx_plan", "mx_force_plan")
 BLOCK = 32
+MX_OP_FORWARD, MX_OP_INPUT_GRADIENT, MX_OP_WEIGHT_GRADIENT = range(3)
+
+
+class PlanInfo(ctypes.Structure):
+    _fields_ = [("config", ctypes.c_int32), ("bm", ctypes.c_int32), ("bn", ctypes.c_int32),
+                ("split_k", ctypes.c_int32), ("k_chunk", ctypes.c_int64), ("name", ctypes.c_char * 48)]
+
 
 _fns = None
 
@@ -39,6 +47,8 @@ def lib():
             fn.argtypes = [i64, i64, i64, p, i64, p, i64, p, i64, p, i64, p] if "gemm" in name else \
                 [i64, i64, p, i64, p, i64, p, i64, p]
             fns[name] = fn
+        fns["mx_plan"].argtypes = [ctypes.c_int, i64, i64, i64, ctypes.POINTER(PlanInfo)]
+        fns["mx_force_plan"].argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int]
         _fns = fns
     return _fns
 
@@ -60,7 +70,20 @@ def _product(name):
 
 mx_pack4, mx_pack8, mx_unpack4, mx_unpack8 = map(_convert, EXPORTED[:4])
 (mx_gemm_bf16_mx4_f32_bt, mx_gemm_bf16_mx4_bf16_bt, mx_gemm_bf16_mx4_f32, mx_gemm_bf16_mx4_bf16,
- mx_gemm_bf16_mx8_f32_at, mx_gemm_bf16_mx8_bf16_at) = map(_product, EXPORTED[4:])
+ mx_gemm_bf16_mx8_f32_at, mx_gemm_bf16_mx8_bf16_at) = map(_product, EXPORTED[4:10])
+
+
+def mx_plan(op, M, N, K) -> dict:
+    """The plan of a product (MX_OP_*) as a dict; raises GemmError on a bad argument."""
+    info = PlanInfo()
+    rc = lib()["mx_plan"](op, M, N, K, ctypes.byref(info))
+    if rc != _b.GEMM_OK:
+        raise _b.GemmError(rc)
+    return {f: getattr(info, f) for f, _ in PlanInfo._fields_} | {"name": info.name.decode()}
+
+
+def mx_force_plan(op, config=-1, split_k=0) -> int:
+    return lib()["mx_force_plan"](op, config, split_k)
 
 
 class MxMatrix(NamedTuple):

@@ -239,6 +239,43 @@ def test_same_bits_on_every_run_and_stream(op, size):
             assert np.array_equal(run_product(op, M, N, K, a, codes, scales, False), first)
 
 
+def configurations(op):
+    """The configurations of an operator (mx_force_plan refuses those of another)."""
+    found = [c for c in range(64) if mx.mx_force_plan(OPS.index(op), c, 0) == b.GEMM_OK]
+    mx.mx_force_plan(OPS.index(op))
+    return found
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("size", [(1, 33, 640), (5, 257, 1029), (13, 130, 2500), (16, 64, 4400), (77, 390, 1537), (300, 270, 1100)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_every_configuration_and_split(op, size):
+    """Each kernel where it would not be chosen too, with K whole and in slices; captured or not, a
+    split sums in the same order."""
+    M, N, K = size
+    a, codes, scales, cols = operands(op, M, N, K, sum(size))
+    want, magnitude = ref.product(op, ref.widen(a), ref.values(codes, scales, cols))
+    lim = ref.bound(K, magnitude, want, False)
+    ran = 0
+    try:
+        for config in configurations(op):
+            for split in (1, 2, 3, 7):
+                assert mx.mx_force_plan(OPS.index(op), config, split) == b.GEMM_OK
+                try:
+                    plan = mx.mx_plan(OPS.index(op), M, N, K)
+                except b.GemmError as e:
+                    assert e.status == b.GEMM_ERR_UNSUPPORTED and M > 16
+                    continue
+                assert plan["config"] == config and plan["split_k"] >= min(split, 2 if K > 256 else 1)
+                C = run_product(op, M, N, K, a, codes, scales, False, pads=(0, 0, 0, 1))
+                off = np.abs(C - want)
+                assert np.all(off <= lim), (plan, float((off / lim).max()), np.argwhere(~(off <= lim))[:4].tolist())
+                ran += 1
+    finally:
+        mx.mx_force_plan(OPS.index(op))
+    assert ran >= 16
+
+
 # ---------------------------------------------------------------- the torch helpers
 
 def packed(rows, cols, width, seed):

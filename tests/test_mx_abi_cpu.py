@@ -114,3 +114,28 @@ def test_helpers_refuse_what_is_not_theirs():
         mx.linear_mx4(x, q4)                    # not on a GPU
     with pytest.raises(ValueError):
         mx.linear_mx4(x[0], q4)                 # no matrix
+
+
+def test_plans_and_their_hook():
+    for op in (mx.MX_OP_FORWARD, mx.MX_OP_INPUT_GRADIENT, mx.MX_OP_WEIGHT_GRADIENT):
+        for M, N, K in ((1, 14336, 4096), (16, 4096, 14336), (77, 130, 1), (2048, 11008, 4096), (5, 5, 0)):
+            plan = mx.mx_plan(op, M, N, K)
+            assert plan["config"] >= 0 and plan["name"].startswith("mx_") and plan["split_k"] >= 1
+            # The slices cover K, and none of them is empty.
+            assert plan["split_k"] * plan["k_chunk"] >= K and (K == 0 or (plan["split_k"] - 1) * plan["k_chunk"] < K)
+        assert mx.mx_plan(op, 0, 5, 5)["config"] == -1
+        for bad in ((-1, 1, 1), (1, -1, 1), (1, 1, -1)):
+            with pytest.raises(b.GemmError):
+                mx.mx_plan(op, *bad)
+        with pytest.raises(b.GemmError) as e:
+            mx.mx_plan(op, 1 << 31, 1, 1)
+        assert e.value.status == b.GEMM_ERR_UNSUPPORTED
+        config = mx.mx_plan(op, 300, 300, 3000)["config"]
+        assert mx.mx_force_plan((op + 1) % 3, config) == BAD
+        try:
+            assert mx.mx_force_plan(op, config, 3) == b.GEMM_OK
+            assert mx.mx_plan(op, 5, 5, 3000)["config"] == config and mx.mx_plan(op, 5, 5, 3000)["split_k"] == 3
+        finally:
+            assert mx.mx_force_plan(op) == b.GEMM_OK
+    for bad in ((3, -1, 0), (-1, -1, 0), (0, 64, 0), (0, -2, 0), (0, -1, -1)):
+        assert mx.mx_force_plan(*bad) == BAD
