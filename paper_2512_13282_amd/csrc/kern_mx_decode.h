@@ -5,8 +5,6 @@
 
 namespace gemm {
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
 __device__ __forceinline__ f32x4_t mfma16_bf16(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
                                                    0, 0, 0);
@@ -178,7 +176,9 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) part[(wave * NT + j) * 64 + lane] = acc[j];
     __syncthreads();
-    float *const ws = static_cast<float *>(a.g.workspace);
+    const bool separate = a.g.reduce_in_kernel == REDUCE_SEPARATE;
+    const uint32_t bytes = NT * 1024;                            // a slice's partial sums
+    const __amdgpu_buffer_rsrc_t parts = mx_parts(a.g, int(blockIdx.x), bytes);
     for (int s = int(threadIdx.x); s < NT * 64; s += 64 * KW) {
         const int64_t m = s & 15, col = n0 + 16 * (s >> 6) + 4 * ((s & 63) >> 4);
         if (m >= M || col >= N) continue;
@@ -187,35 +187,25 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
         for (int k = 1; k < KW; ++k) sum += part[k * NT * 64 + s];
         if (a.g.split_k == 1) {
             mx_store4(a.g, m, col, sum);
-        } else {
+        } else if (separate) {
+            float *const plane = static_cast<float *>(a.g.workspace) + (slice * M + m) * N + col;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (col + r < N) store_coherent(&ws[(slice * M + m) * N + col + r], sum[r]);
+                if (col + r < N) plane[r] = sum[r];
+        } else {
+            mx_store_part(parts, slice * bytes + s * 16, sum);
         }
     }
-    if (a.g.split_k == 1 || a.g.reduce_in_kernel == REDUCE_SEPARATE) return;
-
-    // The slice that finishes last adds the slices up, in their order (store_tile's protocol).
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    int *const last = reinterpret_cast<int *>(lds);
-    if (threadIdx.x == 0)
-        *last = __hip_atomic_fetch_add(&a.g.counters[blockIdx.x], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                unsigned(a.g.split_k - 1);
-    __syncthreads();
-    if (!*last) return;
+    if (a.g.split_k == 1 || separate) return;
+    if (!mx_last_slice(a.g, int(blockIdx.x), *reinterpret_cast<int *>(lds + KW * NT * 1024))) return;
     for (int s = int(threadIdx.x); s < NT * 64; s += 64 * KW) {
         const int64_t m = s & 15, col = n0 + 16 * (s >> 6) + 4 * ((s & 63) >> 4);
         if (m >= M || col >= N) continue;
         f32x4_t sum{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int q = 0; q < a.g.split_k; ++q)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (col + r < N) sum[r] += load_coherent(&ws[(q * M + m) * N + col + r]);
+        for (int q = 0; q < a.g.split_k; ++q) sum += mx_load_part(parts, q * bytes + s * 16);
         mx_store4(a.g, m, col, sum);
     }
-    if (threadIdx.x == 0)
-        __hip_atomic_store(&a.g.counters[blockIdx.x], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    mx_reset_counter(a.g, int(blockIdx.x));
 }
 
 }  // namespace gemm

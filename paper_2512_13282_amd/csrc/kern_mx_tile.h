@@ -187,7 +187,7 @@ void mx_fwd_kernel(MxArgs a) {
         }
     }
     stage_barrier();
-    store_tile<DT_BF16, BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wave_m * (BM / WM), n0 + wave_n * (BN / WN), lane,
+    mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wave_m * (BM / WM), n0 + wave_n * (BN / WN), lane,
                                         *reinterpret_cast<int *>(lds[0]));
 }
 
@@ -431,7 +431,7 @@ void mx_grad_kernel(MxArgs a) {
         multiply(I1{});
     }
     stage_barrier();
-    store_tile<DT_BF16, BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, *reinterpret_cast<int *>(a_lds0));
+    mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, *reinterpret_cast<int *>(a_lds0));
 }
 
 }  // namespace gemm

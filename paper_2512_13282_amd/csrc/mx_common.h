@@ -14,6 +14,7 @@ namespace gemm {
 typedef unsigned u32x4_any_mx __attribute__((ext_vector_type(4), aligned(1)));
 typedef unsigned u32x2_any_mx __attribute__((ext_vector_type(2), aligned(1)));
 typedef unsigned u32_any_mx __attribute__((aligned(1)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 // The scale operand of the conversions for scale byte e: they use its exponent field.
@@ -40,6 +41,91 @@ __device__ __forceinline__ u32x2_t mx8_to_bf16(uint32_t codes, float scale) {
     const float f2 = float(int8_t(codes >> 16)) * scale, f3 = float(int8_t(codes >> 24)) * scale;
     return u32x2_t{perm(__builtin_bit_cast(uint32_t, f1), __builtin_bit_cast(uint32_t, f0), 0x07060302u),
                    perm(__builtin_bit_cast(uint32_t, f3), __builtin_bit_cast(uint32_t, f2), 0x07060302u)};
+}
+
+// ---------------------------------------------------------------------------
+// K slices.  Each slice of an output tile leaves its partial sums in the workspace as its
+// registers hold them, four floats of a thread at a time: slot v of thread t of slice s of
+// the tile at 16 ((s SLOTS + v) THREADS + t), so that every access is a run of 1 KiB per wave
+// (element by element, into rows of C's shape, the sums of 64 x 4096 in two slices took 6 us
+// more).  The slice that arrives last adds the tile's slices up in their order, whichever
+// it is, so the result does not depend on it.
+//
+// The ordering is store_tile's (gemm_common.h): stores and loads at the device's coherence
+// point (sc1), each thread's stores complete before the barrier ahead of the ticket, the
+// loads issued after the ticket's answer.
+// ---------------------------------------------------------------------------
+constexpr int kCoherent = 16;        // the sc1 bit of a buffer access: device scope
+
+__device__ __forceinline__ void mx_store_part(__amdgpu_buffer_rsrc_t r, uint32_t off, f32x4_t v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, int(off), 0, kCoherent);
+}
+__device__ __forceinline__ f32x4_t mx_load_part(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, int(off), 0, kCoherent));
+}
+
+// The workspace of output tile `tile`: split_k slices of `slice_bytes`.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_parts(const KernelArgs &g, int tile, uint32_t slice_bytes) {
+    uint8_t *const base = static_cast<uint8_t *>(g.workspace) + int64_t(tile) * g.split_k * slice_bytes;
+    return make_rsrc(base, uint32_t(g.split_k) * slice_bytes);
+}
+
+// After a thread's partial stores: true in every thread of the slice that arrives last.
+// `flag`: a word of LDS that nothing else uses.
+__device__ __forceinline__ bool mx_last_slice(const KernelArgs &g, int tile, int &flag) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        flag = __hip_atomic_fetch_add(&g.counters[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+               unsigned(g.split_k - 1);
+    __syncthreads();
+    return flag != 0;
+}
+__device__ __forceinline__ void mx_reset_counter(const KernelArgs &g, int tile) {
+    if (threadIdx.x == 0) __hip_atomic_store(&g.counters[tile], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// store_tile for the tile kernels: the last slice's sum as above; whole K, and slices that a
+// kernel of its own adds up, as store_tile does.
+template <int BM, int BN, int TM, int TN>
+__device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&acc)[TM][TN], int tm, int tn, int slice,
+                                              int64_t r0, int64_t c0, int lane, int &flag) {
+    KernelArgs out = g;
+    if (g.split_k > 1 && g.reduce_in_kernel == REDUCE_LAST_SLICE) {
+        constexpr int THREADS = 64 * (BM / (32 * TM)) * (BN / (32 * TN));
+        constexpr uint32_t SLICE = uint32_t(BM) * BN * 4;
+        const int tile = tm * g.tiles_n + tn;
+        const __amdgpu_buffer_rsrc_t parts = mx_parts(g, tile, SLICE);
+        const uint32_t off = threadIdx.x * 16;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4_t v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    mx_store_part(parts, slice * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16, v);
+                }
+        if (!mx_last_slice(g, tile, flag)) return;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
+        for (int s = 0; s < g.split_k; ++s)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4_t v = mx_load_part(parts, s * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[e];
+                    }
+        mx_reset_counter(g, tile);
+        out.split_k = 1;
+    }
+    store_tile<DT_BF16, BM, BN, TM, TN>(out, acc, tm, tn, slice, r0, c0, lane, flag);
 }
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }

@@ -9,7 +9,7 @@ hipError_t launch_mx_fwd(int32_t cfg, const MxArgs &a, int64_t grid, hipStream_t
     const dim3 g{unsigned(grid)};
     if (cfg < 2) {
         const int waves = kMxConfigs[cfg].waves;
-        const size_t x = size_t(a.g.M) * size_t(a.g.k_chunk * 2 + 16), sums = size_t(waves) * 1024;
+        const size_t x = size_t(a.g.M) * size_t(a.g.k_chunk * 2 + 16), sums = size_t(waves) * 1024 + 16;
         const dim3 d{unsigned(a.g.tiles_n), unsigned(a.g.split_k)};
         if (cfg == 0) return launch_mx(mx_decode_kernel<1, 4, 2>, a, d, 256, x > sums ? x : sums, s);
         return launch_mx(mx_decode_kernel<1, 8, 2>, a, d, 512, x > sums ? x : sums, s);

@@ -63,7 +63,8 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2;
     const bool copy_a = !decode && a.g.K > 0 && !loadable(a.g.A, a.g.lda * 2);
     const bool copy_b = !decode && a.g.K > 0 && !loadable(a.g.B, a.g.ldb);
-    const int64_t partial = a.g.split_k > 1 ? padded(a.g.split_k * a.g.M * a.g.N * 4) : 0;
+    // Partial sums: whole tiles (the decode kernel's: 16 rows), at least the planes that the separate reduction reads.
+    const int64_t partial = a.g.split_k > 1 ? a.g.split_k * tm * tn * c.bm * c.bn * 4 : 0;
     const int64_t a_bytes = copy_a ? a_rows * padded(a_used) : 0, b_bytes = copy_b ? b_rows * padded(b_used) : 0;
     if ((copy_a && padded(a_used) > (int64_t(1) << 22)) || (copy_b && padded(b_used) > (int64_t(1) << 22)))
         return LAUNCH_UNSUPPORTED;

@@ -95,126 +95,169 @@ class MxMatrix(NamedTuple):
     cols: int
 
 
-def _row_stride(t):
+# The helpers' per-call work is what bounds the smallest calls, so each is bound once to torch and its entry points,
+# asks each tensor for every property once and takes the stream's handle without a Stream object.
+
+def _ld(stride, rows, cols):
     """The row stride of a matrix whose rows are contiguous (a single row or column has no
-    meaningful other stride)."""
-    rows, cols = t.shape
-    ld, step = t.stride()
+    meaningful other one)."""
+    ld, step = stride
     if step != 1 and cols > 1:
         raise ValueError("rows must be contiguous")
-    return max(ld, cols, 1) if rows > 1 else max(cols, 1)
+    return (ld if ld > cols else cols) if rows > 1 and cols else cols or 1
 
 
-def _check_packed(Q, torch, bits, device):
+def _packed(Q, bits, code_dtype, byte_dtype, device):
+    """(rows, cols, codes' address, row stride, scales' address, row stride) of a packed matrix."""
     codes, scales, cols = Q
-    if codes.dtype != (torch.uint8 if bits == 4 else torch.int8) or scales.dtype != torch.uint8:
+    if codes.dtype != code_dtype or scales.dtype != byte_dtype:
         raise TypeError(f"expected {bits}-bit codes with uint8 scales")
-    if codes.dim() != 2 or scales.dim() != 2 or codes.shape[1] != ((cols + 1) // 2 if bits == 4 else cols) \
-            or scales.shape != (codes.shape[0], -(-cols // BLOCK)):
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError("codes and scales do not fit the matrix")
+    rows, width = codes.shape
+    blocks = (cols + 31) // 32
+    if width != ((cols + 1) // 2 if bits == 4 else cols) or scales.shape != (rows, blocks):
         raise ValueError("codes and scales do not fit the matrix")
     if not codes.is_cuda or codes.get_device() != device or scales.get_device() != device:
         raise ValueError("operands must be on the same GPU")
+    return (rows, cols, codes.data_ptr(), _ld(codes.stride(), rows, width), scales.data_ptr(),
+            _ld(scales.stride(), rows, blocks))
 
 
-def _pack(X, bits):
+def _pack_helper(bits):
     import torch
-    if X.dtype != torch.bfloat16:
-        raise TypeError("expected a bfloat16 matrix")
-    if X.dim() != 2 or not X.is_cuda:
-        raise ValueError("expected a matrix on the GPU")
-    rows, cols = X.shape
-    ldx = _row_stride(X)
-    nbytes, blocks = ((cols + 1) // 2 if bits == 4 else cols), -(-cols // BLOCK)
-    # Rows at a stride of whole 16 bytes: what the products read in aligned pieces.
-    ldq = -(-nbytes // 16) * 16
-    codes = torch.empty((rows, ldq), dtype=torch.uint8 if bits == 4 else torch.int8, device=X.device)[:, :nbytes]
-    scales = torch.empty((rows, blocks), dtype=torch.uint8, device=X.device)
-    rc = (mx_pack4 if bits == 4 else mx_pack8)(rows, cols, X.data_ptr(), ldx, codes.data_ptr(), max(ldq, 1),
-                                               scales.data_ptr(), max(blocks, 1),
-                                               torch._C._cuda_getCurrentRawStream(X.get_device()))
-    if rc != _b.GEMM_OK:
-        raise _b.GemmError(rc)
-    return MxMatrix(codes, scales, cols)
+    fn = lib()[f"mx_pack{bits}"]
+    bf16, byte, code_dtype = torch.bfloat16, torch.uint8, torch.uint8 if bits == 4 else torch.int8
+    raw_stream, empty, ok = torch._C._cuda_getCurrentRawStream, torch.empty, _b.GEMM_OK
+
+    def pack(X):
+        if X.dtype != bf16:
+            raise TypeError("expected a bfloat16 matrix")
+        if X.dim() != 2 or not X.is_cuda:
+            raise ValueError("expected a matrix on the GPU")
+        rows, cols = X.shape
+        width, blocks = ((cols + 1) // 2 if bits == 4 else cols), (cols + 31) // 32
+        # Rows at a stride of whole 16 bytes: what the products read in aligned pieces.
+        ldq = (width + 15) // 16 * 16
+        device = X.device
+        codes = empty((rows, ldq), dtype=code_dtype, device=device)
+        scales = empty((rows, blocks), dtype=byte, device=device)
+        rc = fn(rows, cols, X.data_ptr(), _ld(X.stride(), rows, cols), codes.data_ptr(), ldq or 1, scales.data_ptr(),
+                blocks or 1, raw_stream(X.get_device()))
+        if rc != ok:
+            raise _b.GemmError(rc)
+        return MxMatrix(codes if ldq == width else codes[:, :width], scales, cols)
+
+    return pack
+
+
+def _unpack_helper():
+    import torch
+    fns = {torch.uint8: (lib()["mx_unpack4"], 4), torch.int8: (lib()["mx_unpack8"], 8)}
+    bf16, byte = torch.bfloat16, torch.uint8
+    raw_stream, empty, ok = torch._C._cuda_getCurrentRawStream, torch.empty, _b.GEMM_OK
+
+    def unpack(Q, out):
+        code_dtype = Q.codes.dtype
+        if code_dtype not in fns:
+            raise TypeError("expected uint8 (4-bit) or int8 (8-bit) codes")
+        fn, bits = fns[code_dtype]
+        device = Q.codes.get_device()
+        rows, cols, codes, ldq, scales, lds = _packed(Q, bits, code_dtype, byte, device)
+        if out is None:
+            out = empty((rows, cols), dtype=bf16, device=Q.codes.device)
+        elif out.dtype != bf16 or out.shape != (rows, cols) or out.get_device() != device:
+            raise ValueError("bad output tensor")
+        rc = fn(rows, cols, codes, ldq, scales, lds, out.data_ptr(), _ld(out.stride(), rows, cols), raw_stream(device))
+        if rc != ok:
+            raise _b.GemmError(rc)
+        return out
+
+    return unpack
+
+
+def _product_helper(op):
+    import torch
+    stem, bits = {MX_OP_FORWARD: ("mx_gemm_bf16_mx4_{}_bt", 4), MX_OP_INPUT_GRADIENT: ("mx_gemm_bf16_mx4_{}", 4),
+                  MX_OP_WEIGHT_GRADIENT: ("mx_gemm_bf16_mx8_{}_at", 8)}[op]
+    bf16, byte, code_dtype = torch.bfloat16, torch.uint8, torch.uint8 if bits == 4 else torch.int8
+    fns = {torch.float32: lib()[stem.format("f32")], bf16: lib()[stem.format("bf16")]}
+    raw_stream, empty, ok = torch._C._cuda_getCurrentRawStream, torch.empty, _b.GEMM_OK
+    default = torch.float32 if op == MX_OP_WEIGHT_GRADIENT else bf16
+
+    def multiply(A, Q, out, out_dtype):
+        if A.dtype != bf16:
+            raise TypeError("expected a bfloat16 operand")
+        if A.dim() != 2 or not A.is_cuda:
+            raise ValueError("expected a matrix on the GPU")
+        device = A.get_device()
+        b_rows, b_cols, codes, ldq, scales, lds = _packed(Q, bits, code_dtype, byte, device)
+        rows, cols = A.shape
+        if op == MX_OP_FORWARD:
+            M, K, N, inner = rows, cols, b_rows, b_cols
+        else:
+            inner, N = b_rows, b_cols
+            M, K = (rows, cols) if op == MX_OP_INPUT_GRADIENT else (cols, rows)
+        if K != inner:
+            raise ValueError("operand sizes do not fit")
+        if out is None:
+            out_dtype = out_dtype or default
+            if out_dtype not in fns:
+                raise TypeError("results are bfloat16 or float32")
+            out = empty((M, N), dtype=out_dtype, device=A.device)
+            ldc = N or 1
+        else:
+            out_dtype = out.dtype
+            if out_dtype not in fns or out.shape != (M, N) or out.get_device() != device:
+                raise ValueError("bad output tensor")
+            ldc = _ld(out.stride(), M, N)
+        rc = fns[out_dtype](M, N, K, A.data_ptr(), _ld(A.stride(), rows, cols), codes, ldq, scales, lds, out.data_ptr(),
+                            ldc, raw_stream(device))
+        if rc != ok:
+            raise _b.GemmError(rc)
+        return out
+
+    return multiply
+
+
+_bound = {}
+
+
+def _helper(key, make, *args):
+    fn = _bound.get(key)
+    if fn is None:
+        fn = _bound[key] = make(*args)
+    return fn
 
 
 def pack_mx4(X) -> MxMatrix:
     """A bf16 matrix packed to 4-bit elements, a scale for every 32 of a row."""
-    return _pack(X, 4)
+    return (_bound.get("pack4") or _helper("pack4", _pack_helper, 4))(X)
 
 
 def pack_mx8(X) -> MxMatrix:
     """A bf16 matrix packed to 8-bit elements, a scale for every 32 of a row."""
-    return _pack(X, 8)
+    return (_bound.get("pack8") or _helper("pack8", _pack_helper, 8))(X)
 
 
 def unpack_mx(Q, out=None):
     """The bf16 matrix that a packed one stands for, exactly."""
-    import torch
-    codes, scales, cols = Q
-    bits = 8 if codes.dtype == torch.int8 else 4
-    _check_packed(Q, torch, bits, codes.get_device())
-    rows = codes.shape[0]
-    if out is None:
-        out = torch.empty((rows, cols), dtype=torch.bfloat16, device=codes.device)
-    elif out.dtype != torch.bfloat16 or out.shape != (rows, cols) or out.get_device() != codes.get_device():
-        raise ValueError("bad output tensor")
-    rc = (mx_unpack4 if bits == 4 else mx_unpack8)(rows, cols, codes.data_ptr(), _row_stride(codes), scales.data_ptr(),
-                                                   _row_stride(scales), out.data_ptr(), _row_stride(out),
-                                                   torch._C._cuda_getCurrentRawStream(codes.get_device()))
-    if rc != _b.GEMM_OK:
-        raise _b.GemmError(rc)
-    return out
-
-
-def _multiply(stem, bits, A, Q, M, N, K, inner, out, out_dtype):
-    import torch
-    if A.dtype != torch.bfloat16:
-        raise TypeError("expected a bfloat16 operand")
-    if not A.is_cuda:
-        raise ValueError("operands must be on the same GPU")
-    device = A.get_device()
-    _check_packed(Q, torch, bits, device)
-    if K != inner:
-        raise ValueError("operand sizes do not fit")
-    if out is None:
-        if out_dtype not in (torch.bfloat16, torch.float32):
-            raise TypeError("results are bfloat16 or float32")
-        out = torch.empty((M, N), dtype=out_dtype, device=A.device)
-    elif out.dtype not in (torch.bfloat16, torch.float32) or out.shape != (M, N) or out.get_device() != device:
-        raise ValueError("bad output tensor")
-    fn = lib()[stem.format("f32" if out.dtype == torch.float32 else "bf16")]
-    rc = fn(M, N, K, A.data_ptr(), _row_stride(A), Q.codes.data_ptr(), _row_stride(Q.codes), Q.scales.data_ptr(),
-            _row_stride(Q.scales), out.data_ptr(), _row_stride(out), torch._C._cuda_getCurrentRawStream(device))
-    if rc != _b.GEMM_OK:
-        raise _b.GemmError(rc)
-    return out
-
-
-def _matrix(A):
-    if A.dim() != 2:
-        raise ValueError("expected a matrix")
-    return A.shape
+    return (_bound.get("unpack") or _helper("unpack", _unpack_helper))(Q, out)
 
 
 def linear_mx4(A, W, out=None, out_dtype=None):
     """A (M x K bf16) . W^T over a 4-bit weight W (N x K): M x N, bf16 unless out_dtype or out
     says float32."""
-    import torch
-    M, K = _matrix(A)
-    return _multiply("mx_gemm_bf16_mx4_{}_bt", 4, A, W, M, W.codes.shape[0], K, W.cols, out, out_dtype or torch.bfloat16)
+    return (_bound.get(0) or _helper(0, _product_helper, MX_OP_FORWARD))(A, W, out, out_dtype)
 
 
 def linear_mx4_dx(dY, W, out=None, out_dtype=None):
     """dY (M x N bf16) . W over a 4-bit weight W (N x K): the input gradient, M x K, bf16 unless
     out_dtype or out says float32."""
-    import torch
-    M, N = _matrix(dY)
-    return _multiply("mx_gemm_bf16_mx4_{}", 4, dY, W, M, W.cols, N, W.codes.shape[0], out, out_dtype or torch.bfloat16)
+    return (_bound.get(1) or _helper(1, _product_helper, MX_OP_INPUT_GRADIENT))(dY, W, out, out_dtype)
 
 
 def linear_mx8_dw(dY, X, out=None, out_dtype=None):
     """dY^T . X over an 8-bit input X (tokens x K) and dY (tokens x N bf16): the weight gradient,
     N x K, fp32 unless out_dtype or out says bfloat16."""
-    import torch
-    T, N = _matrix(dY)
-    return _multiply("mx_gemm_bf16_mx8_{}_at", 8, dY, X, N, X.cols, T, X.codes.shape[0], out, out_dtype or torch.float32)
+    return (_bound.get(2) or _helper(2, _product_helper, MX_OP_WEIGHT_GRADIENT))(dY, X, out, out_dtype)
