@@ -14,15 +14,21 @@ namespace gemm {
 // instructions per 32 x 16 fragment) are repeated only by the WM waves that share its rows.
 // k-step t of a 64-k part takes, for lanes of half h, k = 32 h + 8 t + 0..7 of both operands.
 //
-// The block scales of the tile's rows sit in LDS for PANEL k at a time, loaded through
-// registers between two stages: their bytes are too few and too scattered to ride along in
-// each stage.
+// The block scales of the tile's rows sit in LDS for PANEL k at a time, loaded ahead of the
+// first stage and again between two stages: their bytes are too few and too scattered to
+// ride along in each stage.  Straight into LDS where their rows are on dwords; through
+// registers elsewhere, which waits for the stages on their way too.
+//
+// WK > 1: that many groups of waves take turns at the 64-k parts of a stage, and add their
+// sums up in LDS at the end.  A narrow tile's wave has one or two fragments, and its k-steps wait
+// for each other (LDS read, conversion, MFMA: 1000 clocks per 128 k with one wave per
+// SIMD); a second wave fills those waits without more K slices to sum.
 // ---------------------------------------------------------------------------
-template <int BM, int BN, int WM, int WN, int WAVES_PER_EU, int KS, int NS, int PANEL>
-__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN),
+template <int BM, int BN, int WM, int WN, int WK, int WAVES_PER_EU, int KS, int NS, int PANEL>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN * WK, 64 * WM * WN * WK),
                           amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU)))
 void mx_fwd_kernel(MxArgs a) {
-    constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+    constexpr int WAVES = WM * WN * WK, THREADS = 64 * WAVES;
     constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int PARTS = KS / 64;                            // 64-k parts of a stage
     constexpr int A_PART = BM * 128, A_STAGE = A_PART * PARTS;
@@ -36,13 +42,17 @@ void mx_fwd_kernel(MxArgs a) {
     // A panel row is an odd number of dwords: 32 rows lie on 32 banks.
     constexpr int PANEL_PITCH = PANEL / kMxBlock + 4;
     static_assert(PANEL % KS == 0 && PANEL % 256 == 0, "a stage has one panel, of whole odd rows");
+    constexpr int P_INSTR = (BN * PANEL_PITCH + 256 * WAVES - 1) / (256 * WAVES);      // dword loads per lane
+    static_assert((NS - 1) * LPS + P_INSTR < 64, "loads in flight must fit vmcnt");
+    static_assert(PARTS % WK == 0, "the groups have as many parts of a stage each");
+    static_assert((WK - 1) * BM * BN * 4 <= NS * (A_STAGE + B_STAGE), "the groups' sums fit the ring");
 
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NS][A_STAGE + B_STAGE];
-    __shared__ uint8_t panel[BN * PANEL_PITCH];
+    __shared__ __attribute__((aligned(256))) uint8_t panel[P_INSTR * 256 * WAVES];
 
     const int tid = int(threadIdx.x), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wave_m = wave / WN, wave_n = wave % WN;
+    const int group = wave / (WM * WN), wave_m = wave / WN % WM, wave_n = wave % WN;
     int tm, tn, slice;
     map_tile(a.g, tm, tn, slice);
     const int64_t M = a.g.M, N = a.g.N;
@@ -92,25 +102,42 @@ void mx_fwd_kernel(MxArgs a) {
         for (int i = 0; i < A_INSTR; ++i) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
     };
     // The scales of rows n0.. from k0 (of this slice) on; rows and blocks past the end take 0.
+    const bool scale_dwords = ((reinterpret_cast<uintptr_t>(a.scales) | uint64_t(a.ld_scales)) & 3) == 0 &&
+                              a.ld_scales < (int64_t(1) << 22);
     auto load_panel = [&](int k0) {
+        constexpr int ROW = PANEL_PITCH / 4, DWORDS = PANEL / kMxBlock / 4;      // dwords of a panel row: 1 more than used
         const int64_t b0 = (k_begin + k0) / kMxBlock, nb = (a.g.K + kMxBlock - 1) / kMxBlock;
-        constexpr int DW = PANEL / kMxBlock / 4;          // dwords of a panel row
-        for (int p = tid; p < BN * DW; p += THREADS) {
-            const int r = p / DW, d = p % DW;
-            if (k0 + d * 4 * kMxBlock >= nk * KS) continue;      // no stage reads them
-            const uint8_t *const src = a.scales + (n0 + r) * a.ld_scales + b0 + 4 * d;
-            const int64_t left = n0 + r < N ? nb - (b0 + 4 * d) : 0;
-            uint32_t v = 0;
-            if (left >= 4) {
-                v = *reinterpret_cast<const u32_any_mx *>(src);
-            } else {
+        const int64_t rows = N - n0 < BN ? N - n0 : BN;
+        if (scale_dwords) {
+            // A row's last dword may go on past its last block, within its stride or (in the
+            // matrix' last row) an aligned dword that holds one: those scales meet zeros of A,
+            // and are made 0 where they are read (`blocks` below).
+            // readfirstlane: the compiler otherwise forms the (uniform) address on the vector unit
+            const uint64_t at = reinterpret_cast<uint64_t>(a.scales) + uint64_t(n0 * a.ld_scales + b0);
+            const uint64_t base = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(at))))) |
+                                  (uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(at >> 32))))) << 32);
+            const i32x4_t rs = ring_rsrc(reinterpret_cast<const uint8_t *>(base), 0x7fffffffu);
+            const uint32_t dst = lds_addr(panel) + uint32_t(wave) * 256u;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < left) v |= uint32_t(src[e]) << (8 * e);
+            for (int i = 0; i < P_INSTR; ++i) {
+                const int p = (i * WAVES + wave) * 64 + lane, r = p / ROW, d = p % ROW;
+                const bool in = r < rows && d < DWORDS && b0 + 4 * d < nb;
+                ring_load4(rs, dst + i * (WAVES * 256), in ? uint32_t(r * a.ld_scales + 4 * d) : kOOB);
             }
+            return;
+        }
+        for (int p = tid; p < BN * DWORDS; p += THREADS) {
+            const int r = p / DWORDS, d = p % DWORDS;
+            const uint8_t *const src = a.scales + (n0 + r) * a.ld_scales + b0 + 4 * d;
+            const int64_t left = r < rows ? nb - (b0 + 4 * d) : 0;
+            uint32_t v = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) v |= uint32_t(src[e]) << (8 * e);
             *reinterpret_cast<uint32_t *>(&panel[r * PANEL_PITCH + 4 * d]) = v;
         }
     };
+    const int blocks = (k_len + kMxBlock - 1) / kMxBlock;      // of this slice
 
     const int frag_row = lane & 31, half = lane >> 5;
     const int r0 = wave_m * (BM / WM) + frag_row, c0 = wave_n * (BN / WN) + frag_row;
@@ -119,12 +146,12 @@ void mx_fwd_kernel(MxArgs a) {
     for (int p = 0; p < 2; ++p)
 #pragma unroll
         for (int t = 0; t < 4; ++t) a_fo[p][t] = r0 * 128 + 16 * (swz(4 * half + t, r0) ^ (4 * p));
-    int b_fo[TN][PARTS];
+    int b_fo[TN][PARTS / WK];                                  // this group's parts
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q)
-            b_fo[j][q] = A_STAGE + (c0 + 32 * j) * PITCH + 16 * ((2 * q + half) ^ w_swz(c0 + 32 * j));
+        for (int p = 0; p < PARTS / WK; ++p)
+            b_fo[j][p] = A_STAGE + (c0 + 32 * j) * PITCH + 16 * ((2 * (p * WK + group) + half) ^ w_swz(c0 + 32 * j));
 
     f32x16_t acc[TM][TN];
 #pragma unroll
@@ -147,13 +174,15 @@ void mx_fwd_kernel(MxArgs a) {
         load_stage(kt + NS - 1, std::integral_constant<int, (BUF + NS - 1) % NS>{});
         const int block0 = (kt * KS % PANEL) / kMxBlock + half;
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) {
+        for (int p = 0; p < PARTS / WK; ++p) {
+            const int q = p * WK + group;
+            const bool in = kt * (KS / kMxBlock) + half + 2 * q < blocks;     // past the end: no NaN for A's zeros
             u32x4_t w[TN];
             float s[TN];
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                w[j] = *reinterpret_cast<const u32x4_t *>(st + b_fo[j][q]);
-                s[j] = mx4_scale(panel[(c0 + 32 * j) * PANEL_PITCH + block0 + 2 * q]);
+                w[j] = *reinterpret_cast<const u32x4_t *>(st + b_fo[j][p]);
+                s[j] = mx4_scale(in ? panel[(c0 + 32 * j) * PANEL_PITCH + block0 + 2 * q] : 0);
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -172,14 +201,16 @@ void mx_fwd_kernel(MxArgs a) {
     };
 
     if (nk > 0) {
+        load_panel(0);
         static_for<0, NS - 1>([&](auto u) { load_stage(decltype(u)::value, u); });
         for (int kt = 0; kt < nk; kt += NS) {
             static_for<0, NS>([&](auto u) {
                 constexpr int U = decltype(u)::value;
                 if (kt + U < nk) {
-                    if ((kt + U) % (PANEL / KS) == 0) {
-                        if (kt + U > 0) phase_barrier();      // every wave is done with the panel before
+                    if (kt + U > 0 && (kt + U) % (PANEL / KS) == 0) {
+                        phase_barrier();                      // every wave is done with the panel before
                         load_panel((kt + U) * KS);
+                        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                     }
                     iteration(kt + U, u);
                 }
@@ -187,8 +218,33 @@ void mx_fwd_kernel(MxArgs a) {
         }
     }
     stage_barrier();
+    if constexpr (WK > 1) {
+        // The groups' sums, in their order, into the first one's registers.
+        f32x4_t *const sums = reinterpret_cast<f32x4_t *>(&lds[0][0]);
+        constexpr int OWN = THREADS / WK, SLOTS = TM * TN * 4;
+        if (group > 0) {
+#pragma unroll
+            for (int v = 0; v < SLOTS; ++v) {
+                const f32x16_t &x = acc[v / 4 / TN][v / 4 % TN];
+                const int q = 4 * (v % 4);
+                sums[((group - 1) * SLOTS + v) * OWN + tid % OWN] = f32x4_t{x[q], x[q + 1], x[q + 2], x[q + 3]};
+            }
+        }
+        phase_barrier();
+        if (group == 0) {
+#pragma unroll
+            for (int o = 0; o < WK - 1; ++o)
+#pragma unroll
+                for (int v = 0; v < SLOTS; ++v) {
+                    const f32x4_t x = sums[(o * SLOTS + v) * OWN + tid];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[v / 4 / TN][v / 4 % TN][4 * (v % 4) + e] += x[e];
+                }
+        }
+        phase_barrier();
+    }
     mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wave_m * (BM / WM), n0 + wave_n * (BN / WN), lane,
-                                        *reinterpret_cast<int *>(lds[0]));
+                                  group == 0, *reinterpret_cast<int *>(lds[0]));
 }
 
 // ---------------------------------------------------------------------------
@@ -431,7 +487,7 @@ void mx_grad_kernel(MxArgs a) {
         multiply(I1{});
     }
     stage_barrier();
-    mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, *reinterpret_cast<int *>(a_lds0));
+    mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, true, *reinterpret_cast<int *>(a_lds0));
 }
 
 }  // namespace gemm

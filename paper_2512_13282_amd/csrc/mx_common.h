@@ -86,12 +86,15 @@ __device__ __forceinline__ void mx_reset_counter(const KernelArgs &g, int tile) 
 }
 
 // store_tile for the tile kernels: the last slice's sum as above; whole K, and slices that a
-// kernel of its own adds up, as store_tile does.
+// kernel of its own adds up, as store_tile does.  Called by every thread of the workgroup;
+// `holds` says whether this one's registers hold results (the workgroup's first BM x BN / (TM
+// TN 16) threads do).  Rows past M are neither left in the workspace nor fetched.
 template <int BM, int BN, int TM, int TN>
 __device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&acc)[TM][TN], int tm, int tn, int slice,
-                                              int64_t r0, int64_t c0, int lane, int &flag) {
+                                              int64_t r0, int64_t c0, int lane, bool holds, int &flag) {
     KernelArgs out = g;
     if (g.split_k > 1 && g.reduce_in_kernel == REDUCE_LAST_SLICE) {
+        const int64_t rows = holds ? g.M - r0 : 0;        // slot q of fragment row i: rows 32 i + 8 q .. + 7
         constexpr int THREADS = 64 * (BM / (32 * TM)) * (BN / (32 * TN));
         constexpr uint32_t SLICE = uint32_t(BM) * BN * 4;
         const int tile = tm * g.tiles_n + tn;
@@ -103,6 +106,7 @@ __device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&ac
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
+                    if (32 * i + 8 * q >= rows) continue;
                     const f32x4_t v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
                     mx_store_part(parts, slice * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16, v);
                 }
@@ -111,21 +115,39 @@ __device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&ac
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
-        for (int s = 0; s < g.split_k; ++s)
+        // Small tiles fetch up to four slices at once: one after the other, each waits out a trip
+        // to the coherence point.
+        constexpr int G = TM * TN >= 4 ? 1 : 4 / (TM * TN);
+        const int whole = g.split_k / G * G;
+        auto add = [&](int s, auto n_c) {
+            constexpr int COUNT = decltype(n_c)::value;
+            f32x4_t v[COUNT][TM][TN][4];
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int u = 0; u < COUNT; ++u)
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x4_t v = mx_load_part(parts, s * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16);
+                    for (int j = 0; j < TN; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[e];
-                    }
+                        for (int q = 0; q < 4; ++q)
+                            v[u][i][j][q] = mx_load_part(parts, 32 * i + 8 * q < rows ? (s + u) * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16 : kOOB);
+#pragma unroll
+            for (int u = 0; u < COUNT; ++u)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[u][i][j][q][e];
+        };
+        for (int s = 0; s < whole; s += G) add(s, std::integral_constant<int, G>{});
+        for (int s = whole; s < g.split_k; ++s) add(s, std::integral_constant<int, 1>{});
         mx_reset_counter(g, tile);
         out.split_k = 1;
     }
-    store_tile<DT_BF16, BM, BN, TM, TN>(out, acc, tm, tn, slice, r0, c0, lane, flag);
+    if (holds) store_tile<DT_BF16, BM, BN, TM, TN>(out, acc, tm, tn, slice, r0, c0, lane, flag);
 }
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }

@@ -19,6 +19,21 @@ const MxConfig kMxConfigs[] = {
     {MX_DW, 64, 128, 4, 2, "mx_dw_64x128"},
     {MX_DW, 128, 128, 4, 2, "mx_dw_128x128"},
     {MX_DW, 256, 256, 8, 1, "mx_dw_256x256"},
+    {MX_FWD, 32, 128, 8, 2, "mx_T14_32x128_1x4x2_w2_k128_n3"},
+    {MX_FWD, 32, 128, 8, 2, "mx_T15_32x128_1x4x2_w2_k128_n4"},
+    {MX_FWD, 32, 128, 8, 1, "mx_T16_32x128_1x4x2_w2_k256_n3"},
+    {MX_FWD, 32, 128, 16, 1, "mx_T17_32x128_1x4x4_w4_k256_n2"},
+    {MX_FWD, 32, 128, 8, 2, "mx_T18_32x128_1x4x2_w4_k128_n2"},
+    {MX_FWD, 64, 128, 8, 1, "mx_T19_64x128_1x4x2_w2_k128_n3"},
+    {MX_FWD, 64, 128, 8, 1, "mx_T20_64x128_2x2x2_w2_k128_n3"},
+    {MX_FWD, 128, 256, 8, 1, "mx_T21_128x256_2x4x1_w2_k64_n3"},
+    {MX_FWD, 128, 256, 8, 2, "mx_T22_128x256_2x4x1_w4_k64_n2"},
+    {MX_FWD, 32, 256, 16, 1, "mx_T23_32x256_1x8x2_w4_k256_n2"},
+    {MX_FWD, 32, 128, 8, 1, "mx_T24_32x128_1x2x4_w2_k256_n3"},
+    {MX_FWD, 64, 64, 8, 1, "mx_T25_64x64_1x2x4_w2_k256_n3"},
+    {MX_FWD, 32, 64, 8, 1, "mx_T26_32x64_1x2x4_w2_k256_n3"},
+    {MX_FWD, 64, 64, 8, 1, "mx_T27_64x64_2x2x2_w2_k256_n2"},
+    {MX_FWD, 128, 128, 8, 1, "mx_T28_128x128_2x2x2_w2_k128_n3"},
 };
 const int32_t kMxNumConfigs = sizeof(kMxConfigs) / sizeof(kMxConfigs[0]);
 
