@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
     }
     u32x4_t w[U][NT];
     uint32_t sc[U][NT];
-    auto load = [&](int u, int c) {
+    auto load = [&](int u, int c) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             w[u][j] = *reinterpret_cast<const u32x4_any_mx *>(wp[j] + c * 64);
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
     f32x4_t acc[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    auto multiply = [&](int u, int c) {
+    auto multiply = [&](int u, int c) __attribute__((always_inline)) {
         u32x4_t x[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) x[t] = *reinterpret_cast<const u32x4_t *>(xrow + c * 256 + 16 * t);

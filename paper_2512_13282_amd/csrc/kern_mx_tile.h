@@ -5,6 +5,47 @@
 
 namespace gemm {
 
+// Adds the sums of WK groups of waves up, in their order, into the first group's registers,
+// through `bytes` of LDS that nothing else uses any more, in as many passes as that takes.
+template <int WK, int BYTES, int TM, int TN>
+__device__ __forceinline__ void mx_sum_groups(f32x16_t (&acc)[TM][TN], uint8_t *lds, int group, int tid) {
+    if constexpr (WK > 1) {
+        f32x4_t *const sums = reinterpret_cast<f32x4_t *>(lds);
+        const int own = int(blockDim.x) / WK;
+        constexpr int SLOTS = TM * TN * 4, MOST = BYTES / 16;      // values that fit; own <= 512
+        auto pass = [&](auto first_c, auto count_c) __attribute__((always_inline)) {
+            constexpr int FIRST = decltype(first_c)::value, COUNT = decltype(count_c)::value;
+            if (group > 0) {
+#pragma unroll
+                for (int v = FIRST; v < FIRST + COUNT; ++v) {
+                    const f32x16_t &x = acc[v / 4 / TN][v / 4 % TN];
+                    const int q = 4 * (v % 4);
+                    sums[((group - 1) * COUNT + v - FIRST) * own + tid - group * own] = f32x4_t{x[q], x[q + 1], x[q + 2], x[q + 3]};
+                }
+            }
+            phase_barrier();
+            if (group == 0) {
+#pragma unroll
+                for (int o = 0; o < WK - 1; ++o)
+#pragma unroll
+                    for (int v = FIRST; v < FIRST + COUNT; ++v) {
+                        const f32x4_t x = sums[(o * COUNT + v - FIRST) * own + tid];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[v / 4 / TN][v / 4 % TN][4 * (v % 4) + e] += x[e];
+                    }
+            }
+            phase_barrier();
+        };
+        constexpr int OWN = 256;                                    // most threads of a group that take several passes
+        constexpr int FIT = MOST / ((WK - 1) * OWN) < 1 ? 1 : MOST / ((WK - 1) * OWN);
+        constexpr int COUNT = SLOTS <= FIT ? SLOTS : FIT >= SLOTS / 2 ? SLOTS / 2 : SLOTS / 4;
+        static_assert((WK - 1) * COUNT * OWN * 16 <= BYTES, "a pass fits");
+        static_for<0, SLOTS / COUNT>([&](auto p) {
+            pass(std::integral_constant<int, decltype(p)::value * COUNT>{}, std::integral_constant<int, COUNT>{});
+        });
+    }
+}
+
 // ---------------------------------------------------------------------------
 // C = A . W^T, W 4-bit N x K.  Both operands go from memory straight into a ring of NS LDS
 // stages of KS k: A as BM rows of 128 bytes per 64 k (16-byte chunks XOR-swizzled by swz), W
@@ -39,16 +80,18 @@ void mx_fwd_kernel(MxArgs a) {
     static_assert(A_INSTR >= 1 && A_INSTR * 1024 * WAVES == A_STAGE, "A stage split");
     static_assert(B_INSTR >= 1 && B_INSTR * 1024 * WAVES == B_STAGE, "W stage split");
     static_assert(NS >= 2 && (NS - 1) * LPS < 64, "loads in flight must fit vmcnt");
-    // A panel row is an odd number of dwords: 32 rows lie on 32 banks.
-    constexpr int PANEL_PITCH = PANEL / kMxBlock + 4;
-    static_assert(PANEL % KS == 0 && PANEL % 256 == 0, "a stage has one panel, of whole odd rows");
-    constexpr int P_INSTR = (BN * PANEL_PITCH + 256 * WAVES - 1) / (256 * WAVES);      // dword loads per lane
+    // A panel row is P_CPR chunks of 16 scales; chunk c of row r sits at chunk c ^ p_swz(r), which
+    // puts 16 consecutive rows' scales of one block on different banks.
+    constexpr int P_PITCH = PANEL / kMxBlock, P_CPR = P_PITCH / 16;
+    static_assert(PANEL % KS == 0 && P_CPR >= 1 && P_CPR <= 8 && (P_CPR & (P_CPR - 1)) == 0, "panel rows");
+    constexpr int P_BYTES = (BN * P_PITCH + 1024 * WAVES - 1) / (1024 * WAVES) * (1024 * WAVES);
+    constexpr int P_INSTR = P_BYTES / (256 * WAVES);           // dword loads per lane
     static_assert((NS - 1) * LPS + P_INSTR < 64, "loads in flight must fit vmcnt");
     static_assert(PARTS % WK == 0, "the groups have as many parts of a stage each");
-    static_assert((WK - 1) * BM * BN * 4 <= NS * (A_STAGE + B_STAGE), "the groups' sums fit the ring");
+    static_assert(WK == 1 || THREADS / WK <= 256, "mx_sum_groups");
 
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NS][A_STAGE + B_STAGE];
-    __shared__ __attribute__((aligned(256))) uint8_t panel[P_INSTR * 256 * WAVES];
+    __shared__ __attribute__((aligned(1024))) uint8_t panel[P_BYTES];
 
     const int tid = int(threadIdx.x), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -89,52 +132,58 @@ void mx_fwd_kernel(MxArgs a) {
     const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + m0 * lda_b + k_begin * 2;
     const uint8_t *const b_base = static_cast<const uint8_t *>(a.g.B) + n0 * ldq + k_begin / 2;
 
-    auto load_stage = [&](int kt, auto buf_c) {
+    auto load_stage = [&](int kt, auto buf_c) __attribute__((always_inline)) {
         constexpr int BUF = decltype(buf_c)::value;
         const int rem = k_len - kt * KS;
         const uint32_t dst = lds_addr(lds[BUF]) + uint32_t(wave) * 1024u;
-        const i32x4_t ra = ring_rsrc(a_base + int64_t(kt) * (KS * 2), rem > 0 ? a_bytes : 0u);
-        const i32x4_t rb = ring_rsrc(b_base + int64_t(kt) * PITCH, rem > 0 ? b_bytes : 0u);
+        const i32x4_t ra = ring_rsrc(uniform(a_base + int64_t(kt) * (KS * 2)), uniform(rem > 0 ? a_bytes : 0u));
+        const i32x4_t rb = ring_rsrc(uniform(b_base + int64_t(kt) * PITCH), uniform(rem > 0 ? b_bytes : 0u));
 #pragma unroll
         for (int i = 0; i < B_INSTR; ++i)
             ring_load16(rb, dst + A_STAGE + i * (WAVES * 1024), b_k[i] < rem ? b_voff[i] : kOOB);
 #pragma unroll
         for (int i = 0; i < A_INSTR; ++i) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
     };
-    // The scales of rows n0.. from k0 (of this slice) on; rows and blocks past the end take 0.
-    const bool scale_dwords = ((reinterpret_cast<uintptr_t>(a.scales) | uint64_t(a.ld_scales)) & 3) == 0 &&
-                              a.ld_scales < (int64_t(1) << 22);
-    auto load_panel = [&](int k0) {
-        constexpr int ROW = PANEL_PITCH / 4, DWORDS = PANEL / kMxBlock / 4;      // dwords of a panel row: 1 more than used
+    // The scales of rows n0.. from k0 (of this slice) on, 16 or 4 bytes at a time where rows and
+    // addresses allow it, else byte by byte.  Rows past N take 0; a row's last piece may go on
+    // past its last block, within its stride or (in the matrix' last row) an aligned piece
+    // that holds one: those scales are made 0 where they are read (`blocks` below).
+    auto p_swz = [](int row) { return (row / (16 / P_CPR)) & (P_CPR - 1); };
+    const uint64_t scale_bits = reinterpret_cast<uintptr_t>(a.scales) | uint64_t(a.ld_scales) |
+                                (a.ld_scales < (int64_t(1) << 22) ? 0u : 1u);
+    auto load_panel = [&](int k0) __attribute__((always_inline)) {
         const int64_t b0 = (k_begin + k0) / kMxBlock, nb = (a.g.K + kMxBlock - 1) / kMxBlock;
         const int64_t rows = N - n0 < BN ? N - n0 : BN;
-        if (scale_dwords) {
-            // A row's last dword may go on past its last block, within its stride or (in the
-            // matrix' last row) an aligned dword that holds one: those scales meet zeros of A,
-            // and are made 0 where they are read (`blocks` below).
-            // readfirstlane: the compiler otherwise forms the (uniform) address on the vector unit
-            const uint64_t at = reinterpret_cast<uint64_t>(a.scales) + uint64_t(n0 * a.ld_scales + b0);
-            const uint64_t base = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(at))))) |
-                                  (uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(at >> 32))))) << 32);
-            const i32x4_t rs = ring_rsrc(reinterpret_cast<const uint8_t *>(base), 0x7fffffffu);
-            const uint32_t dst = lds_addr(panel) + uint32_t(wave) * 256u;
+        if ((scale_bits & 3) != 0) {
+            for (int p = tid; p < BN * P_PITCH / 4; p += THREADS) {
+                const int r = p / (P_PITCH / 4), d = p % (P_PITCH / 4);
+                const uint8_t *const src = a.scales + (n0 + r) * a.ld_scales + b0 + 4 * d;
+                const int64_t left = r < rows ? nb - (b0 + 4 * d) : 0;
+                uint32_t v = 0;
 #pragma unroll
-            for (int i = 0; i < P_INSTR; ++i) {
-                const int p = (i * WAVES + wave) * 64 + lane, r = p / ROW, d = p % ROW;
-                const bool in = r < rows && d < DWORDS && b0 + 4 * d < nb;
-                ring_load4(rs, dst + i * (WAVES * 256), in ? uint32_t(r * a.ld_scales + 4 * d) : kOOB);
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) v |= uint32_t(src[e]) << (8 * e);
+                *reinterpret_cast<uint32_t *>(&panel[r * P_PITCH + 16 * ((d / 4) ^ p_swz(r)) + 4 * (d % 4)]) = v;
             }
             return;
         }
-        for (int p = tid; p < BN * DWORDS; p += THREADS) {
-            const int r = p / DWORDS, d = p % DWORDS;
-            const uint8_t *const src = a.scales + (n0 + r) * a.ld_scales + b0 + 4 * d;
-            const int64_t left = r < rows ? nb - (b0 + 4 * d) : 0;
-            uint32_t v = 0;
+        const i32x4_t rs = ring_rsrc(uniform(a.scales + n0 * a.ld_scales + b0), 0x7fffffffu);
+        if ((scale_bits & 15) == 0 && b0 % 16 == 0) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < left) v |= uint32_t(src[e]) << (8 * e);
-            *reinterpret_cast<uint32_t *>(&panel[r * PANEL_PITCH + 4 * d]) = v;
+            for (int i = 0; i < P_INSTR / 4; ++i) {
+                const int p = (i * WAVES + wave) * 64 + lane, r = p / P_CPR, c = (p % P_CPR) ^ p_swz(r);
+                const bool in = r < rows && b0 + 16 * c < nb;
+                ring_load16(rs, lds_addr(panel) + uint32_t(i * WAVES + wave) * 1024u, in ? uint32_t(r * a.ld_scales + 16 * c) : kOOB);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < P_INSTR; ++i) {
+                const int p = (i * WAVES + wave) * 64 + lane, r = p / (P_PITCH / 4), d = p % (P_PITCH / 4);
+                const int c = (d / 4) ^ p_swz(r);
+                const bool in = r < rows && b0 + 16 * c + 4 * (d % 4) < nb;
+                ring_load4(rs, lds_addr(panel) + uint32_t(i * WAVES + wave) * 256u,
+                           in ? uint32_t(r * a.ld_scales + 16 * c + 4 * (d % 4)) : kOOB);
+            }
         }
     };
     const int blocks = (k_len + kMxBlock - 1) / kMxBlock;      // of this slice
@@ -159,7 +208,21 @@ void mx_fwd_kernel(MxArgs a) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
 
-    auto iteration = [&](int kt, auto buf_c) {
+    // Fragments of two k-steps: one multiplied while the next is read and converted.
+    u32x4_t fa[2][TM], fb[2][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[1][i] = u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[1][j] = u32x4_t{0u, 0u, 0u, 0u};
+    auto multiply = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma32<DT_BF16>(fa[slot][i], fb[slot][j], acc[i][j]);
+    };
+    // One stage.  Slot 1 holds the fragments of the k-step before, whose MFMAs run under the
+    // latency of this stage's first reads.
+    auto iteration = [&](int kt, auto buf_c) __attribute__((always_inline)) {
         constexpr int BUF = decltype(buf_c)::value;
         ring_barrier<(NS - 2) * LPS>();
         uint8_t *const st = lds[BUF];
@@ -175,27 +238,25 @@ void mx_fwd_kernel(MxArgs a) {
         const int block0 = (kt * KS % PANEL) / kMxBlock + half;
 #pragma unroll
         for (int p = 0; p < PARTS / WK; ++p) {
-            const int q = p * WK + group;
+            const int q = p * WK + group, b = block0 + 2 * q;
             const bool in = kt * (KS / kMxBlock) + half + 2 * q < blocks;     // past the end: no NaN for A's zeros
             u32x4_t w[TN];
             float s[TN];
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
+                const int r = c0 + 32 * j;
                 w[j] = *reinterpret_cast<const u32x4_t *>(st + b_fo[j][p]);
-                s[j] = mx4_scale(in ? panel[(c0 + 32 * j) * PANEL_PITCH + block0 + 2 * q] : 0);
+                s[j] = mx4_scale(in ? panel[r * P_PITCH + 16 * ((b >> 4) ^ p_swz(r)) + (b & 15)] : 0);
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                u32x4_t fa[TM], fb[TN];
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
-                    fa[i] = *reinterpret_cast<const u32x4_t *>(st + q * A_PART + a_fo[i & 1][t] + 4096 * i);
+                    fa[t & 1][i] = *reinterpret_cast<const u32x4_t *>(st + q * A_PART + a_fo[i & 1][t] + 4096 * i);
+                multiply(1 - (t & 1));
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = mx4_to_bf16(w[j][t], s[j]);
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma32<DT_BF16>(fa[i], fb[j], acc[i][j]);
+                for (int j = 0; j < TN; ++j) fb[t & 1][j] = mx4_to_bf16(w[j][t], s[j]);
+                __builtin_amdgcn_sched_barrier(0);        // one k-step ahead, no further: registers
             }
         }
     };
@@ -216,33 +277,10 @@ void mx_fwd_kernel(MxArgs a) {
                 }
             });
         }
+        multiply(1);
     }
     stage_barrier();
-    if constexpr (WK > 1) {
-        // The groups' sums, in their order, into the first one's registers.
-        f32x4_t *const sums = reinterpret_cast<f32x4_t *>(&lds[0][0]);
-        constexpr int OWN = THREADS / WK, SLOTS = TM * TN * 4;
-        if (group > 0) {
-#pragma unroll
-            for (int v = 0; v < SLOTS; ++v) {
-                const f32x16_t &x = acc[v / 4 / TN][v / 4 % TN];
-                const int q = 4 * (v % 4);
-                sums[((group - 1) * SLOTS + v) * OWN + tid % OWN] = f32x4_t{x[q], x[q + 1], x[q + 2], x[q + 3]};
-            }
-        }
-        phase_barrier();
-        if (group == 0) {
-#pragma unroll
-            for (int o = 0; o < WK - 1; ++o)
-#pragma unroll
-                for (int v = 0; v < SLOTS; ++v) {
-                    const f32x4_t x = sums[(o * SLOTS + v) * OWN + tid];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[v / 4 / TN][v / 4 % TN][4 * (v % 4) + e] += x[e];
-                }
-        }
-        phase_barrier();
-    }
+    mx_sum_groups<WK, NS * (A_STAGE + B_STAGE)>(acc, &lds[0][0], group, tid);
     mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wave_m * (BM / WM), n0 + wave_n * (BN / WN), lane,
                                   group == 0, *reinterpret_cast<int *>(lds[0]));
 }
@@ -252,25 +290,26 @@ void mx_fwd_kernel(MxArgs a) {
 // K x N): the blocks lie along N, across the sum, so every k of a column has another scale
 // and no scale can be applied after the matrix instruction.  B is converted to bf16 (exactly)
 // once per workgroup, on its way into LDS: a thread takes one block of 32 codes of one row k
-// through registers per stage of 64 k.  A goes straight from memory into LDS.
+// through registers per stage.  A goes straight from memory into LDS.  A stage is 64 k for
+// each of WK groups of waves, which add their sums up at the end (as mx_fwd_kernel's).
 //
-// LDS, two stages each: A as BM rows of 128 bytes (DX), or as 64 rows (k) of BM elements read
+// LDS, two stages each: A as BM rows of 128 bytes per 64 k (DX), or as rows (k) of BM elements read
 // back transposed (DW), both as gemm_lds_kernel lays them out.  B in one region per block column:
-// 64 rows (k) of 32 bf16, the 64-byte rows back to back, the regions 64 bytes further apart.
+// rows (k) of 32 bf16, the 64-byte rows back to back, the regions 64 bytes further apart.
 // A transpose read then covers two runs of 256 bytes, and the eight lanes that write one row's
 // chunks hit different banks (the regions of blocks 0-3 by their offset, 4-7 by a flipped chunk).
 //
 // B's codes are loaded two stages ahead into registers, A one stage ahead.
 // ---------------------------------------------------------------------------
-template <int OP, int BM, int BN, int WM, int WN, int WAVES_PER_EU>
-__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN),
+template <int OP, int BM, int BN, int WM, int WN, int WK, int WAVES_PER_EU, int NSA>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN * WK, 64 * WM * WN * WK),
                           amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU)))
 void mx_grad_kernel(MxArgs a) {
     constexpr bool DW = OP == MX_DW;
-    constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+    constexpr int WAVES = WM * WN * WK, THREADS = 64 * WAVES;
     constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr int BK = 64;
-    constexpr int A_STAGE = BM * 128;
+    constexpr int BK = 64 * WK;
+    constexpr int A_PART = BM * 128, A_STAGE = A_PART * WK;
     constexpr int A_PITCH = DW ? BM * 2 : 128, A_CPR = A_PITCH / 16;
     constexpr int A_INSTR = A_STAGE / 1024 / WAVES;
     constexpr int BLOCKS = BN / kMxBlock, REGION = BK * 64 + 64;
@@ -278,15 +317,15 @@ void mx_grad_kernel(MxArgs a) {
     constexpr int RAW = CODES / 16 + 1;                      // loads per thread and stage: codes and a scale
     static_assert(A_INSTR >= 1 && A_INSTR * 1024 * WAVES == A_STAGE, "A stage split");
     static_assert(BK * BLOCKS == THREADS, "one block of one row per thread");
+    static_assert(WK == 1 || THREADS / WK <= 256, "mx_sum_groups");
 
-    __shared__ __attribute__((aligned(1024))) uint8_t a_lds0[A_STAGE];
-    __shared__ __attribute__((aligned(1024))) uint8_t a_lds1[A_STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t a_lds[NSA][A_STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t b_lds0[BLOCKS * REGION];
     __shared__ __attribute__((aligned(1024))) uint8_t b_lds1[BLOCKS * REGION];
 
     const int tid = int(threadIdx.x), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wave_m = wave / WN, wave_n = wave % WN;
+    const int group = wave / (WM * WN), wave_m = wave / WN % WM, wave_n = wave % WN;
     int tm, tn, slice;
     map_tile(a.g, tm, tn, slice);
     const int64_t M = a.g.M, N = a.g.N;
@@ -309,20 +348,19 @@ void mx_grad_kernel(MxArgs a) {
             a_k[i] = row;
             a_voff[i] = m0 + 8 * c < M ? uint32_t(row * lda_b + 16 * c) : kOOB;
         } else {
-            const int row = (i * WAVES + wave) * 8 + (lane >> 3);
+            const int row = ((i * WAVES + wave) * 8 + (lane >> 3)) % BM, part = ((i * WAVES + wave) * 8) / BM;
             const int c = swz(lane & 7, row);
-            a_k[i] = 8 * c;
-            a_voff[i] = uint32_t(row * lda_b + 16 * c);
+            a_k[i] = 64 * part + 8 * c;
+            a_voff[i] = uint32_t(row * lda_b + 128 * part + 16 * c);
         }
     }
     const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + (DW ? k_begin * lda_b + m0 * 2 : m0 * lda_b + k_begin * 2);
-    auto load_a = [&](int kt, auto buf_c) {
-        constexpr int BUF = decltype(buf_c)::value;
+    auto load_a = [&](int kt, int buf) __attribute__((always_inline)) {
         const int rem = k_len - kt * BK;
-        const uint32_t dst = lds_addr(BUF ? a_lds1 : a_lds0) + uint32_t(wave) * 1024u;
-        const i32x4_t ra = DW ? ring_rsrc(a_base + int64_t(kt) * BK * lda_b,
-                                          uint32_t(__builtin_amdgcn_readfirstlane(int((rem <= 0 ? 0 : rem < BK ? rem : BK) * lda_b))))
-                              : ring_rsrc(a_base + int64_t(kt) * 128, rem > 0 ? a_bytes : 0u);
+        const uint32_t dst = lds_addr(a_lds[0]) + uint32_t(buf * A_STAGE) + uint32_t(wave) * 1024u;
+        const i32x4_t ra = DW ? ring_rsrc(uniform(a_base + int64_t(kt) * BK * lda_b),
+                                          uniform(uint32_t((rem <= 0 ? 0 : rem < BK ? rem : BK) * lda_b)))
+                              : ring_rsrc(uniform(a_base + int64_t(kt) * (BK * 2)), uniform(rem > 0 ? a_bytes : 0u));
 #pragma unroll
         for (int i = 0; i < A_INSTR; ++i)
             ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
@@ -338,7 +376,7 @@ void mx_grad_kernel(MxArgs a) {
     const bool b_in2 = n0 + b_blk * kMxBlock + 16 < N;
     u32x4_t raw[2][CODES / 16];
     uint32_t raw_scale[2];
-    auto load_b = [&](int kt, auto set_c) {
+    auto load_b = [&](int kt, auto set_c) __attribute__((always_inline)) {
         constexpr int SET = decltype(set_c)::value;
         const bool in = b_in && kt * BK + b_row < k_len;
         const __amdgpu_buffer_rsrc_t rq = make_rsrc(q_base + int64_t(kt) * BK * ldq, kOOB);
@@ -350,7 +388,7 @@ void mx_grad_kernel(MxArgs a) {
     };
     const int b_wo = b_blk * REGION + b_row * 64, b_flip = (b_blk >> 2) & 1;
     // Chunk t (eight columns) of the thread's block, converted and written.
-    auto write_b = [&](auto set_c, auto buf_c, auto t_c) {
+    auto write_b = [&](auto set_c, auto buf_c, auto t_c) __attribute__((always_inline)) {
         constexpr int SET = decltype(set_c)::value, T = decltype(t_c)::value;
         uint8_t *const dst = decltype(buf_c)::value ? b_lds1 : b_lds0;
         u32x4_t v;
@@ -377,24 +415,23 @@ void mx_grad_kernel(MxArgs a) {
         for (int i = 0; i < TM; ++i) {
             const int colb = (wrow0 + 32 * i) * 2 + (g16 & 3) * 8 + (grp & 1) * 32;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) a_fo[i][s] = (16 * s + tr_k) * A_PITCH + (((colb >> 4) ^ bz) << 4) + (colb & 15);
+            for (int s = 0; s < 4; ++s) a_fo[i][s] = (64 * group + 16 * s + tr_k) * A_PITCH + (((colb >> 4) ^ bz) << 4) + (colb & 15);
         }
     } else {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) a_fo[p][s] = r0 * 128 + 16 * (swz(2 * s + half, r0) ^ (4 * p));
+            for (int s = 0; s < 4; ++s) a_fo[p][s] = group * A_PART + r0 * 128 + 16 * (swz(2 * s + half, r0) ^ (4 * p));
     }
     int b_fo[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int blk = wcol0 / 32 + j;
-        b_fo[j] = blk * REGION + tr_k * 64 + 16 * ((2 * (grp & 1) + ((g16 & 3) >> 1)) ^ ((blk >> 2) & 1)) + 8 * (g16 & 1);
+        b_fo[j] = blk * REGION + (64 * group + tr_k) * 64 + 16 * ((2 * (grp & 1) + ((g16 & 3) >> 1)) ^ ((blk >> 2) & 1)) + 8 * (g16 & 1);
     }
     u32x4_t fa[2][TM], fb[2][TN];
-    auto load_frags = [&](auto buf_c, auto s_c, auto slot_c) {
+    auto load_frags = [&](const uint8_t *as, auto buf_c, auto s_c, auto slot_c) __attribute__((always_inline)) {
         constexpr int S = decltype(s_c)::value, SLOT = decltype(slot_c)::value;
-        const uint8_t *const as = decltype(buf_c)::value ? a_lds1 : a_lds0;
         const uint8_t *const bs = decltype(buf_c)::value ? b_lds1 : b_lds0;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -420,7 +457,7 @@ void mx_grad_kernel(MxArgs a) {
     for (int i = 0; i < TM; ++i) fa[1][i] = u32x4_t{0u, 0u, 0u, 0u};
 #pragma unroll
     for (int j = 0; j < TN; ++j) fb[1][j] = u32x4_t{0u, 0u, 0u, 0u};
-    auto multiply = [&](auto slot_c) {
+    auto multiply = [&](auto slot_c) __attribute__((always_inline)) {
         constexpr int SLOT = decltype(slot_c)::value;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -433,49 +470,57 @@ void mx_grad_kernel(MxArgs a) {
     using I3 = std::integral_constant<int, 3>;
 
     // K ends inside a chunk of A's rows: what follows it is not part of the sum.
-    auto cut_a = [&](int kt, auto buf_c) {
+    auto cut_a = [&](int kt, uint8_t *as) __attribute__((always_inline)) {
         if constexpr (!DW) {
             if (kt != nk - 1 || (k_len & 7) == 0) return;
-            uint8_t *const as = decltype(buf_c)::value ? a_lds1 : a_lds0;
-            const int kl = k_len - kt * BK;
+            const int kl = k_len - kt * BK, part = kl / 64, c = kl % 64 / 8;
             for (int r = tid; r < BM; r += THREADS)
-                for (int e = kl & 7; e < 8; ++e) reinterpret_cast<uint16_t *>(as + r * 128 + 16 * swz(kl / 8, r))[e] = 0;
+                for (int e = kl & 7; e < 8; ++e) reinterpret_cast<uint16_t *>(as + part * A_PART + r * 128 + 16 * swz(c, r))[e] = 0;
             phase_barrier();
         }
     };
-    // One stage: buffer BUF holds stage kt, set 1 - BUF the codes of stage kt + 1.  On entry
-    // slot 1 holds the fragments of the stage before's last k-step, whose MFMAs run under the
-    // latency of this stage's first reads.
-    auto stage = [&](int kt, auto buf_c) {
+    // One stage: A's buffer a_buf and B's BUF hold stage kt, set 1 - BUF the codes of stage
+    // kt + 1.  On entry slot 1 holds the fragments of the stage before's last k-step, whose
+    // MFMAs run under the latency of this stage's first reads.
+    //
+    // Loads complete in the order they were issued: A of stage kt + 1 (NSA = 3: issued a stage
+    // ago, ahead of the codes) is in LDS when the codes of stage kt + 1 have arrived.  With
+    // two buffers it is issued at the stage's begin and waited for at its end.
+    int a_buf = 0;
+    auto stage = [&](int kt, auto buf_c) __attribute__((always_inline)) {
         constexpr int BUF = decltype(buf_c)::value;
         using OTHER = std::integral_constant<int, 1 - BUF>;
-        cut_a(kt, buf_c);
-        // The codes of stage kt + 1 have arrived (loaded a stage ago): said here, before the
-        // loads below, so that their use does not wait for those.
+        uint8_t *const as = a_lds[0] + a_buf * A_STAGE;
+        cut_a(kt, as);
+        // The codes of stage kt + 1 have arrived: said here, before the loads below, so that
+        // their use does not wait for those.
 #pragma unroll
         for (int i = 0; i < CODES / 16; ++i) asm volatile("" : "+v"(raw[1 - BUF][i]));
         asm volatile("" : "+v"(raw_scale[1 - BUF]));
-        load_a(kt + 1, OTHER{});
+        load_a(kt + NSA - 1, a_buf == 0 ? NSA - 1 : a_buf - 1);
         load_b(kt + 2, buf_c);
-        load_frags(buf_c, I0{}, I0{});
+        load_frags(as, buf_c, I0{}, I0{});
         write_b(OTHER{}, OTHER{}, I0{});
         multiply(I1{});
-        load_frags(buf_c, I1{}, I1{});
+        load_frags(as, buf_c, I1{}, I1{});
         write_b(OTHER{}, OTHER{}, I1{});
         multiply(I0{});
-        load_frags(buf_c, I2{}, I0{});
+        load_frags(as, buf_c, I2{}, I0{});
         write_b(OTHER{}, OTHER{}, I2{});
         multiply(I1{});
-        load_frags(buf_c, I3{}, I1{});
+        load_frags(as, buf_c, I3{}, I1{});
         write_b(OTHER{}, OTHER{}, I3{});
         multiply(I0{});
-        ring_barrier<RAW>();              // A of stage kt + 1 is in LDS; the codes of kt + 2 may be on their way
+        if constexpr (NSA == 2) ring_barrier<RAW>();      // the codes of kt + 2 may be on their way
+        else phase_barrier();
+        a_buf = a_buf == NSA - 1 ? 0 : a_buf + 1;
     };
 
     if (nk > 0) {
         load_b(0, I0{});
         load_b(1, I1{});
-        load_a(0, I0{});
+        load_a(0, 0);
+        if constexpr (NSA == 3) load_a(1, 1);
         static_for<0, 4>([&](auto t) { write_b(I0{}, I0{}, t); });
         stage_barrier();
         int kt = 0;
@@ -487,7 +532,8 @@ void mx_grad_kernel(MxArgs a) {
         multiply(I1{});
     }
     stage_barrier();
-    mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, true, *reinterpret_cast<int *>(a_lds0));
+    mx_sum_groups<WK, BLOCKS * REGION>(acc, b_lds0, group, tid);
+    mx_store_tile<BM, BN, TM, TN>(a.g, acc, tm, tn, slice, m0 + wrow0, n0 + wcol0, lane, group == 0, *reinterpret_cast<int *>(a_lds[0]));
 }
 
 }  // namespace gemm

@@ -17,6 +17,14 @@ typedef unsigned u32_any_mx __attribute__((aligned(1)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
+// A value that is the same in every lane, as a scalar: the compiler may form the uniform operands of
+// a buffer resource on the vector unit, which the inline-assembly loads cannot take.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return uint32_t(__builtin_amdgcn_readfirstlane(int(v))); }
+__device__ __forceinline__ const uint8_t *uniform(const uint8_t *p) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const uint8_t *>(uint64_t(uniform(uint32_t(at))) | (uint64_t(uniform(uint32_t(at >> 32))) << 32));
+}
+
 // The scale operand of the conversions for scale byte e: they use its exponent field.
 __device__ __forceinline__ float mx4_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
 

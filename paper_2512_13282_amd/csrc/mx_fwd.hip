@@ -28,7 +28,7 @@ hipError_t launch_mx_fwd(int32_t cfg, const MxArgs &a, int64_t grid, hipStream_t
         case 20: return launch_mx(mx_fwd_kernel<64,128,2,2,2,2,128,3,1024>, a, g, 512, 0, s);
         case 21: return launch_mx(mx_fwd_kernel<128,256,2,4,1,2,64,3,1024>, a, g, 512, 0, s);
         case 22: return launch_mx(mx_fwd_kernel<128,256,2,4,1,4,64,2,1024>, a, g, 512, 0, s);
-        case 23: return launch_mx(mx_fwd_kernel<32,256,1,8,2,4,256,2,1024>, a, g, 1024, 0, s);
+        case 23: return launch_mx(mx_fwd_kernel<64,128,1,4,2,2,256,2,1024>, a, g, 512, 0, s);
         case 24: return launch_mx(mx_fwd_kernel<32,128,1,2,4,2,256,3,1024>, a, g, 512, 0, s);
         case 25: return launch_mx(mx_fwd_kernel<64,64,1,2,4,2,256,3,1024>, a, g, 512, 0, s);
         case 26: return launch_mx(mx_fwd_kernel<32,64,1,2,4,2,256,3,1024>, a, g, 512, 0, s);

@@ -28,12 +28,36 @@ const MxConfig kMxConfigs[] = {
     {MX_FWD, 64, 128, 8, 1, "mx_T20_64x128_2x2x2_w2_k128_n3"},
     {MX_FWD, 128, 256, 8, 1, "mx_T21_128x256_2x4x1_w2_k64_n3"},
     {MX_FWD, 128, 256, 8, 2, "mx_T22_128x256_2x4x1_w4_k64_n2"},
-    {MX_FWD, 32, 256, 16, 1, "mx_T23_32x256_1x8x2_w4_k256_n2"},
+    {MX_FWD, 64, 128, 8, 1, "mx_T23_64x128_1x4x2_w2_k256_n2"},
     {MX_FWD, 32, 128, 8, 1, "mx_T24_32x128_1x2x4_w2_k256_n3"},
     {MX_FWD, 64, 64, 8, 1, "mx_T25_64x64_1x2x4_w2_k256_n3"},
     {MX_FWD, 32, 64, 8, 1, "mx_T26_32x64_1x2x4_w2_k256_n3"},
     {MX_FWD, 64, 64, 8, 1, "mx_T27_64x64_2x2x2_w2_k256_n2"},
     {MX_FWD, 128, 128, 8, 1, "mx_T28_128x128_2x2x2_w2_k128_n3"},
+    {MX_DX, 32, 64, 8, 1, "mx_T29_32x64_1x2x4_w2_a3"},
+    {MX_DX, 32, 64, 4, 2, "mx_T30_32x64_1x2x2_w4_a3"},
+    {MX_DX, 32, 128, 8, 2, "mx_T31_32x128_1x4x2_w2_a3"},
+    {MX_DX, 64, 64, 4, 2, "mx_T32_64x64_1x2x2_w2_a3"},
+    {MX_DX, 64, 128, 8, 1, "mx_T33_64x128_1x4x2_w2_a3"},
+    {MX_DX, 64, 128, 8, 1, "mx_T34_64x128_2x2x2_w2_a3"},
+    {MX_DX, 64, 128, 4, 2, "mx_T35_64x128_2x2x1_w3_a3"},
+    {MX_DX, 128, 64, 2, 2, "mx_T36_128x64_2x1x1_w2_a3"},
+    {MX_DX, 128, 128, 4, 1, "mx_T37_128x128_2x2x1_w2_a3"},
+    {MX_DX, 64, 256, 8, 1, "mx_T38_64x256_1x8x1_w2_a3"},
+    {MX_DX, 128, 256, 8, 1, "mx_T39_128x256_2x4x1_w2_a3"},
+    {MX_DX, 128, 256, 8, 1, "mx_T40_128x256_2x4x1_w4_a2"},
+    {MX_DW, 32, 64, 8, 1, "mx_T41_32x64_1x2x4_w2_a3"},
+    {MX_DW, 32, 64, 4, 2, "mx_T42_32x64_1x2x2_w4_a3"},
+    {MX_DW, 32, 128, 8, 2, "mx_T43_32x128_1x4x2_w2_a3"},
+    {MX_DW, 64, 64, 4, 2, "mx_T44_64x64_1x2x2_w2_a3"},
+    {MX_DW, 64, 128, 8, 1, "mx_T45_64x128_1x4x2_w2_a3"},
+    {MX_DW, 64, 128, 8, 1, "mx_T46_64x128_2x2x2_w2_a3"},
+    {MX_DW, 64, 128, 4, 2, "mx_T47_64x128_2x2x1_w3_a3"},
+    {MX_DW, 128, 64, 2, 2, "mx_T48_128x64_2x1x1_w2_a3"},
+    {MX_DW, 128, 128, 4, 1, "mx_T49_128x128_2x2x1_w2_a3"},
+    {MX_DW, 64, 256, 8, 1, "mx_T50_64x256_1x8x1_w2_a3"},
+    {MX_DW, 128, 256, 8, 1, "mx_T51_128x256_2x4x1_w2_a3"},
+    {MX_DW, 128, 256, 8, 1, "mx_T52_128x256_2x4x1_w4_a2"},
 };
 const int32_t kMxNumConfigs = sizeof(kMxConfigs) / sizeof(kMxConfigs[0]);
 

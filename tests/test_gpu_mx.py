@@ -241,7 +241,7 @@ def test_same_bits_on_every_run_and_stream(op, size):
 
 def configurations(op):
     """The configurations of an operator (mx_force_plan refuses those of another)."""
-    found = [c for c in range(64) if mx.mx_force_plan(OPS.index(op), c, 0) == b.GEMM_OK]
+    found = [c for c in range(128) if mx.mx_force_plan(OPS.index(op), c, 0) == b.GEMM_OK]
     mx.mx_force_plan(OPS.index(op))
     return found
 
