@@ -132,17 +132,27 @@ void mx_fwd_kernel(MxArgs a) {
     const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + m0 * lda_b + k_begin * 2;
     const uint8_t *const b_base = static_cast<const uint8_t *>(a.g.B) + n0 * ldq + k_begin / 2;
 
-    auto load_stage = [&](int kt, auto buf_c) __attribute__((always_inline)) {
-        constexpr int BUF = decltype(buf_c)::value;
+    // Loads FROM .. TO - 1 of a stage's LPS (W's first).  A stage's loads go out a few with each
+    // k-step: all at once they back up the vector memory path, and every wave of the
+    // workgroup waits behind them at the same time instead of multiplying.
+    auto load_some = [&](int kt, auto buf_c, auto from_c, auto to_c) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(buf_c)::value, FROM = decltype(from_c)::value, TO = decltype(to_c)::value;
         const int rem = k_len - kt * KS;
         const uint32_t dst = lds_addr(lds[BUF]) + uint32_t(wave) * 1024u;
         const i32x4_t ra = ring_rsrc(uniform(a_base + int64_t(kt) * (KS * 2)), uniform(rem > 0 ? a_bytes : 0u));
         const i32x4_t rb = ring_rsrc(uniform(b_base + int64_t(kt) * PITCH), uniform(rem > 0 ? b_bytes : 0u));
 #pragma unroll
-        for (int i = 0; i < B_INSTR; ++i)
-            ring_load16(rb, dst + A_STAGE + i * (WAVES * 1024), b_k[i] < rem ? b_voff[i] : kOOB);
-#pragma unroll
-        for (int i = 0; i < A_INSTR; ++i) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
+        for (int i = FROM; i < TO; ++i) {
+            if (i < B_INSTR) {
+                ring_load16(rb, dst + A_STAGE + i * (WAVES * 1024), b_k[i] < rem ? b_voff[i] : kOOB);
+            } else {
+                const int j = i - B_INSTR;
+                ring_load16(ra, dst + j * (WAVES * 1024), a_k[j] < rem ? a_voff[j] : kOOB);
+            }
+        }
+    };
+    auto load_stage = [&](int kt, auto buf_c) __attribute__((always_inline)) {
+        load_some(kt, buf_c, std::integral_constant<int, 0>{}, std::integral_constant<int, LPS>{});
     };
     // The scales of rows n0.. from k0 (of this slice) on, 16 or 4 bytes at a time where rows and
     // addresses allow it, else byte by byte.  Rows past N take 0; a row's last piece may go on
@@ -234,10 +244,9 @@ void mx_fwd_kernel(MxArgs a) {
                     reinterpret_cast<uint16_t *>(st + part * A_PART + r * 128 + 16 * swz(c, r))[e] = 0;
             phase_barrier();
         }
-        load_stage(kt + NS - 1, std::integral_constant<int, (BUF + NS - 1) % NS>{});
         const int block0 = (kt * KS % PANEL) / kMxBlock + half;
-#pragma unroll
-        for (int p = 0; p < PARTS / WK; ++p) {
+        static_for<0, PARTS / WK>([&](auto p_c) __attribute__((always_inline)) {
+            constexpr int p = decltype(p_c)::value;
             const int q = p * WK + group, b = block0 + 2 * q;
             const bool in = kt * (KS / kMxBlock) + half + 2 * q < blocks;     // past the end: no NaN for A's zeros
             u32x4_t w[TN];
@@ -248,8 +257,10 @@ void mx_fwd_kernel(MxArgs a) {
                 w[j] = *reinterpret_cast<const u32x4_t *>(st + b_fo[j][p]);
                 s[j] = mx4_scale(in ? panel[r * P_PITCH + 16 * ((b >> 4) ^ p_swz(r)) + (b & 15)] : 0);
             }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            static_for<0, 4>([&](auto t_c) __attribute__((always_inline)) {
+                constexpr int t = decltype(t_c)::value, STEP = 4 * p + t, STEPS = 4 * PARTS / WK;
+                load_some(kt + NS - 1, std::integral_constant<int, (BUF + NS - 1) % NS>{},
+                          std::integral_constant<int, STEP * LPS / STEPS>{}, std::integral_constant<int, (STEP + 1) * LPS / STEPS>{});
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
                     fa[t & 1][i] = *reinterpret_cast<const u32x4_t *>(st + q * A_PART + a_fo[i & 1][t] + 4096 * i);
@@ -257,8 +268,8 @@ void mx_fwd_kernel(MxArgs a) {
 #pragma unroll
                 for (int j = 0; j < TN; ++j) fb[t & 1][j] = mx4_to_bf16(w[j][t], s[j]);
                 __builtin_amdgcn_sched_barrier(0);        // one k-step ahead, no further: registers
-            }
-        }
+            });
+        });
     };
 
     if (nk > 0) {
@@ -299,9 +310,9 @@ void mx_fwd_kernel(MxArgs a) {
 // A transpose read then covers two runs of 256 bytes, and the eight lanes that write one row's
 // chunks hit different banks (the regions of blocks 0-3 by their offset, 4-7 by a flipped chunk).
 //
-// B's codes are loaded two stages ahead into registers, A one stage ahead.
+// B's codes are loaded two stages ahead into registers, A one stage ahead into LDS.
 // ---------------------------------------------------------------------------
-template <int OP, int BM, int BN, int WM, int WN, int WK, int WAVES_PER_EU, int NSA>
+template <int OP, int BM, int BN, int WM, int WN, int WK, int WAVES_PER_EU>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN * WK, 64 * WM * WN * WK),
                           amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU)))
 void mx_grad_kernel(MxArgs a) {
@@ -319,7 +330,7 @@ void mx_grad_kernel(MxArgs a) {
     static_assert(BK * BLOCKS == THREADS, "one block of one row per thread");
     static_assert(WK == 1 || THREADS / WK <= 256, "mx_sum_groups");
 
-    __shared__ __attribute__((aligned(1024))) uint8_t a_lds[NSA][A_STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t a_lds[2][A_STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t b_lds0[BLOCKS * REGION];
     __shared__ __attribute__((aligned(1024))) uint8_t b_lds1[BLOCKS * REGION];
 
@@ -362,8 +373,7 @@ void mx_grad_kernel(MxArgs a) {
                                           uniform(uint32_t((rem <= 0 ? 0 : rem < BK ? rem : BK) * lda_b)))
                               : ring_rsrc(uniform(a_base + int64_t(kt) * (BK * 2)), uniform(rem > 0 ? a_bytes : 0u));
 #pragma unroll
-        for (int i = 0; i < A_INSTR; ++i)
-            ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
+        for (int i = 0; i < A_INSTR; ++i) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
     };
 
     // ---- B: this thread's block of row b_row of each stage.
@@ -479,25 +489,20 @@ void mx_grad_kernel(MxArgs a) {
             phase_barrier();
         }
     };
-    // One stage: A's buffer a_buf and B's BUF hold stage kt, set 1 - BUF the codes of stage
-    // kt + 1.  On entry slot 1 holds the fragments of the stage before's last k-step, whose
-    // MFMAs run under the latency of this stage's first reads.
-    //
-    // Loads complete in the order they were issued: A of stage kt + 1 (NSA = 3: issued a stage
-    // ago, ahead of the codes) is in LDS when the codes of stage kt + 1 have arrived.  With
-    // two buffers it is issued at the stage's begin and waited for at its end.
-    int a_buf = 0;
+    // One stage: buffers BUF hold stage kt, set 1 - BUF the codes of stage kt + 1.  On entry
+    // slot 1 holds the fragments of the stage before's last k-step, whose MFMAs run under the
+    // latency of this stage's first reads.
     auto stage = [&](int kt, auto buf_c) __attribute__((always_inline)) {
         constexpr int BUF = decltype(buf_c)::value;
         using OTHER = std::integral_constant<int, 1 - BUF>;
-        uint8_t *const as = a_lds[0] + a_buf * A_STAGE;
-        cut_a(kt, as);
-        // The codes of stage kt + 1 have arrived: said here, before the loads below, so that
-        // their use does not wait for those.
+        const uint8_t *const as = a_lds[BUF];
+        cut_a(kt, a_lds[BUF]);
+        // The codes of stage kt + 1 have arrived (loaded a stage ago): said here, before the
+        // loads below, so that their use does not wait for those.
 #pragma unroll
         for (int i = 0; i < CODES / 16; ++i) asm volatile("" : "+v"(raw[1 - BUF][i]));
         asm volatile("" : "+v"(raw_scale[1 - BUF]));
-        load_a(kt + NSA - 1, a_buf == 0 ? NSA - 1 : a_buf - 1);
+        load_a(kt + 1, 1 - BUF);
         load_b(kt + 2, buf_c);
         load_frags(as, buf_c, I0{}, I0{});
         write_b(OTHER{}, OTHER{}, I0{});
@@ -511,16 +516,13 @@ void mx_grad_kernel(MxArgs a) {
         load_frags(as, buf_c, I3{}, I1{});
         write_b(OTHER{}, OTHER{}, I3{});
         multiply(I0{});
-        if constexpr (NSA == 2) ring_barrier<RAW>();      // the codes of kt + 2 may be on their way
-        else phase_barrier();
-        a_buf = a_buf == NSA - 1 ? 0 : a_buf + 1;
+        ring_barrier<RAW>();              // A of stage kt + 1 is in LDS; the codes of kt + 2 may be on their way
     };
 
     if (nk > 0) {
         load_b(0, I0{});
         load_b(1, I1{});
         load_a(0, 0);
-        if constexpr (NSA == 3) load_a(1, 1);
         static_for<0, 4>([&](auto t) { write_b(I0{}, I0{}, t); });
         stage_barrier();
         int kt = 0;

@@ -15,25 +15,15 @@ hipError_t launch_mx_fwd(int32_t cfg, const MxArgs &a, int64_t grid, hipStream_t
         return launch_mx(mx_decode_kernel<1, 8, 2>, a, d, 512, x > sums ? x : sums, s);
     }
     switch (cfg) {
-        case 2: return launch_mx(mx_fwd_kernel<32, 128, 1, 4, 1, 2, 128, 3, 1024>, a, g, 256, 0, s);
-        case 3: return launch_mx(mx_fwd_kernel<64, 128, 2, 2, 1, 2, 128, 3, 1024>, a, g, 256, 0, s);
-        case 4: return launch_mx(mx_fwd_kernel<128, 128, 2, 2, 1, 2, 64, 3, 1024>, a, g, 256, 0, s);
-        case 5: return launch_mx(mx_fwd_kernel<256, 256, 2, 4, 1, 2, 64, 3, 4096>, a, g, 512, 0, s);
-        case 14: return launch_mx(mx_fwd_kernel<32,128,1,4,2,2,128,3,1024>, a, g, 512, 0, s);
-        case 15: return launch_mx(mx_fwd_kernel<32,128,1,4,2,2,128,4,1024>, a, g, 512, 0, s);
-        case 16: return launch_mx(mx_fwd_kernel<32,128,1,4,2,2,256,3,1024>, a, g, 512, 0, s);
-        case 17: return launch_mx(mx_fwd_kernel<32,128,1,4,4,4,256,2,1024>, a, g, 1024, 0, s);
-        case 18: return launch_mx(mx_fwd_kernel<32,128,1,4,2,4,128,2,1024>, a, g, 512, 0, s);
-        case 19: return launch_mx(mx_fwd_kernel<64,128,1,4,2,2,128,3,1024>, a, g, 512, 0, s);
-        case 20: return launch_mx(mx_fwd_kernel<64,128,2,2,2,2,128,3,1024>, a, g, 512, 0, s);
-        case 21: return launch_mx(mx_fwd_kernel<128,256,2,4,1,2,64,3,1024>, a, g, 512, 0, s);
-        case 22: return launch_mx(mx_fwd_kernel<128,256,2,4,1,4,64,2,1024>, a, g, 512, 0, s);
-        case 23: return launch_mx(mx_fwd_kernel<64,128,1,4,2,2,256,2,1024>, a, g, 512, 0, s);
-        case 24: return launch_mx(mx_fwd_kernel<32,128,1,2,4,2,256,3,1024>, a, g, 512, 0, s);
-        case 25: return launch_mx(mx_fwd_kernel<64,64,1,2,4,2,256,3,1024>, a, g, 512, 0, s);
-        case 26: return launch_mx(mx_fwd_kernel<32,64,1,2,4,2,256,3,1024>, a, g, 512, 0, s);
-        case 27: return launch_mx(mx_fwd_kernel<64,64,2,2,2,2,256,2,1024>, a, g, 512, 0, s);
-        case 28: return launch_mx(mx_fwd_kernel<128,128,2,2,2,2,128,3,1024>, a, g, 512, 0, s);
+        case 2: return launch_mx(mx_fwd_kernel<32, 64, 1, 2, 4, 2, 256, 3, 1024>, a, g, 512, 0, s);
+        case 3: return launch_mx(mx_fwd_kernel<32, 128, 1, 4, 2, 2, 256, 3, 1024>, a, g, 512, 0, s);
+        case 4: return launch_mx(mx_fwd_kernel<64, 64, 1, 2, 4, 2, 256, 3, 1024>, a, g, 512, 0, s);
+        case 5: return launch_mx(mx_fwd_kernel<64, 128, 1, 4, 2, 2, 128, 3, 1024>, a, g, 512, 0, s);
+        case 6: return launch_mx(mx_fwd_kernel<128, 128, 2, 2, 2, 2, 128, 3, 1024>, a, g, 512, 0, s);
+        case 7: return launch_mx(mx_fwd_kernel<128, 128, 2, 2, 1, 2, 64, 3, 1024>, a, g, 256, 0, s);
+        case 8: return launch_mx(mx_fwd_kernel<128, 256, 2, 4, 1, 2, 64, 3, 1024>, a, g, 512, 0, s);
+        case 9: return launch_mx(mx_fwd_kernel<192, 256, 2, 4, 1, 2, 64, 3, 4096>, a, g, 512, 0, s);
+        case 10: return launch_mx(mx_fwd_kernel<256, 256, 2, 4, 1, 2, 64, 3, 4096>, a, g, 512, 0, s);
         default: return hipErrorInvalidValue;
     }
 }
