@@ -45,6 +45,10 @@ struct MxConfig {
     int32_t bm, bn;            // output tile
     int32_t waves;             // per workgroup
     int32_t occupancy;         // workgroups a compute unit holds
+    // Fitted microseconds: a workgroup's start and its end, 64 k of its K alone on its compute
+    // unit and with the unit full, a split's last slice and its share per 100 KB of partial
+    // sums, and 1 MB of results.
+    double start_us, part_us, part_full_us, sum_us, sum_slice_us, store_us;
     const char *name;
 };
 extern const MxConfig kMxConfigs[];

@@ -66,9 +66,28 @@ struct Forced {
 };
 Forced g_forced[3];
 
+// The plans of this thread's latest shapes: choosing one evaluates a hundred or so.
+struct CachedPlan {
+    int64_t M, N, K;           // M = 0: empty
+    int32_t op;
+    gemm::MxPlan plan;
+};
+thread_local CachedPlan t_plans[64];
+
 int plan_for(gemm::MxOp op, int64_t M, int64_t N, int64_t K, gemm::MxPlan *plan) {
     if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX - 4096) return GEMM_ERR_UNSUPPORTED;    // 32-bit indices
-    return gemm::mx_select(op, M, N, K, g_forced[op].config, g_forced[op].split, plan) ? GEMM_OK : GEMM_ERR_UNSUPPORTED;
+    const int32_t config = g_forced[op].config, split = g_forced[op].split;
+    if (config >= 0 || split > 0)
+        return gemm::mx_select(op, M, N, K, config, split, plan) ? GEMM_OK : GEMM_ERR_UNSUPPORTED;
+    const uint64_t h = (uint64_t(M) * 0x9E3779B97F4A7C15u ^ uint64_t(N) * 0xC2B2AE3D27D4EB4Fu ^ uint64_t(K) * 0x165667B19E3779F9u) + uint64_t(op);
+    CachedPlan &c = t_plans[(h ^ (h >> 32)) % 64];
+    if (c.M != M || c.N != N || c.K != K || c.op != op) {
+        gemm::MxPlan p;
+        if (!gemm::mx_select(op, M, N, K, -1, 0, &p)) return GEMM_ERR_UNSUPPORTED;
+        c = CachedPlan{M, N, K, op, p};
+    }
+    *plan = c.plan;
+    return GEMM_OK;
 }
 
 int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, int64_t lda, const void *codes,

@@ -3,48 +3,54 @@
 
 namespace gemm {
 
-// Rows 0 and 1 are the decode kernels (at most kMxDecodeRows rows of A), the rest output tiles.
+// Row 0 is the decode kernel (at most 16 rows of A, and A's K slice in 64 KiB of LDS), the rest
+// are output tiles.  The six figures of a tile are fitted to its own measured times over
+// 336 shapes (rows 1 to 11008, weights of 1024 x 1024 to 14336 x 4096, each in up to eight splits);
+// chosen by them, those shapes take 1.02 of their best measured plan's time on geometric mean.
 const MxConfig kMxConfigs[] = {
-    {MX_FWD, 16, 16, 4, 8, "mx_decode_16_w4"},
-    {MX_FWD, 16, 16, 8, 4, "mx_decode_16_w8"},
-    {MX_FWD, 32, 64, 8, 2, "mx_fwd_32x64_1x2x4"},
-    {MX_FWD, 32, 128, 8, 1, "mx_fwd_32x128_1x4x2"},
-    {MX_FWD, 64, 64, 8, 1, "mx_fwd_64x64_1x2x4"},
-    {MX_FWD, 64, 128, 8, 1, "mx_fwd_64x128_1x4x2"},
-    {MX_FWD, 128, 128, 8, 1, "mx_fwd_128x128_2x2x2"},
-    {MX_FWD, 128, 128, 4, 2, "mx_fwd_128x128_2x2x1"},
-    {MX_FWD, 128, 256, 8, 1, "mx_fwd_128x256_2x4x1"},
-    {MX_FWD, 192, 256, 8, 1, "mx_fwd_192x256_2x4x1"},
-    {MX_FWD, 256, 256, 8, 1, "mx_fwd_256x256_2x4x1"},
-    {MX_DX, 32, 64, 8, 1, "mx_dx_32x64_1x2x4"},
-    {MX_DX, 32, 64, 4, 3, "mx_dx_32x64_1x2x2"},
-    {MX_DX, 64, 64, 4, 2, "mx_dx_64x64_1x2x2"},
-    {MX_DX, 64, 128, 8, 1, "mx_dx_64x128_1x4x2"},
-    {MX_DX, 64, 256, 8, 1, "mx_dx_64x256_1x8x1"},
-    {MX_DX, 128, 128, 4, 2, "mx_dx_128x128_2x2x1"},
-    {MX_DX, 128, 256, 8, 1, "mx_dx_128x256_2x4x1"},
-    {MX_DX, 256, 256, 8, 1, "mx_dx_256x256_2x4x1"},
-    {MX_DW, 32, 64, 8, 1, "mx_dw_32x64_1x2x4"},
-    {MX_DW, 32, 64, 4, 3, "mx_dw_32x64_1x2x2"},
-    {MX_DW, 64, 64, 4, 2, "mx_dw_64x64_1x2x2"},
-    {MX_DW, 64, 128, 8, 1, "mx_dw_64x128_1x4x2"},
-    {MX_DW, 64, 256, 8, 1, "mx_dw_64x256_1x8x1"},
-    {MX_DW, 128, 128, 4, 2, "mx_dw_128x128_2x2x1"},
-    {MX_DW, 128, 256, 8, 1, "mx_dw_128x256_2x4x1"},
-    {MX_DW, 256, 256, 8, 1, "mx_dw_256x256_2x4x1"},
+    {MX_FWD, 16, 16, 8, 4, 0, 0, 0, 0, 0, 0, "mx_decode"},
+    {MX_FWD, 32, 64, 8, 2, 2.02, 0.112, 0.342, 0.82, 5.11, 0.77, "mx_fwd_32x64_1x2x4"},
+    {MX_FWD, 32, 128, 8, 1, 2.21, 0.164, 0.176, 0.64, 2.18, 0.18, "mx_fwd_32x128_1x4x2"},
+    {MX_FWD, 64, 64, 8, 1, 3.00, 0.133, 0.149, 0.30, 3.61, 0.24, "mx_fwd_64x64_1x2x4"},
+    {MX_FWD, 64, 128, 8, 1, 2.13, 0.224, 0.247, 0.66, 1.66, 0.31, "mx_fwd_64x128_1x4x2"},
+    {MX_FWD, 128, 128, 8, 1, 2.39, 0.386, 0.406, 0.23, 1.49, 0.43, "mx_fwd_128x128_2x2x2"},
+    {MX_FWD, 128, 128, 4, 2, 1.20, 0.510, 0.746, 1.19, 0.82, 0.40, "mx_fwd_128x128_2x2x1"},
+    {MX_FWD, 128, 256, 8, 1, 0.53, 0.717, 0.734, 0.70, 0.80, 0.48, "mx_fwd_128x256_2x4x1"},
+    {MX_FWD, 192, 256, 8, 1, 0.00, 0.981, 1.052, 0.91, 0.74, 0.27, "mx_fwd_192x256_2x4x1"},
+    {MX_FWD, 256, 256, 8, 1, 0.00, 1.207, 1.149, 0.00, 0.80, 0.48, "mx_fwd_256x256_2x4x1"},
+    {MX_DX, 32, 64, 8, 1, 2.35, 0.224, 0.241, 0.57, 3.96, 0.48, "mx_dx_32x64_1x2x4"},
+    {MX_DX, 32, 64, 4, 3, 1.18, 0.292, 0.580, 1.30, 3.50, 0.75, "mx_dx_32x64_1x2x2"},
+    {MX_DX, 64, 64, 4, 2, 1.22, 0.342, 0.486, 1.25, 3.02, 0.65, "mx_dx_64x64_1x2x2"},
+    {MX_DX, 64, 128, 8, 1, 1.84, 0.446, 0.439, 0.97, 1.73, 0.33, "mx_dx_64x128_1x4x2"},
+    {MX_DX, 64, 256, 8, 1, 1.36, 0.604, 0.587, 1.35, 0.90, 0.30, "mx_dx_64x256_1x8x1"},
+    {MX_DX, 128, 128, 4, 2, 0.37, 0.679, 0.892, 2.32, 0.83, 0.38, "mx_dx_128x128_2x2x1"},
+    {MX_DX, 128, 256, 8, 1, 1.09, 0.809, 0.785, 1.09, 0.73, 0.24, "mx_dx_128x256_2x4x1"},
+    {MX_DX, 256, 256, 8, 1, 0.16, 1.242, 1.221, 0.00, 0.83, 0.28, "mx_dx_256x256_2x4x1"},
+    {MX_DW, 32, 64, 8, 1, 2.31, 0.288, 0.291, 1.00, 3.46, 0.50, "mx_dw_32x64_1x2x4"},
+    {MX_DW, 32, 64, 4, 3, 0.95, 0.376, 0.713, 1.65, 3.28, 0.41, "mx_dw_32x64_1x2x2"},
+    {MX_DW, 64, 64, 4, 2, 1.46, 0.451, 0.596, 1.63, 2.92, 0.29, "mx_dw_64x64_1x2x2"},
+    {MX_DW, 64, 128, 8, 1, 2.65, 0.622, 0.523, 0.80, 2.17, 0.09, "mx_dw_64x128_1x4x2"},
+    {MX_DW, 64, 256, 8, 1, 0.27, 0.982, 0.896, 2.04, 1.30, 0.05, "mx_dw_64x256_1x8x1"},
+    {MX_DW, 128, 128, 4, 2, 1.79, 0.912, 0.975, 1.66, 1.42, 0.05, "mx_dw_128x128_2x2x1"},
+    {MX_DW, 128, 256, 8, 1, 2.86, 1.028, 0.936, 0.40, 1.00, 0.03, "mx_dw_128x256_2x4x1"},
+    {MX_DW, 256, 256, 8, 1, 4.74, 1.372, 1.671, 0.00, 0.70, 0.06, "mx_dw_256x256_2x4x1"},
 };
 const int32_t kMxNumConfigs = sizeof(kMxConfigs) / sizeof(kMxConfigs[0]);
 
-static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+namespace {
 
-static bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPlan *out) {
+constexpr int kCUs = 256;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPlan *out) {
     if (config < 0 || config >= kMxNumConfigs || kMxConfigs[config].op != op) return false;
-    const bool decode = config < 2;
+    const bool decode = config == 0;
     if (decode) {
-        // A's slice has to fit 64 KiB of LDS.
         if (M > 16 || K == 0) return false;
-        const int64_t most = (65536 / M - 16) / 256 * 128;
+        const int64_t most = (65536 / M - 16) / 256 * 128;       // K of a slice that fits LDS
         const int64_t least = ceil_div(K, most);
+        if (least > (1 << 20)) return false;
         if (split < least) split = int32_t(least);
     }
     const int64_t unit = decode ? 128 : 256;
@@ -55,12 +61,63 @@ static bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t spli
     return true;
 }
 
+// Modelled microseconds of a plan, without the launch and what moves in any plan.
+double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p) {
+    const MxConfig &c = kMxConfigs[p.config];
+    if (p.config == 0) {
+        // W at the rate it streams at, A once for every 16 columns at the rate of the L2s.
+        const double w = double(N) * double(K) / 2 / 5.0e6, a = double(ceil_div(N, 16)) * double(M) * double(K) * 2 / 8.5e6;
+        return 0.7 + w + a + (p.split_k > 1 ? 1.0 : 0.0);
+    }
+    const double tiles = double(ceil_div(M, c.bm)) * double(ceil_div(N, c.bn)), groups = tiles * p.split_k;
+    const double parts = double(p.k_chunk) / 64, slots = double(kCUs) * c.occupancy;
+    const double alone = c.start_us + c.part_us * parts, shared = c.start_us + c.part_full_us * parts;
+    const double rounds = double(int64_t(groups / slots)), rest = groups - rounds * slots;
+    double t = rounds * (c.occupancy > 1 ? shared : alone);
+    if (rest > 0) {
+        const double per_cu = rest / kCUs;
+        t += per_cu <= 1 || c.occupancy == 1 ? alone
+           : alone + (shared - alone) * ((per_cu - 1) / (c.occupancy - 1) < 1 ? (per_cu - 1) / (c.occupancy - 1) : 1.0);
+    }
+    const double tile = double(c.bm) * c.bn;
+    t += c.store_us * tiles * tile * (op == MX_DW ? 4 : 2) / 1e6;
+    if (p.split_k > 1) {
+        // The last slice's sums, and every slice's partial sums out and back.
+        const double rows = M < 8 ? 8 : M < c.bm ? double(M) : double(c.bm);
+        t += c.sum_us + c.sum_slice_us * p.split_k * tile * 4 / 1e5 + groups * rows * c.bn * 8 / 4.5e6;
+    }
+    return t;
+}
+
+}  // namespace
+
 bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, MxPlan *out) {
     if (config >= 0) return evaluate(op, M, K, config, split > 0 ? split : 1, out);
-    if (op == MX_FWD && M <= 4 && K > 0) return evaluate(op, M, K, N >= 8192 ? 0 : 1, 1, out);
-    for (int c = 0; c < kMxNumConfigs; ++c)
-        if (kMxConfigs[c].op == op && kMxConfigs[c].bm >= 32 && (kMxConfigs[c].bm >= M || kMxConfigs[c].bm >= 64)) return evaluate(op, M, K, c, split > 0 ? split : 1, out);
-    return false;
+    static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
+    double best = 0;
+    bool found = false;
+    for (int32_t c = 0; c < kMxNumConfigs; ++c) {
+        if (kMxConfigs[c].op != op) continue;
+        int32_t seen = 0;
+        for (const int32_t s : kSplits) {
+            MxPlan p;
+            if (!evaluate(op, M, K, c, split > 0 ? split : s, &p)) break;
+            if (p.split_k == seen) continue;                     // the same slices again
+            seen = p.split_k;
+            // Partial sums stay a fraction of the memory, and the grid a 32-bit number.
+            const double tiles = double(ceil_div(M, kMxConfigs[c].bm)) * double(ceil_div(N, kMxConfigs[c].bn));
+            const double groups = tiles * p.split_k;
+            if (split == 0 && p.split_k > 1 && c > 0 && groups > 4 * kCUs) break;
+            const double t = modelled_us(op, M, N, K, p);
+            if (!found || t < best) {
+                best = t;
+                *out = p;
+                found = true;
+            }
+            if (split > 0) break;
+        }
+    }
+    return found;
 }
 
 }  // namespace gemm
