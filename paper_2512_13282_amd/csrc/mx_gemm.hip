@@ -6,14 +6,21 @@ namespace gemm {
 
 // Rows of `used` bytes at any address and stride, copied to rows of `pitch` bytes (a multiple
 // of 16) on 16-byte addresses, zeros behind each row: what the tile kernels load straight into
-// LDS, 16 aligned bytes at a time.
-__global__ __launch_bounds__(256) void mx_realign_kernel(const uint8_t *src, int64_t stride, int64_t used, uint8_t *dst,
-                                                         int64_t pitch, int64_t rows) {
-    const int64_t pieces = pitch / 16, total = rows * pieces, step = int64_t(gridDim.x) * 256;
+// LDS, 16 aligned bytes at a time.  Both operands in one launch, for the launch is what the
+// smaller copies cost.
+struct MxCopy {
+    const uint8_t *src;
+    uint8_t *dst;
+    int64_t stride, used, pitch, rows;     // rows 0: nothing to copy
+};
+__global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
+    const int64_t x_total = x.rows * (x.pitch / 16), total = x_total + y.rows * (y.pitch / 16), step = int64_t(gridDim.x) * 256;
     for (int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x; id < total; id += step) {
-        const int64_t r = id / pieces, c = id - r * pieces;
-        const uint8_t *const p = src + r * stride + 16 * c;
-        const int64_t left = used - 16 * c;
+        const bool first = id < x_total;
+        const int64_t at = first ? id : id - x_total, pieces = (first ? x.pitch : y.pitch) / 16;
+        const int64_t r = (at | pieces) >> 32 == 0 ? uint32_t(at) / uint32_t(pieces) : at / pieces, c = at - r * pieces;
+        const uint8_t *const p = first ? x.src + r * x.stride + 16 * c : y.src + r * y.stride + 16 * c;
+        const int64_t left = (first ? x.used : y.used) - 16 * c;
         u32x4_t v{0u, 0u, 0u, 0u};
         if (left >= 16) {
             v = *reinterpret_cast<const u32x4_any_mx *>(p);
@@ -22,7 +29,7 @@ __global__ __launch_bounds__(256) void mx_realign_kernel(const uint8_t *src, int
             for (int e = 0; e < 16; ++e)
                 if (e < left) v[e / 4] |= uint32_t(p[e]) << (8 * (e & 3));
         }
-        *reinterpret_cast<u32x4_t *>(dst + r * pitch + 16 * c) = v;
+        *reinterpret_cast<u32x4_t *>(first ? x.dst + r * x.pitch + 16 * c : y.dst + r * y.pitch + 16 * c) = v;
     }
 }
 
@@ -34,12 +41,6 @@ bool loadable(const void *p, int64_t stride) {
 }
 int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
-bool realign(const void *src, int64_t stride, int64_t used, void *dst, int64_t rows, hipStream_t stream) {
-    const int64_t n = (rows * (padded(used) / 16) + 255) / 256;
-    hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream,
-                       static_cast<const uint8_t *>(src), stride, used, static_cast<uint8_t *>(dst), padded(used), rows);
-    return hipGetLastError() == hipSuccess;
-}
 }  // namespace
 
 int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_ptr) {
@@ -81,21 +82,27 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
         a.g.workspace = ws;
         a.g.counters = counters;
         uint8_t *const copies = static_cast<uint8_t *>(ws) + partial;
-        if (copy_a) {
-            if (!realign(a.g.A, a.g.lda * 2, a_used, copies, a_rows, stream)) return LAUNCH_HIP_ERROR;
-            a.g.A = copies;
-            a.g.lda = padded(a_used) / 2;
-        }
-        if (copy_b) {
-            if (!realign(a.g.B, a.g.ldb, b_used, copies + a_bytes, b_rows, stream)) return LAUNCH_HIP_ERROR;
-            a.g.B = copies + a_bytes;
-            a.g.ldb = padded(b_used);
+        if (copy_a || copy_b) {
+            MxCopy x{}, y{};
+            if (copy_a) {
+                x = MxCopy{static_cast<const uint8_t *>(a.g.A), copies, a.g.lda * 2, a_used, padded(a_used), a_rows};
+                a.g.A = x.dst;
+                a.g.lda = x.pitch / 2;
+            }
+            if (copy_b) {
+                y = MxCopy{static_cast<const uint8_t *>(a.g.B), copies + a_bytes, a.g.ldb, b_used, padded(b_used), b_rows};
+                a.g.B = y.dst;
+                a.g.ldb = y.pitch;
+            }
+            const int64_t n = ((a_bytes + b_bytes) / 16 + 255) / 256;
+            hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream, x, y);
+            if (hipGetLastError() != hipSuccess) return LAUNCH_HIP_ERROR;
         }
     }
     hipError_t e = op == MX_FWD ? launch_mx_fwd(plan.config, a, grid, stream)
                  : op == MX_DX ? launch_mx_dx(plan.config, a, grid, stream) : launch_mx_dw(plan.config, a, grid, stream);
     if (e == hipSuccess && a.g.split_k > 1 && a.g.reduce_in_kernel == REDUCE_SEPARATE) {
-        int64_t blocks = (a.g.M * a.g.N + 255) / 256;
+        const int64_t blocks = (a.g.M * a.g.N + 255) / 256;
         e = launch_splitk_reduce<DT_BF16>(a.g, blocks < 8192 ? blocks : 8192, stream);
     }
     return e == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
