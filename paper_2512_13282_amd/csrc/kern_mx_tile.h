@@ -366,6 +366,9 @@ void mx_grad_kernel(MxArgs a) {
         }
     }
     const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + (DW ? k_begin * lda_b + m0 * 2 : m0 * lda_b + k_begin * 2);
+    // Where a wave's loads are all of one group of eight rows and that lies past M, they are left out
+    // (16 x 4096 x 4096: 10.8 -> 10.4 us); the rows' results are not stored, whatever LDS holds.
+    const bool no_a = !DW && WAVES % (BM / 8) == 0 && uniform(uint32_t(m0 + wave % (BM / 8) * 8 >= M)) != 0;
     auto load_a = [&](int kt, int buf) __attribute__((always_inline)) {
         const int rem = k_len - kt * BK;
         const uint32_t dst = lds_addr(a_lds[0]) + uint32_t(buf * A_STAGE) + uint32_t(wave) * 1024u;
@@ -373,7 +376,8 @@ void mx_grad_kernel(MxArgs a) {
                                           uniform(uint32_t((rem <= 0 ? 0 : rem < BK ? rem : BK) * lda_b)))
                               : ring_rsrc(uniform(a_base + int64_t(kt) * (BK * 2)), uniform(rem > 0 ? a_bytes : 0u));
 #pragma unroll
-        for (int i = 0; i < A_INSTR; ++i) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
+        for (int i = 0; i < A_INSTR; ++i)
+            if (!no_a) ring_load16(ra, dst + i * (WAVES * 1024), a_k[i] < rem ? a_voff[i] : kOOB);
     };
 
     // ---- B: this thread's block of row b_row of each stage.

@@ -123,13 +123,12 @@ __device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&ac
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
-        // Small tiles fetch up to four slices at once: one after the other, each waits out a trip
-        // to the coherence point.
-        constexpr int G = TM * TN >= 4 ? 1 : 4 / (TM * TN);
-        const int whole = g.split_k / G * G;
-        auto add = [&](int s, auto n_c) {
-            constexpr int COUNT = decltype(n_c)::value;
-            f32x4_t v[COUNT][TM][TN][4];
+        // Small tiles fetch four slices at once, eight where no more than 16 rows hold results (slots
+        // 0 and 1 of the only fragment row): one after the other, each waits out a trip to
+        // the coherence point.
+        auto add = [&](int s, auto n_c, auto q_c) __attribute__((always_inline)) {
+            constexpr int COUNT = decltype(n_c)::value, Q = decltype(q_c)::value;
+            f32x4_t v[COUNT][TM][TN][Q];
 #pragma unroll
             for (int u = 0; u < COUNT; ++u)
 #pragma unroll
@@ -137,7 +136,7 @@ __device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&ac
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
+                        for (int q = 0; q < Q; ++q)
                             v[u][i][j][q] = mx_load_part(parts, 32 * i + 8 * q < rows ? (s + u) * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16 : kOOB);
 #pragma unroll
             for (int u = 0; u < COUNT; ++u)
@@ -146,12 +145,19 @@ __device__ __forceinline__ void mx_store_tile(const KernelArgs &g, f32x16_t (&ac
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
+                        for (int q = 0; q < Q; ++q)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[u][i][j][q][e];
         };
-        for (int s = 0; s < whole; s += G) add(s, std::integral_constant<int, G>{});
-        for (int s = whole; s < g.split_k; ++s) add(s, std::integral_constant<int, 1>{});
+        constexpr int G = TM * TN >= 4 ? 1 : 4 / (TM * TN);
+        using I1 = std::integral_constant<int, 1>;
+        using I2 = std::integral_constant<int, 2>;
+        using I4 = std::integral_constant<int, 4>;
+        int s = 0;
+        if (TM * TN == 1 && rows <= 16)
+            for (; s + 8 <= g.split_k; s += 8) add(s, std::integral_constant<int, 8>{}, I2{});
+        for (; s + G <= g.split_k; s += G) add(s, std::integral_constant<int, G>{}, I4{});
+        for (; s < g.split_k; ++s) add(s, I1{}, I4{});
         mx_reset_counter(g, tile);
         out.split_k = 1;
     }
