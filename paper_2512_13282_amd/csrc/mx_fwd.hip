@@ -18,8 +18,8 @@ hipError_t launch_mx_fwd(int32_t cfg, const MxArgs &a, int64_t grid, hipStream_t
         case 4: return launch_mx(mx_fwd_kernel<64, 128, 1, 4, 2, 2, 128, 3, 1024>, a, g, 512, 0, s);
         case 5: return launch_mx(mx_fwd_kernel<128, 128, 2, 2, 2, 2, 128, 3, 1024>, a, g, 512, 0, s);
         case 6: return launch_mx(mx_fwd_kernel<128, 128, 2, 2, 1, 2, 64, 3, 1024>, a, g, 256, 0, s);
-        case 7: return launch_mx(mx_fwd_kernel<128, 256, 2, 4, 1, 2, 64, 3, 1024>, a, g, 512, 0, s);
-        case 8: return launch_mx(mx_fwd_kernel<192, 256, 2, 4, 1, 2, 64, 3, 4096>, a, g, 512, 0, s);
+        case 7: return launch_mx(mx_fwd_kernel<128, 256, 2, 4, 1, 2, 128, 3, 2048>, a, g, 512, 0, s);
+        case 8: return launch_mx(mx_fwd_kernel<192, 256, 2, 4, 1, 2, 128, 2, 4096>, a, g, 512, 0, s);
         case 9: return launch_mx(mx_fwd_kernel<256, 256, 2, 4, 1, 2, 64, 3, 4096>, a, g, 512, 0, s);
         default: return hipErrorInvalidValue;
     }

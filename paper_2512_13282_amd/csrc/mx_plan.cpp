@@ -5,35 +5,35 @@ namespace gemm {
 
 // Row 0 is the decode kernel (at most 16 rows of A, and A's K slice in 64 KiB of LDS), the rest
 // are output tiles.  The six figures of a tile are fitted to its own measured times over
-// 336 shapes (rows 1 to 11008, weights of 1024 x 1024 to 14336 x 4096, each in up to eight splits);
-// chosen by them, those shapes take 1.02 of their best measured plan's time on geometric mean.
+// 470 shapes (rows 1 to 11008, weights of 1024 x 1024 to 14336 x 4096, each in up to eight splits);
+// chosen by them, those shapes take 1.01 of their best measured plan's time on geometric mean (the worst 1.19).
 const MxConfig kMxConfigs[] = {
     {MX_FWD, 16, 16, 8, 4, 0, 0, 0, 0, 0, 0, "mx_decode"},
-    {MX_FWD, 32, 64, 8, 2, 2.02, 0.112, 0.342, 0.82, 5.11, 0.77, "mx_fwd_32x64_1x2x4"},
-    {MX_FWD, 32, 128, 8, 1, 2.21, 0.164, 0.176, 0.64, 2.18, 0.18, "mx_fwd_32x128_1x4x2"},
-    {MX_FWD, 64, 64, 8, 1, 3.00, 0.133, 0.149, 0.30, 3.61, 0.24, "mx_fwd_64x64_1x2x4"},
-    {MX_FWD, 64, 128, 8, 1, 2.13, 0.224, 0.247, 0.66, 1.66, 0.31, "mx_fwd_64x128_1x4x2"},
-    {MX_FWD, 128, 128, 8, 1, 2.39, 0.386, 0.406, 0.23, 1.49, 0.43, "mx_fwd_128x128_2x2x2"},
-    {MX_FWD, 128, 128, 4, 2, 1.20, 0.510, 0.746, 1.19, 0.82, 0.40, "mx_fwd_128x128_2x2x1"},
-    {MX_FWD, 128, 256, 8, 1, 0.53, 0.717, 0.734, 0.70, 0.80, 0.48, "mx_fwd_128x256_2x4x1"},
-    {MX_FWD, 192, 256, 8, 1, 0.00, 0.981, 1.052, 0.91, 0.74, 0.27, "mx_fwd_192x256_2x4x1"},
-    {MX_FWD, 256, 256, 8, 1, 0.00, 1.207, 1.149, 0.00, 0.80, 0.48, "mx_fwd_256x256_2x4x1"},
-    {MX_DX, 32, 64, 8, 1, 2.35, 0.224, 0.241, 0.57, 3.96, 0.48, "mx_dx_32x64_1x2x4"},
-    {MX_DX, 32, 64, 4, 3, 1.18, 0.292, 0.580, 1.30, 3.50, 0.75, "mx_dx_32x64_1x2x2"},
-    {MX_DX, 64, 64, 4, 2, 1.22, 0.342, 0.486, 1.25, 3.02, 0.65, "mx_dx_64x64_1x2x2"},
-    {MX_DX, 64, 128, 8, 1, 1.84, 0.446, 0.439, 0.97, 1.73, 0.33, "mx_dx_64x128_1x4x2"},
-    {MX_DX, 64, 256, 8, 1, 1.36, 0.604, 0.587, 1.35, 0.90, 0.30, "mx_dx_64x256_1x8x1"},
-    {MX_DX, 128, 128, 4, 2, 0.37, 0.679, 0.892, 2.32, 0.83, 0.38, "mx_dx_128x128_2x2x1"},
-    {MX_DX, 128, 256, 8, 1, 1.09, 0.809, 0.785, 1.09, 0.73, 0.24, "mx_dx_128x256_2x4x1"},
-    {MX_DX, 256, 256, 8, 1, 0.16, 1.242, 1.221, 0.00, 0.83, 0.28, "mx_dx_256x256_2x4x1"},
-    {MX_DW, 32, 64, 8, 1, 2.31, 0.288, 0.291, 1.00, 3.46, 0.50, "mx_dw_32x64_1x2x4"},
-    {MX_DW, 32, 64, 4, 3, 0.95, 0.376, 0.713, 1.65, 3.28, 0.41, "mx_dw_32x64_1x2x2"},
-    {MX_DW, 64, 64, 4, 2, 1.46, 0.451, 0.596, 1.63, 2.92, 0.29, "mx_dw_64x64_1x2x2"},
-    {MX_DW, 64, 128, 8, 1, 2.65, 0.622, 0.523, 0.80, 2.17, 0.09, "mx_dw_64x128_1x4x2"},
-    {MX_DW, 64, 256, 8, 1, 0.27, 0.982, 0.896, 2.04, 1.30, 0.05, "mx_dw_64x256_1x8x1"},
-    {MX_DW, 128, 128, 4, 2, 1.79, 0.912, 0.975, 1.66, 1.42, 0.05, "mx_dw_128x128_2x2x1"},
-    {MX_DW, 128, 256, 8, 1, 2.86, 1.028, 0.936, 0.40, 1.00, 0.03, "mx_dw_128x256_2x4x1"},
-    {MX_DW, 256, 256, 8, 1, 4.74, 1.372, 1.671, 0.00, 0.70, 0.06, "mx_dw_256x256_2x4x1"},
+    {MX_FWD, 32, 64, 8, 2, 2.17, 0.113, 0.308, 0.97, 4.21, 0.54, "mx_fwd_32x64_1x2x4"},
+    {MX_FWD, 32, 128, 8, 1, 2.36, 0.167, 0.178, 0.83, 1.62, 0.12, "mx_fwd_32x128_1x4x2"},
+    {MX_FWD, 64, 64, 8, 1, 3.01, 0.136, 0.153, 0.34, 3.46, 0.12, "mx_fwd_64x64_1x2x4"},
+    {MX_FWD, 64, 128, 8, 1, 1.89, 0.226, 0.252, 0.74, 1.61, 0.37, "mx_fwd_64x128_1x4x2"},
+    {MX_FWD, 128, 128, 8, 1, 1.93, 0.388, 0.414, 0.55, 1.44, 0.48, "mx_fwd_128x128_2x2x2"},
+    {MX_FWD, 128, 128, 4, 2, 0.57, 0.516, 0.691, 1.44, 0.80, 0.48, "mx_fwd_128x128_2x2x1"},
+    {MX_FWD, 128, 256, 8, 1, 0.09, 0.649, 0.708, 0.54, 0.89, 0.50, "mx_fwd_128x256_2x4x1"},
+    {MX_FWD, 192, 256, 8, 1, 0.00, 0.982, 1.022, 0.00, 0.73, 0.41, "mx_fwd_192x256_2x4x1"},
+    {MX_FWD, 256, 256, 8, 1, 0.00, 1.209, 1.266, 0.00, 0.81, 0.45, "mx_fwd_256x256_2x4x1"},
+    {MX_DX, 32, 64, 8, 1, 2.61, 0.211, 0.232, 0.71, 2.41, 0.48, "mx_dx_32x64_1x2x4"},
+    {MX_DX, 32, 64, 4, 3, 1.55, 0.269, 0.535, 1.24, 2.04, 0.76, "mx_dx_32x64_1x2x2"},
+    {MX_DX, 64, 64, 4, 2, 1.37, 0.332, 0.464, 1.21, 2.91, 0.71, "mx_dx_64x64_1x2x2"},
+    {MX_DX, 64, 128, 8, 1, 1.83, 0.436, 0.436, 0.74, 1.73, 0.44, "mx_dx_64x128_1x4x2"},
+    {MX_DX, 64, 256, 8, 1, 0.77, 0.604, 0.593, 1.38, 0.92, 0.43, "mx_dx_64x256_1x8x1"},
+    {MX_DX, 128, 128, 4, 2, 0.00, 0.678, 0.876, 2.36, 0.85, 0.44, "mx_dx_128x128_2x2x1"},
+    {MX_DX, 128, 256, 8, 1, 0.49, 0.809, 0.802, 1.11, 0.79, 0.36, "mx_dx_128x256_2x4x1"},
+    {MX_DX, 256, 256, 8, 1, 0.00, 1.222, 1.301, 0.00, 0.84, 0.37, "mx_dx_256x256_2x4x1"},
+    {MX_DW, 32, 64, 8, 1, 1.86, 0.263, 0.319, 1.26, 2.14, 0.53, "mx_dw_32x64_1x2x4"},
+    {MX_DW, 32, 64, 4, 3, 0.89, 0.341, 0.635, 1.83, 2.27, 0.22, "mx_dw_32x64_1x2x2"},
+    {MX_DW, 64, 64, 4, 2, 1.20, 0.418, 0.572, 1.24, 2.70, 0.22, "mx_dw_64x64_1x2x2"},
+    {MX_DW, 64, 128, 8, 1, 1.35, 0.580, 0.572, 1.05, 2.00, 0.14, "mx_dw_64x128_1x4x2"},
+    {MX_DW, 64, 256, 8, 1, 0.00, 0.852, 0.911, 2.15, 1.17, 0.05, "mx_dw_64x256_1x8x1"},
+    {MX_DW, 128, 128, 4, 2, 0.00, 0.864, 1.068, 1.32, 1.30, 0.09, "mx_dw_128x128_2x2x1"},
+    {MX_DW, 128, 256, 8, 1, 0.67, 0.997, 0.982, 0.31, 0.98, 0.09, "mx_dw_128x256_2x4x1"},
+    {MX_DW, 256, 256, 8, 1, 2.07, 1.372, 1.688, 0.00, 0.70, 0.10, "mx_dw_256x256_2x4x1"},
 };
 const int32_t kMxNumConfigs = sizeof(kMxConfigs) / sizeof(kMxConfigs[0]);
 
@@ -75,9 +75,8 @@ double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p) {
     const double rounds = double(int64_t(groups / slots)), rest = groups - rounds * slots;
     double t = rounds * (c.occupancy > 1 ? shared : alone);
     if (rest > 0) {
-        const double per_cu = rest / kCUs;
-        t += per_cu <= 1 || c.occupancy == 1 ? alone
-           : alone + (shared - alone) * ((per_cu - 1) / (c.occupancy - 1) < 1 ? (per_cu - 1) / (c.occupancy - 1) : 1.0);
+        const double per_cu = double(ceil_div(int64_t(rest), kCUs));     // on the fullest
+        t += per_cu <= 1 ? alone : alone + (shared - alone) * (per_cu - 1) / (c.occupancy - 1);
     }
     const double tile = double(c.bm) * c.bn;
     t += c.store_us * tiles * tile * (op == MX_DW ? 4 : 2) / 1e6;
