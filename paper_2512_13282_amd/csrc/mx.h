@@ -53,6 +53,7 @@ struct MxConfig {
 };
 extern const MxConfig kMxConfigs[];
 extern const int32_t kMxNumConfigs;
+constexpr int32_t kMxDecode = 0;                 // the row of the decode kernel
 
 // The plan for a product.  config >= 0 and split > 0 say which one to evaluate instead.
 // False where that configuration is not the operator's, or cannot hold the rows.

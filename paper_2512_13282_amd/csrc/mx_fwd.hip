@@ -7,9 +7,9 @@ namespace gemm {
 
 hipError_t launch_mx_fwd(int32_t cfg, const MxArgs &a, int64_t grid, hipStream_t s) {
     const dim3 g{unsigned(grid)};
-    if (cfg == 0) {
+    if (cfg == kMxDecode) {
         const size_t x = size_t(a.g.M) * size_t(a.g.k_chunk * 2 + 16), sums = 8 * 1024 + 16;
-        return launch_mx(mx_decode_kernel<1, 8, 2>, a, dim3(unsigned(a.g.tiles_n), unsigned(a.g.split_k)), 512, x > sums ? x : sums, s);
+        return launch_mx(mx_decode_kernel<8, 2>, a, dim3(unsigned(a.g.tiles_n), unsigned(a.g.split_k)), 512, x > sums ? x : sums, s);
     }
     switch (cfg) {
         case 1: return launch_mx(mx_fwd_kernel<32, 64, 1, 2, 4, 2, 256, 3, 1024>, a, g, 512, 0, s);

@@ -47,7 +47,7 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     MxArgs a = a0;
     const MxConfig &c = kMxConfigs[plan.config];
-    const bool decode = plan.config == 0;
+    const bool decode = plan.config == kMxDecode;
     const int64_t tm = decode ? 1 : (a.g.M + c.bm - 1) / c.bm, tn = (a.g.N + c.bn - 1) / c.bn;
     const int64_t grid = tm * tn * plan.split_k;
     if (grid > 0x7fffffff) return LAUNCH_HIP_ERROR;

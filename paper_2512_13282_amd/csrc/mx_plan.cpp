@@ -45,7 +45,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPlan *out) {
     if (config < 0 || config >= kMxNumConfigs || kMxConfigs[config].op != op) return false;
-    const bool decode = config == 0;
+    const bool decode = config == kMxDecode;
     if (decode) {
         if (M > 16 || K == 0) return false;
         const int64_t most = (65536 / M - 16) / 256 * 128;       // K of a slice that fits LDS
@@ -64,7 +64,7 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
 // Modelled microseconds of a plan, without the launch and what moves in any plan.
 double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p) {
     const MxConfig &c = kMxConfigs[p.config];
-    if (p.config == 0) {
+    if (p.config == kMxDecode) {
         // W at the rate it streams at, A once for every 16 columns at the rate of the L2s.
         const double w = double(N) * double(K) / 2 / 5.0e6, a = double(ceil_div(N, 16)) * double(M) * double(K) * 2 / 8.5e6;
         return 0.7 + w + a + (p.split_k > 1 ? 1.0 : 0.0);
@@ -85,7 +85,11 @@ double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p) {
         const double rows = M < 8 ? 8 : M < c.bm ? double(M) : double(c.bm);
         t += c.sum_us + c.sum_slice_us * p.split_k * tile * 4 / 1e5 + groups * rows * c.bn * 8 / 4.5e6;
     }
-    return t;
+    // No tile is faster than the operands' way out of memory, at the rate they stream at (124 MB for
+    // 1 x 28672 x 8192: 31.7 us, where the decode kernel takes 28.0).
+    const double moved = 2.0 * double(M) * double(K) + double(N) * double(K) * (op == MX_DW ? 1.03 : 0.53) +
+                         double(M) * double(N) * (op == MX_DW ? 4 : 2);
+    return t > moved / 4.4e6 ? t : moved / 4.4e6;
 }
 
 }  // namespace
@@ -106,7 +110,7 @@ bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t
             // Partial sums stay a fraction of the memory, and the grid a 32-bit number.
             const double tiles = double(ceil_div(M, kMxConfigs[c].bm)) * double(ceil_div(N, kMxConfigs[c].bn));
             const double groups = tiles * p.split_k;
-            if (split == 0 && p.split_k > 1 && c > 0 && groups > 4 * kCUs) break;
+            if (split == 0 && p.split_k > 1 && c != kMxDecode && groups > 4 * kCUs) break;
             const double t = modelled_us(op, M, N, K, p);
             if (!found || t < best) {
                 best = t;
