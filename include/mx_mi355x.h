@@ -30,7 +30,10 @@
  * GEMM_ERR_INVALID_VALUE is returned for a negative size, a stride that is too small,
  * a NULL pointer whose operand is non-empty, a bf16 or fp32 pointer that is not
  * aligned to its element size, and an output that overlaps an input or another output;
- * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more.
+ * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more, or with rows of A,
+ * At or the codes longer than 4 MiB (one to sixteen rows of A over W^T take any length).
+ * Operands whose rows do not lie on 16-byte addresses are copied to rows that do, in the
+ * stream's workspace, ahead of a product (A of up to sixteen rows over W^T is not).
  */
 #ifndef MX_MI355X_H
 #define MX_MI355X_H

@@ -115,7 +115,11 @@ int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, i
     a.g.epilogue = bf16_out ? gemm::EPI_BF16 : gemm::EPI_NONE;
     a.scales = scales;
     a.ld_scales = lds;
-    return status(gemm::launch_mx_gemm(a, op, plan, stream));
+    try {
+        return status(gemm::launch_mx_gemm(a, op, plan, stream));
+    } catch (...) {      // the workspace table's own memory
+        return GEMM_ERR_NO_MEMORY;
+    }
 }
 
 }  // namespace

@@ -36,10 +36,17 @@ __global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
 namespace {
 // An operand as the tile kernels need it: rows on 16-byte addresses, no further apart than
 // 32-bit offsets within a tile allow.
+constexpr int64_t kMostStride = int64_t(1) << 22;
 bool loadable(const void *p, int64_t stride) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0 && stride <= (int64_t(1) << 22);
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0 && stride <= kMostStride;
 }
 int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+bool realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
+    const int64_t n = (x.rows * (x.pitch / 16) + y.rows * (y.pitch / 16) + 255) / 256;
+    hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream, x, y);
+    return hipGetLastError() == hipSuccess;
+}
 
 }  // namespace
 
@@ -62,17 +69,21 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const int64_t a_rows = op == MX_DW ? a.g.K : a.g.M, a_used = (op == MX_DW ? a.g.M : a.g.K) * 2;
     const int64_t b_rows = op == MX_FWD ? a.g.N : a.g.K, b_cols = op == MX_FWD ? a.g.K : a.g.N;
     const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2;
+    const int64_t s_used = (b_cols + kMxBlock - 1) / kMxBlock;
     const bool copy_a = !decode && a.g.K > 0 && !loadable(a.g.A, a.g.lda * 2);
     const bool copy_b = !decode && a.g.K > 0 && !loadable(a.g.B, a.g.ldb);
+    // The gradient kernel offsets scale rows in 32 bits too; any alignment will do.
+    const bool copy_s = op != MX_FWD && a.g.K > 0 && a.ld_scales > kMostStride;
     // Partial sums: whole tiles (the decode kernel's: 16 rows), at least the planes that the separate reduction reads.
     const int64_t partial = a.g.split_k > 1 ? a.g.split_k * tm * tn * c.bm * c.bn * 4 : 0;
     const int64_t a_bytes = copy_a ? a_rows * padded(a_used) : 0, b_bytes = copy_b ? b_rows * padded(b_used) : 0;
-    if ((copy_a && padded(a_used) > (int64_t(1) << 22)) || (copy_b && padded(b_used) > (int64_t(1) << 22)))
+    const int64_t s_bytes = copy_s ? b_rows * padded(s_used) : 0;
+    if ((copy_a && padded(a_used) > kMostStride) || (copy_b && padded(b_used) > kMostStride) || (copy_s && padded(s_used) > kMostStride))
         return LAUNCH_UNSUPPORTED;
-    if (partial + a_bytes + b_bytes > 0) {
+    if (partial + a_bytes + b_bytes + s_bytes > 0) {
         void *ws = nullptr;
         uint32_t *counters = nullptr;
-        const size_t bytes = size_t(partial + a_bytes + b_bytes);
+        const size_t bytes = size_t(partial + a_bytes + b_bytes + s_bytes);
         int rc = acquire_workspace(stream_ptr, bytes, a.g.split_k > 1 ? tm * tn : 0, &ws, &counters);
         if (rc == LAUNCH_NO_COUNTERS) {
             a.g.reduce_in_kernel = REDUCE_SEPARATE;     // the same sums in the same order
@@ -82,21 +93,23 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
         a.g.workspace = ws;
         a.g.counters = counters;
         uint8_t *const copies = static_cast<uint8_t *>(ws) + partial;
-        if (copy_a || copy_b) {
-            MxCopy x{}, y{};
-            if (copy_a) {
-                x = MxCopy{static_cast<const uint8_t *>(a.g.A), copies, a.g.lda * 2, a_used, padded(a_used), a_rows};
-                a.g.A = x.dst;
-                a.g.lda = x.pitch / 2;
-            }
-            if (copy_b) {
-                y = MxCopy{static_cast<const uint8_t *>(a.g.B), copies + a_bytes, a.g.ldb, b_used, padded(b_used), b_rows};
-                a.g.B = y.dst;
-                a.g.ldb = y.pitch;
-            }
-            const int64_t n = ((a_bytes + b_bytes) / 16 + 255) / 256;
-            hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream, x, y);
-            if (hipGetLastError() != hipSuccess) return LAUNCH_HIP_ERROR;
+        MxCopy x{}, y{};
+        if (copy_a) {
+            x = MxCopy{static_cast<const uint8_t *>(a.g.A), copies, a.g.lda * 2, a_used, padded(a_used), a_rows};
+            a.g.A = x.dst;
+            a.g.lda = x.pitch / 2;
+        }
+        if (copy_b) {
+            y = MxCopy{static_cast<const uint8_t *>(a.g.B), copies + a_bytes, a.g.ldb, b_used, padded(b_used), b_rows};
+            a.g.B = y.dst;
+            a.g.ldb = y.pitch;
+        }
+        if ((copy_a || copy_b) && !realign(x, y, stream)) return LAUNCH_HIP_ERROR;
+        if (copy_s) {
+            x = MxCopy{a.scales, copies + a_bytes + b_bytes, a.ld_scales, s_used, padded(s_used), b_rows};
+            a.scales = x.dst;
+            a.ld_scales = x.pitch;
+            if (!realign(x, MxCopy{}, stream)) return LAUNCH_HIP_ERROR;
         }
     }
     hipError_t e = op == MX_FWD ? launch_mx_fwd(plan.config, a, grid, stream)

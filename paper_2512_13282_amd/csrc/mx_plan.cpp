@@ -50,7 +50,7 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
         if (M > 16 || K == 0) return false;
         const int64_t most = (65536 / M - 16) / 256 * 128;       // K of a slice that fits LDS
         const int64_t least = ceil_div(K, most);
-        if (least > (1 << 20)) return false;
+        if (least > 4096) return false;
         if (split < least) split = int32_t(least);
     }
     const int64_t unit = decode ? 128 : 256;
@@ -58,7 +58,9 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
     out->config = config;
     out->k_chunk = chunk;
     out->split_k = int32_t(K > 0 ? ceil_div(K, chunk) : 1);
-    return true;
+    // A tile's partial sums are addressed with 32 bits, and slices are a grid dimension.
+    const MxConfig &c = kMxConfigs[config];
+    return out->split_k <= 65535 && int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX;
 }
 
 // Modelled microseconds of a plan, without the launch and what moves in any plan.

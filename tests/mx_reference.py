@@ -10,7 +10,8 @@ BLOCK = 32
 
 
 def widen(bits: np.ndarray) -> np.ndarray:
-    return inputs.f32_from_bf16_bits(bits).astype(np.float64)
+    with np.errstate(invalid="ignore"):     # signalling NaN patterns
+        return inputs.f32_from_bf16_bits(bits).astype(np.float64)
 
 
 def scale_values(e: np.ndarray) -> np.ndarray:

@@ -195,6 +195,21 @@ def test_products_with_strides_and_offsets(op, size, pads, offsets):
 
 
 @pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("M", [3, 40])
+def test_rows_far_apart(op, M):
+    """Strides past 4 MiB, one operand at a time: rows whose offsets within a tile pass 32 bits."""
+    N, K = 70, 48
+    far = (1 << 26) + 5
+    a, codes, scales, cols = operands(op, M, N, K, 77)
+    want, magnitude = ref.product(op, ref.widen(a), ref.values(codes, scales, cols))
+    for which in range(3):
+        pads = [0, 0, 0, 0]
+        pads[which] = far // (2 if which == 0 else 1)
+        C = run_product(op, M, N, K, a, codes, scales, False, pads=tuple(pads))
+        assert np.all(np.abs(C - want) <= ref.bound(K, magnitude, want, False)), which
+
+
+@pytest.mark.parametrize("op", OPS)
 @pytest.mark.parametrize("M,N", [(1, 1), (3, 70), (130, 257)])
 def test_empty_sum_writes_zeros(op, M, N):
     a, codes, scales, _ = operands(op, M, N, 0, 1)
@@ -359,6 +374,41 @@ def test_helpers_take_strided_operands_and_outputs():
     row = mx.MxMatrix(W.codes[7:8], W.scales[7:8], W.cols)
     lim = torch.from_numpy(ref.bound(200, *ref.product("fwd", x.double().cpu().numpy(), numbers(row))[::-1], True)).to(DEV)
     assert torch.all((mx.linear_mx4(x, row).double() - mx.linear_mx4(x, W)[:, 7:8].double()).abs() <= 2 * lim)
+
+
+def test_offsets_past_32_bits():
+    """Matrices of more than 4 GiB: their last rows packed, multiplied and unpacked as a matrix of
+    their own is."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    rows, cols, tail = 66000, 65600, 200
+    assert rows * cols > 1 << 32
+    # 8-bit codes of 66000 tokens; the tail's gradient is the whole one's where all other rows of dY are zero.
+    codes = torch.zeros(rows, cols, dtype=torch.int8, device=DEV)
+    scales = torch.full((rows, cols // 32), 127, dtype=torch.uint8, device=DEV)
+    codes[-tail:] = torch.randint(-127, 128, (tail, cols), generator=gen, device=DEV, dtype=torch.int8)
+    X, own = mx.MxMatrix(codes, scales, cols), mx.MxMatrix(codes[-tail:].clone(), scales[-tail:].clone(), cols)
+    dY = torch.zeros(rows, 16, dtype=torch.bfloat16, device=DEV)
+    dY[-tail:] = torch.randint(-8, 9, (tail, 16), generator=gen, device=DEV)       # sums of integers: exact in any order
+    assert torch.equal(mx.linear_mx8_dw(dY, X), mx.linear_mx8_dw(dY[-tail:].contiguous(), own))
+    part = mx.unpack_mx(X)
+    assert torch.equal(part[-tail:], mx.unpack_mx(own))
+    again = mx.pack_mx8(part)
+    assert torch.equal(mx.unpack_mx(again)[-tail:], part[-tail:])
+    del codes, scales, X, part, again, dY
+    # A 4-bit weight of 131200 x 66048, forward over its rows and backward over its columns.
+    rows, cols = 131200, 66048
+    codes = torch.randint(0, 256, (rows, cols // 2), generator=gen, device=DEV, dtype=torch.uint8)
+    scales = torch.full((rows, cols // 32), 127, dtype=torch.uint8, device=DEV)
+    assert codes.numel() > 1 << 32
+    W, own = mx.MxMatrix(codes, scales, cols), mx.MxMatrix(codes[-tail:].clone(), scales[-tail:].clone(), cols)
+    for M in (1, 20, 70):
+        x = torch.randint(-2, 3, (M, cols), generator=gen, device=DEV).to(torch.bfloat16)
+        assert torch.equal(mx.linear_mx4(x, W, out_dtype=torch.float32)[:, -tail:], mx.linear_mx4(x, own, out_dtype=torch.float32))
+        dy = torch.zeros(M, rows, dtype=torch.bfloat16, device=DEV)
+        dy[:, -tail:] = torch.randint(-2, 3, (M, tail), generator=gen, device=DEV)
+        assert torch.equal(mx.linear_mx4_dx(dy, W, out_dtype=torch.float32),
+                           mx.linear_mx4_dx(dy[:, -tail:].contiguous(), own, out_dtype=torch.float32))
 
 
 def test_helpers_refuse():
