@@ -31,9 +31,9 @@
  * a NULL pointer whose operand is non-empty, a bf16 or fp32 pointer that is not
  * aligned to its element size, and an output that overlaps an input or another output;
  * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more, or with rows of A,
- * At or the codes longer than 4 MiB (one to sixteen rows of A over W^T take any length).
+ * At or the codes longer than 4 MiB (a few rows of A over W^T take any length).
  * Operands whose rows do not lie on 16-byte addresses are copied to rows that do, in the
- * stream's workspace, ahead of a product (A of up to sixteen rows over W^T is not).
+ * stream's workspace, ahead of a product (but for a few rows of A over W^T).
  */
 #ifndef MX_MI355X_H
 #define MX_MI355X_H
@@ -93,7 +93,7 @@ int mx_gemm_bf16_mx8_bf16_at(int64_t M, int64_t N, int64_t K, const uint16_t *At
                              const int8_t *codes, int64_t ldq, const uint8_t *scales, int64_t lds,
                              uint16_t *C, int64_t ldc, void *stream);
 
-/* Pure host: the plan that a product of these sizes would use: the kernel's
+/* Pure host: the plan that a product of these sizes, its operands on aligned rows, would use: the kernel's
  * configuration (-1: nothing to do), its output tile, the number of K slices and the K
  * of each.  GEMM_ERR_INVALID_VALUE: an unknown op, a negative size, a NULL out. */
 typedef struct mx_plan_info {

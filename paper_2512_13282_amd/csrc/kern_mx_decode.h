@@ -38,7 +38,8 @@ __device__ __forceinline__ void mx_store4(const KernelArgs &g, int64_t m, int64_
 
 // ---------------------------------------------------------------------------
 // A workgroup holds 16 rows of W (columns of C), one of S slices of K and all rows of A, at
-// most 16.  Its KW waves take contiguous parts of the slice and add their sums up in LDS.
+// most 16 MT.  Its KW waves take contiguous parts of the slice and add their sums up in LDS.
+// Neither operand has to lie on aligned rows.
 //
 // W goes straight from memory into registers, U chunks of 128 k on the way per wave: lane l
 // loads the 16 bytes (one block of 32 codes) of row l % 16, block l / 16 of the chunk.  One
@@ -46,7 +47,9 @@ __device__ __forceinline__ void mx_store4(const KernelArgs &g, int64_t m, int64_
 // sixteen bytes is the lane's share of the chunk's t-th 16 x 16 x 32 MFMA: lanes of group
 // g = l / 16 hold k = 32 g + 8 t + 0..7, for W and for A.  The MFMAs multiply up to sixteen
 // rows of A at the price of one; the matrix unit is idle otherwise, and the vector unit has
-// the conversions to do.  Output register r of lane l is C[l % 16][4 (l / 16) + r].
+// the conversions to do.  Output register r of lane l is C[l % 16][4 (l / 16) + r].  MT = 3 serves
+// 17 to 48 rows whose operands the tile kernels would have copied first (37 x 2051 x 2049: a launch
+// and 3 us less).
 //
 // A's slice sits in LDS (rows 16 bytes past a multiple of 256, which puts sixteen rows on all
 // banks; past the end of K zeros).  Its first pieces are loaded ahead of W's, so that writing them
@@ -58,7 +61,7 @@ __device__ __forceinline__ void mx_store4(const KernelArgs &g, int64_t m, int64_
 // 32 rows of W to a workgroup 10 and more; four waves with four chunks each 9.4 at 1 x 14336 x 4096,
 // but 8.2 at 1 x 11008 x 4096 and 11.0 against 10.1 at 2 x 14336 x 4096; non-temporal loads of W 9.9.
 // ---------------------------------------------------------------------------
-template <int KW, int U>
+template <int MT, int KW, int U>
 __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
@@ -118,13 +121,22 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
     for (int p = int(threadIdx.x) + 64 * KW; p < total; p += 64 * KW) put(p, fetch(p));
     __syncthreads();
 
-    const uint8_t *const xrow = lds + (l16 < M ? l16 : int(M) - 1) * pitch + 64 * grp + int(c0 - wg0) * 256;
-    f32x4_t acc{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint8_t *xrow[MT];
+    f32x4_t acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        xrow[m] = lds + (16 * m + l16 < M ? 16 * m + l16 : int(M) - 1) * pitch + 64 * grp + int(c0 - wg0) * 256;
+        acc[m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
     auto multiply = [&](int u, int c) __attribute__((always_inline)) {
         const float s = mx4_scale((sc[u] >> (8 * grp)) & 0xffu);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-            acc = mfma16_bf16(mx4_to_bf16(w[u][t], s), *reinterpret_cast<const u32x4_t *>(xrow + c * 256 + 16 * t), acc);
+        for (int t = 0; t < 4; ++t) {
+            const u32x4_t wf = mx4_to_bf16(w[u][t], s);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+                acc[m] = mfma16_bf16(wf, *reinterpret_cast<const u32x4_t *>(xrow[m] + c * 256 + 16 * t), acc[m]);
+        }
     };
     int i = 0;
     for (; i + 2 * U <= n; i += U) {
@@ -168,41 +180,43 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
 
     // Sum over the waves, in LDS (A is done with), in a fixed order.
     __syncthreads();
-    f32x4_t *const part = reinterpret_cast<f32x4_t *>(lds);      // [KW][64]
-    part[wave * 64 + lane] = acc;
+    f32x4_t *const part = reinterpret_cast<f32x4_t *>(lds);      // [KW][MT][64]
+#pragma unroll
+    for (int m = 0; m < MT; ++m) part[(wave * MT + m) * 64 + lane] = acc[m];
     __syncthreads();
     const bool separate = a.g.reduce_in_kernel == REDUCE_SEPARATE;
-    constexpr uint32_t BYTES = 1024;                             // a slice's partial sums
+    constexpr uint32_t BYTES = 1024 * MT;                        // a slice's partial sums
     const __amdgpu_buffer_rsrc_t parts = mx_parts(a.g, int(blockIdx.x), BYTES);
-    const int64_t col = n0 + 4 * grp;
-    const bool holds = wave == 0 && l16 < M && col < N;
+    const int64_t m = 16 * wave + l16, col = n0 + 4 * grp;       // wave w < MT has rows 16 w ..
+    const bool holds = wave < MT && m < M && col < N;
+    const uint32_t at = uint32_t(wave * 64 + lane);
     if (holds) {
-        f32x4_t sum = part[lane];
+        f32x4_t sum = part[at];
 #pragma unroll
-        for (int k = 1; k < KW; ++k) sum += part[k * 64 + lane];
+        for (int k = 1; k < KW; ++k) sum += part[k * MT * 64 + at];
         if (a.g.split_k == 1) {
-            mx_store4(a.g, l16, col, sum);
+            mx_store4(a.g, m, col, sum);
         } else if (separate) {
-            float *const plane = static_cast<float *>(a.g.workspace) + (slice * M + l16) * N + col;
+            float *const plane = static_cast<float *>(a.g.workspace) + (slice * M + m) * N + col;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 if (col + r < N) plane[r] = sum[r];
         } else {
-            mx_store_part(parts, slice * BYTES + lane * 16, sum);
+            mx_store_part(parts, slice * BYTES + at * 16, sum);
         }
     }
     if (a.g.split_k == 1 || separate) return;
-    if (!mx_last_slice(a.g, int(blockIdx.x), *reinterpret_cast<int *>(lds + KW * 1024))) return;
+    if (!mx_last_slice(a.g, int(blockIdx.x), *reinterpret_cast<int *>(lds + KW * MT * 1024))) return;
     if (holds) {
         f32x4_t sum{0.0f, 0.0f, 0.0f, 0.0f};
         for (int q = 0; q < a.g.split_k; q += 8) {       // eight loads on the way; past the last slice zeros
             f32x4_t v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = mx_load_part(parts, (q + u) * BYTES + lane * 16);
+            for (int u = 0; u < 8; ++u) v[u] = mx_load_part(parts, (q + u) * BYTES + at * 16);
 #pragma unroll
             for (int u = 0; u < 8; ++u) sum += v[u];
         }
-        mx_store4(a.g, l16, col, sum);
+        mx_store4(a.g, m, col, sum);
     }
     mx_reset_counter(a.g, int(blockIdx.x));
 }

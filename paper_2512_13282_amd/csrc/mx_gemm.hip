@@ -34,12 +34,6 @@ __global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
 }
 
 namespace {
-// An operand as the tile kernels need it: rows on 16-byte addresses, no further apart than
-// 32-bit offsets within a tile allow.
-constexpr int64_t kMostStride = int64_t(1) << 22;
-bool loadable(const void *p, int64_t stride) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0 && stride <= kMostStride;
-}
 int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
 bool realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
@@ -54,7 +48,7 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     MxArgs a = a0;
     const MxConfig &c = kMxConfigs[plan.config];
-    const bool decode = plan.config == kMxDecode;
+    const bool decode = plan.config == kMxDecode || plan.config == kMxDecode48;
     const int64_t tm = decode ? 1 : (a.g.M + c.bm - 1) / c.bm, tn = (a.g.N + c.bn - 1) / c.bn;
     const int64_t grid = tm * tn * plan.split_k;
     if (grid > 0x7fffffff) return LAUNCH_HIP_ERROR;
@@ -70,15 +64,15 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const int64_t b_rows = op == MX_FWD ? a.g.N : a.g.K, b_cols = op == MX_FWD ? a.g.K : a.g.N;
     const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2;
     const int64_t s_used = (b_cols + kMxBlock - 1) / kMxBlock;
-    const bool copy_a = !decode && a.g.K > 0 && !loadable(a.g.A, a.g.lda * 2);
-    const bool copy_b = !decode && a.g.K > 0 && !loadable(a.g.B, a.g.ldb);
+    const bool copy_a = !decode && a.g.K > 0 && !mx_loadable(a.g.A, a.g.lda * 2);
+    const bool copy_b = !decode && a.g.K > 0 && !mx_loadable(a.g.B, a.g.ldb);
     // The gradient kernel offsets scale rows in 32 bits too; any alignment will do.
-    const bool copy_s = op != MX_FWD && a.g.K > 0 && a.ld_scales > kMostStride;
+    const bool copy_s = op != MX_FWD && a.g.K > 0 && a.ld_scales > kMxMostStride;
     // Partial sums: whole tiles (the decode kernel's: 16 rows), at least the planes that the separate reduction reads.
     const int64_t partial = a.g.split_k > 1 ? a.g.split_k * tm * tn * c.bm * c.bn * 4 : 0;
     const int64_t a_bytes = copy_a ? a_rows * padded(a_used) : 0, b_bytes = copy_b ? b_rows * padded(b_used) : 0;
     const int64_t s_bytes = copy_s ? b_rows * padded(s_used) : 0;
-    if ((copy_a && padded(a_used) > kMostStride) || (copy_b && padded(b_used) > kMostStride) || (copy_s && padded(s_used) > kMostStride))
+    if ((copy_a && padded(a_used) > kMxMostStride) || (copy_b && padded(b_used) > kMxMostStride) || (copy_s && padded(s_used) > kMxMostStride))
         return LAUNCH_UNSUPPORTED;
     if (partial + a_bytes + b_bytes + s_bytes > 0) {
         void *ws = nullptr;

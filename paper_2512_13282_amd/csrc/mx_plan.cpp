@@ -3,12 +3,13 @@
 
 namespace gemm {
 
-// Row 0 is the decode kernel (at most 16 rows of A, and A's K slice in 64 KiB of LDS), the rest
-// are output tiles.  The six figures of a tile are fitted to its own measured times over
+// Rows 0 and 1 are the decode kernel (at most 16 or 48 rows of A, A's K slice in 64 KiB of LDS), the
+// rest are output tiles.  The six figures of a tile are fitted to its own measured times over
 // 470 shapes (rows 1 to 11008, weights of 1024 x 1024 to 14336 x 4096, each in up to eight splits);
 // chosen by them, those shapes take 1.01 of their best measured plan's time on geometric mean (the worst 1.19).
 const MxConfig kMxConfigs[] = {
-    {MX_FWD, 16, 16, 8, 4, 0, 0, 0, 0, 0, 0, "mx_decode"},
+    {MX_FWD, 16, 16, 8, 4, 0, 0, 0, 0, 0, 0, "mx_decode_16"},
+    {MX_FWD, 48, 16, 8, 2, 0, 0, 0, 0, 0, 0, "mx_decode_48"},
     {MX_FWD, 32, 64, 8, 2, 2.17, 0.113, 0.308, 0.97, 4.21, 0.54, "mx_fwd_32x64_1x2x4"},
     {MX_FWD, 32, 128, 8, 1, 2.36, 0.167, 0.178, 0.83, 1.62, 0.12, "mx_fwd_32x128_1x4x2"},
     {MX_FWD, 64, 64, 8, 1, 3.01, 0.136, 0.153, 0.34, 3.46, 0.12, "mx_fwd_64x64_1x2x4"},
@@ -45,9 +46,9 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPlan *out) {
     if (config < 0 || config >= kMxNumConfigs || kMxConfigs[config].op != op) return false;
-    const bool decode = config == kMxDecode;
+    const bool decode = config == kMxDecode || config == kMxDecode48;
     if (decode) {
-        if (M > 16 || K == 0) return false;
+        if (M > kMxConfigs[config].bm || K == 0) return false;
         const int64_t most = (65536 / M - 16) / 256 * 128;       // K of a slice that fits LDS
         const int64_t least = ceil_div(K, most);
         if (least > 4096) return false;
@@ -64,9 +65,9 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
 }
 
 // Modelled microseconds of a plan, without the launch and what moves in any plan.
-double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p) {
+double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p, int64_t copied) {
     const MxConfig &c = kMxConfigs[p.config];
-    if (p.config == kMxDecode) {
+    if (p.config == kMxDecode || p.config == kMxDecode48) {
         // W at the rate it streams at, A once for every 16 columns at the rate of the L2s.
         const double w = double(N) * double(K) / 2 / 5.0e6, a = double(ceil_div(N, 16)) * double(M) * double(K) * 2 / 8.5e6;
         return 0.7 + w + a + (p.split_k > 1 ? 1.0 : 0.0);
@@ -91,12 +92,14 @@ double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p) {
     // 1 x 28672 x 8192: 31.7 us, where the decode kernel takes 28.0).
     const double moved = 2.0 * double(M) * double(K) + double(N) * double(K) * (op == MX_DW ? 1.03 : 0.53) +
                          double(M) * double(N) * (op == MX_DW ? 4 : 2);
-    return t > moved / 4.4e6 ? t : moved / 4.4e6;
+    // Operands copied to aligned rows first: a launch and both ways through memory.
+    const double copy = copied > 0 ? 3.5 + 2.0 * double(copied) / 4.5e6 : 0.0;
+    return (t > moved / 4.4e6 ? t : moved / 4.4e6) + copy;
 }
 
 }  // namespace
 
-bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, MxPlan *out) {
+bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied, int32_t config, int32_t split, MxPlan *out) {
     if (config >= 0) return evaluate(op, M, K, config, split > 0 ? split : 1, out);
     static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
     double best = 0;
@@ -112,8 +115,8 @@ bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t
             // Partial sums stay a fraction of the memory, and the grid a 32-bit number.
             const double tiles = double(ceil_div(M, kMxConfigs[c].bm)) * double(ceil_div(N, kMxConfigs[c].bn));
             const double groups = tiles * p.split_k;
-            if (split == 0 && p.split_k > 1 && c != kMxDecode && groups > 4 * kCUs) break;
-            const double t = modelled_us(op, M, N, K, p);
+            if (split == 0 && p.split_k > 1 && kMxConfigs[c].bn > 16 && groups > 4 * kCUs) break;
+            const double t = modelled_us(op, M, N, K, p, copied);
             if (!found || t < best) {
                 best = t;
                 *out = p;

@@ -262,7 +262,7 @@ def configurations(op):
 
 
 @pytest.mark.parametrize("op", OPS)
-@pytest.mark.parametrize("size", [(1, 33, 640), (5, 257, 1029), (13, 130, 2500), (16, 64, 4400), (77, 390, 1537), (300, 270, 1100)],
+@pytest.mark.parametrize("size", [(1, 33, 640), (5, 257, 1029), (13, 130, 2500), (16, 64, 4400), (17, 100, 1500), (48, 70, 900), (77, 390, 1537), (300, 270, 1100)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_every_configuration_and_split(op, size):
     """Each kernel where it would not be chosen too, with K whole and in slices; captured or not, a
@@ -279,7 +279,7 @@ def test_every_configuration_and_split(op, size):
                 try:
                     plan = mx.mx_plan(OPS.index(op), M, N, K)
                 except b.GemmError as e:
-                    assert e.status == b.GEMM_ERR_UNSUPPORTED and M > 16
+                    assert e.status == b.GEMM_ERR_UNSUPPORTED and config < 2 and M > (16, 48)[config]
                     continue
                 assert plan["config"] == config and plan["split_k"] >= min(split, 2 if K > 256 else 1)
                 C = run_product(op, M, N, K, a, codes, scales, False, pads=(0, 0, 0, 1))
