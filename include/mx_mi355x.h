@@ -2,8 +2,9 @@
  * mx_mi355x.h -- C ABI of the MI355X (gfx950) products over block-scaled operands:
  * linear layers whose weight is held in 4 bits, activation checkpoints in 8 bits.
  *
- * Formats (the OCP Microscaling formats MXFP4 and MXINT8).  A packed matrix of
- * `rows` x `cols` elements has two parts:
+ * Formats (the OCP Microscaling formats MXFP4 and MXINT8; the latter's specification
+ * takes a code for a multiple of 2^-6, here it is a whole number, so the same matrix has
+ * scale bytes 6 smaller here).  A packed matrix of `rows` x `cols` elements has two parts:
  *
  *   scales  one byte e for every block of 32 consecutive elements of a row (the
  *           row's last block may be shorter), the power of two 2^(e - 127); e = 255

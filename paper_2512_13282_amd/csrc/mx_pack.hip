@@ -4,8 +4,12 @@
 // of 32: bf16 is read and written 16 bytes per thread, codes 4 or 8 bytes, all contiguous
 // across the wave.  The largest magnitude of a block is the largest of its bit patterns
 // without their signs (infinities and NaN above every finite one), so its power of two is
-// that pattern's exponent field and no logarithm is taken.  Bound by memory: four to six
-// bytes move per element and both conversions are a handful of instructions for it.
+// that pattern's exponent field and no logarithm is taken.
+//
+// Bound by memory: 2.5 to 3 bytes move per element and both conversions are a handful of
+// instructions for it.  14336 x 4096 to 4 bits and back: 30.9 and 23.5 us (4.8 and 6.3 TB/s; a
+// large copy moves 4.8, and the second finds part of the codes in the cache); 2048 x 11008 to 8
+// bits and back: 14.4 and 13.1 us.
 #include "mx_common.h"
 
 namespace gemm {
