@@ -318,12 +318,12 @@ void mx_fwd_kernel(MxArgs a) {
 //
 // B's codes are loaded two stages ahead into registers, A one stage ahead into LDS.
 //
-// Measured: DX 2048 x 4096 x 11008 158 us (1170 TFLOP/s, the matrix unit busy 52 % of the clocks),
-// 96 x 4096 x 4096 17.6 us (the load path: 288 KB per CU; the sum of four slices); DW 11008 x 4096 x
-// 2048 182 us (1010 TFLOP/s, 46 % busy; 2.69 rounds of tiles, 6.4 us of stores of C in each), 16 x
-// 4096 x 2048 9.4 us.  Against it: A in a ring of three stages made no difference (64.3 and 64.8 us at
-// 2048 x 4096 x 4096); the loads in two halves 114 against 106 us (DX 2048 x 8192 x 4096); a small
-// tile's fragments read a whole stage ahead 17.9 against 17.7 (DX 96 x 4096 x 4096); X unpacked to
+// Few rows are mx_rows_kernel's.
+//
+// Measured: DX 2048 x 4096 x 11008 158 us (1170 TFLOP/s, the matrix unit busy 52 % of the clocks); DW
+// 11008 x 4096 x 2048 182 us (1010 TFLOP/s, 46 % busy; 2.69 rounds of tiles, 6.4 us of stores of C in
+// each).  Against it: A in a ring of three stages made no difference (64.3 and 64.8 us at
+// 2048 x 4096 x 4096); the loads in two halves 114 against 106 us (DX 2048 x 8192 x 4096); X unpacked to
 // bf16 by a launch of its own 180 against 183.5 us (DW 11008 x 4096 x 2048) but 74 against 69 (4096 x
 // 4096 x 2048).
 // ---------------------------------------------------------------------------
@@ -381,8 +381,8 @@ void mx_grad_kernel(MxArgs a) {
         }
     }
     const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + (DW ? k_begin * lda_b + m0 * 2 : m0 * lda_b + k_begin * 2);
-    // Where a wave's loads are all of one group of eight rows and that lies past M, they are left out
-    // (16 x 4096 x 4096: 10.8 -> 10.4 us); the rows' results are not stored, whatever LDS holds.
+    // Where a wave's loads are all of one group of eight rows and that lies past M, they are left out;
+    // the rows' results are not stored, whatever LDS holds.
     const bool no_a = !DW && WAVES % (BM / 8) == 0 && uniform(uint32_t(m0 + wave % (BM / 8) * 8 >= M)) != 0;
     auto load_a = [&](int kt, int buf) __attribute__((always_inline)) {
         const int rem = k_len - kt * BK;

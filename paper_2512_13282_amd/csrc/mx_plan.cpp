@@ -4,8 +4,9 @@
 namespace gemm {
 
 // Rows 0 and 1 are the decode kernel (at most 16 or 48 rows of A, A's K slice in 64 KiB of LDS), the
-// rest are output tiles.  The six figures of a tile are fitted to its own measured times over
-// 470 shapes (rows 1 to 11008, weights of 1024 x 1024 to 14336 x 4096, each in up to eight splits);
+// rest are output tiles: mx_rows_kernel's where no waves are named, else mx_fwd_kernel's and
+// mx_grad_kernel's.  The six figures of a tile are fitted to its own measured times over
+// 550 shapes (rows 1 to 11008, weights of 1024 x 1024 to 14336 x 4096, each in up to eight splits);
 // chosen by them, those shapes take 1.01 of their best measured plan's time on geometric mean (the worst 1.19).
 const MxConfig kMxConfigs[] = {
     {MX_FWD, 16, 16, 8, 4, 0, 0, 0, 0, 0, 0, "mx_decode_16"},
@@ -19,22 +20,20 @@ const MxConfig kMxConfigs[] = {
     {MX_FWD, 128, 256, 8, 1, 0.09, 0.649, 0.708, 0.54, 0.89, 0.50, "mx_fwd_128x256_2x4x1"},
     {MX_FWD, 192, 256, 8, 1, 0.00, 0.982, 1.022, 0.00, 0.73, 0.41, "mx_fwd_192x256_2x4x1"},
     {MX_FWD, 256, 256, 8, 1, 0.00, 1.209, 1.266, 0.00, 0.81, 0.45, "mx_fwd_256x256_2x4x1"},
-    {MX_DX, 32, 64, 8, 1, 2.61, 0.211, 0.232, 0.71, 2.41, 0.48, "mx_dx_32x64_1x2x4"},
-    {MX_DX, 32, 64, 4, 3, 1.55, 0.269, 0.535, 1.24, 2.04, 0.76, "mx_dx_32x64_1x2x2"},
-    {MX_DX, 64, 64, 4, 2, 1.37, 0.332, 0.464, 1.21, 2.91, 0.71, "mx_dx_64x64_1x2x2"},
-    {MX_DX, 64, 128, 8, 1, 1.83, 0.436, 0.436, 0.74, 1.73, 0.44, "mx_dx_64x128_1x4x2"},
-    {MX_DX, 64, 256, 8, 1, 0.77, 0.604, 0.593, 1.38, 0.92, 0.43, "mx_dx_64x256_1x8x1"},
-    {MX_DX, 128, 128, 4, 2, 0.00, 0.678, 0.876, 2.36, 0.85, 0.44, "mx_dx_128x128_2x2x1"},
-    {MX_DX, 128, 256, 8, 1, 0.49, 0.809, 0.802, 1.11, 0.79, 0.36, "mx_dx_128x256_2x4x1"},
-    {MX_DX, 256, 256, 8, 1, 0.00, 1.222, 1.301, 0.00, 0.84, 0.37, "mx_dx_256x256_2x4x1"},
-    {MX_DW, 32, 64, 8, 1, 1.86, 0.263, 0.319, 1.26, 2.14, 0.53, "mx_dw_32x64_1x2x4"},
-    {MX_DW, 32, 64, 4, 3, 0.89, 0.341, 0.635, 1.83, 2.27, 0.22, "mx_dw_32x64_1x2x2"},
-    {MX_DW, 64, 64, 4, 2, 1.20, 0.418, 0.572, 1.24, 2.70, 0.22, "mx_dw_64x64_1x2x2"},
-    {MX_DW, 64, 128, 8, 1, 1.35, 0.580, 0.572, 1.05, 2.00, 0.14, "mx_dw_64x128_1x4x2"},
-    {MX_DW, 64, 256, 8, 1, 0.00, 0.852, 0.911, 2.15, 1.17, 0.05, "mx_dw_64x256_1x8x1"},
-    {MX_DW, 128, 128, 4, 2, 0.00, 0.864, 1.068, 1.32, 1.30, 0.09, "mx_dw_128x128_2x2x1"},
-    {MX_DW, 128, 256, 8, 1, 0.67, 0.997, 0.982, 0.31, 0.98, 0.09, "mx_dw_128x256_2x4x1"},
-    {MX_DW, 256, 256, 8, 1, 2.07, 1.372, 1.688, 0.00, 0.70, 0.10, "mx_dw_256x256_2x4x1"},
+    {MX_DX, 16, 128, 8, 2, 0.24, 0.186, 0.321, 1.45, 2.55, 0.89, "mx_dx_16x128"},
+    {MX_DX, 32, 128, 8, 1, 1.63, 0.208, 0.219, 0.32, 1.36, 0.69, "mx_dx_32x128"},
+    {MX_DX, 48, 128, 8, 1, 2.31, 0.260, 0.253, 0.26, 1.14, 0.51, "mx_dx_48x128"},
+    {MX_DX, 64, 128, 8, 1, 1.78, 0.442, 0.441, 0.79, 1.70, 0.41, "mx_dx_64x128_1x4x2"},
+    {MX_DX, 64, 256, 8, 1, 0.18, 0.614, 0.598, 1.34, 0.99, 0.49, "mx_dx_64x256_1x8x1"},
+    {MX_DX, 128, 128, 4, 2, 0.00, 0.677, 0.892, 1.69, 0.83, 0.43, "mx_dx_128x128_2x2x1"},
+    {MX_DX, 128, 256, 8, 1, 0.00, 0.815, 0.808, 0.27, 0.85, 0.39, "mx_dx_128x256_2x4x1"},
+    {MX_DX, 256, 256, 8, 1, 0.00, 1.222, 1.297, 0.00, 0.79, 0.37, "mx_dx_256x256_2x4x1"},
+    {MX_DW, 32, 128, 8, 2, 1.12, 0.272, 0.483, 1.46, 0.97, 0.17, "mx_dw_32x128"},
+    {MX_DW, 32, 64, 4, 3, 0.83, 0.344, 0.647, 1.97, 1.96, 0.21, "mx_dw_32x64_1x2x2"},
+    {MX_DW, 64, 256, 8, 1, 0.00, 0.834, 0.908, 2.62, 1.06, 0.05, "mx_dw_64x256_1x8x1"},
+    {MX_DW, 128, 128, 4, 2, 0.00, 0.861, 1.075, 1.79, 1.20, 0.09, "mx_dw_128x128_2x2x1"},
+    {MX_DW, 128, 256, 8, 1, 0.56, 0.992, 0.974, 0.68, 0.95, 0.10, "mx_dw_128x256_2x4x1"},
+    {MX_DW, 256, 256, 8, 1, 2.13, 1.372, 1.668, 0.00, 0.60, 0.10, "mx_dw_256x256_2x4x1"},
 };
 const int32_t kMxNumConfigs = sizeof(kMxConfigs) / sizeof(kMxConfigs[0]);
 
