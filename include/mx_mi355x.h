@@ -34,7 +34,8 @@
  * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more, or with rows of A,
  * At or the codes longer than 4 MiB (a few rows of A over W^T take any length).
  * Operands whose rows do not lie on 16-byte addresses are copied to rows that do, in the
- * stream's workspace, ahead of a product (but for a few rows of A over W^T).
+ * stream's workspace, ahead of a product (but for a few rows of A over W^T, and A and At
+ * where the results have few rows).
  */
 #ifndef MX_MI355X_H
 #define MX_MI355X_H

@@ -26,15 +26,19 @@ namespace gemm {
 // Bound by latencies one after the other: launch, first loads, the sum in LDS, and where K is
 // split the slices' sum (2.5 + 1 + 1 + 4 us of the smaller ones), the load path between them.  DX, against
 // the best of mx_grad_kernel: 1 x 4096 x 4096 7.3 us (10.1), 16 x 4096 x 4096 8.0 (10.3), 16 x 14336 x
-// 4096 12.9 (17.4), 96 x 4096 x 4096 13.2 (17.6), 256 x 4096 x 4096 18.9 (24.2).  DW: 16 x 4096 x 2048
-// 8.2 (9.4), 4096 x 16 x 2048 10.2 (10.8), 64 x 4096 x 2048 9.5 (11.5), 16 x 14336 x 4096 16.5 (22.2).
+// 4096 12.6 (17.4), 96 x 4096 x 4096 13.2 (17.6), 256 x 4096 x 4096 18.5 (24.2).  DW: 16 x 4096 x 2048
+// 8.3 (9.4), 4096 x 16 x 2048 10.7 (10.8), 64 x 4096 x 2048 9.6 (11.5), 16 x 14336 x 4096 15.8 (22.2).
+// Pieces of 64 bytes leave half of each 128-byte line that the load path moves unused; W through
+// LDS in 16-byte pieces, in the same rows, took 8 to 10 per cent longer.
 //
 // U and the waves per SIMD by registers: 16 rows and DW leave room for two workgroups per compute unit
 // (against U = 3 in one, 16 x 14336 x 4096: 13.3; DW 64 x 4096 x 2048 10.1 with U = 2), 32 and 48 rows
 // would spill.  64 rows (16 MT) were never the best.
 // ---------------------------------------------------------------------------
 template <int OP, int MT, int KW, int U, int WAVES_PER_EU>
-__global__ __attribute__((amdgpu_flat_work_group_size(64 * KW, 64 * KW), amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU))) void mx_rows_kernel(MxArgs a) {
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * KW, 64 * KW),
+                          amdgpu_waves_per_eu(WAVES_PER_EU, WAVES_PER_EU)))
+void mx_rows_kernel(MxArgs a) {
     constexpr bool DW = OP == MX_DW;
     constexpr int CODES = DW ? 2 : 1;                        // dwords of a lane's eight codes
     static_assert(KW == 8, "the sum's 512 threads hold four results of each 16 x 128 part");
@@ -53,58 +57,90 @@ __global__ __attribute__((amdgpu_flat_work_group_size(64 * KW, 64 * KW), amdgpu_
     const int64_t k_end = k_begin + a.g.k_chunk < K ? k_begin + a.g.k_chunk : K;
     const int steps = int((k_end - k_begin + 31) / 32), per = (steps + KW - 1) / KW;
     const int64_t k0 = k_begin + int64_t(wave) * per * 32;
-    const int n = steps - wave * per < per ? steps - wave * per : per;      // <= 0 for a wave without any
+    const int mine = steps - wave * per < per ? steps - wave * per : per;   // <= 0 for a wave without any
+    const bool cut = (k_end - k_begin) % 32 != 0 && mine > 0 && wave * per + mine == steps;
+    const int n = cut ? mine - 1 : mine;                     // whole steps; where K ends in a step, that comes last
 
-    // Offsets within a step; lanes past N and rows past M load nothing, and so do rows past K
-    // (their codes and scales: zeros).
+    // Offsets within a step.  Lanes past N load nothing, and of the step that K ends in neither do rows
+    // past it (their codes and scales: zeros).  A may lie at any address, so every load of it stays
+    // inside its rows: rows of C past M take the last one's, and are not stored.
     const bool in = n0 + 8 * l16 < N;
-    uint32_t w_off[8], s_off[2], a_off[DW ? 8 : MT];
+    uint32_t w_off[DW ? 1 : 8], s_off[2], a_off[DW ? 1 : MT];
+    // DW, short of registers, moves the base from row to row instead.
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w_off[i] = in ? uint32_t((8 * grp + i) * ldq + 4 * CODES * l16) : kOOB;
+    for (int i = 0; i < (DW ? 1 : 8); ++i) w_off[i] = in ? uint32_t((8 * grp + i) * ldq + 4 * CODES * l16) : kOOB;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) s_off[i] = n0 + 8 * (l16 & 12) < N ? uint32_t((8 * grp + 2 * (lane & 3) + i) * lds_ + l16 / 4) : kOOB;   // the quad's block
+    for (int i = 0; i < 2; ++i)                              // of the quad's block
+        s_off[i] = n0 + 8 * (l16 & 12) < N ? uint32_t((8 * grp + 2 * (lane & 3) + i) * lds_ + l16 / 4) : kOOB;
+    const int64_t a_last = M >= 2 ? M - 2 : 0, a_col = m0 < a_last ? m0 : a_last;      // DW: the last dword of A's rows
     if constexpr (DW) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a_off[i] = m0 + 2 * l16 < M ? uint32_t((8 * grp + i) * lda_b + 4 * l16) : kOOB;
+        a_off[0] = uint32_t(8 * grp * lda_b + 2 * ((m0 + 2 * l16 < a_last ? m0 + 2 * l16 : a_last) - a_col));
     } else {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) a_off[m] = m0 + 16 * m + l16 < M ? uint32_t((16 * m + l16) * lda_b + 16 * grp) : kOOB;
+        for (int m = 0; m < MT; ++m) a_off[m] = uint32_t((m0 + 16 * m + l16 < M ? 16 * m + l16 : M - 1 - m0) * lda_b + 16 * grp);
     }
     const uint8_t *const w_base = static_cast<const uint8_t *>(a.g.B) + k0 * ldq + (DW ? n0 : n0 / 2);
     const uint8_t *const s_base = a.scales + k0 * lds_ + n0 / kMxBlock;
-    const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + (DW ? k0 * lda_b + m0 * 2 : m0 * lda_b + k0 * 2);
+    const uint8_t *const a_base = static_cast<const uint8_t *>(a.g.A) + (DW ? k0 * lda_b + a_col * 2 : m0 * lda_b + k0 * 2);
 
     uint32_t w[U][8][CODES], sc[U][2];
     uint32_t af[U][DW ? 8 : 4 * MT];                         // DX: fragments; DW: dwords of eight rows
-    auto load = [&](int u, int c) __attribute__((always_inline)) {
-        const int64_t left = k_end - (k0 + 32 * int64_t(c));
-        const int64_t rows = left < 32 ? left : 32;
+    auto load_b = [&](int u, int c, int rows) __attribute__((always_inline)) {
         // A row of the step ends before the next begins: rows past the step's are out of range.
-        const __amdgpu_buffer_rsrc_t rw = make_rsrc(w_base + int64_t(c) * 32 * ldq, uint32_t(rows * ldq));
         const __amdgpu_buffer_rsrc_t rs = make_rsrc(s_base + int64_t(c) * 32 * lds_, uint32_t(rows * lds_));
-        const __amdgpu_buffer_rsrc_t ra = DW ? make_rsrc(a_base + int64_t(c) * 32 * lda_b, uint32_t(rows * lda_b))
-                                             : make_rsrc(a_base + int64_t(c) * 64, kOOB);
 #pragma unroll
         for (int i = 0; i < 2; ++i) sc[u][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, int(s_off[i]), 0, 0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if constexpr (DW) {
-                const u32x2_t x = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rw, int(w_off[i]), 0, 0));
+                const __amdgpu_buffer_rsrc_t rw = make_rsrc(w_base + (int64_t(c) * 32 + i) * ldq, uint32_t(rows > i ? (rows - i) * ldq : 0));
+                const u32x2_t x = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rw, int(w_off[0]), 0, 0));
                 w[u][i][0] = x[0];
                 w[u][i][1] = x[1];
             } else {
+                const __amdgpu_buffer_rsrc_t rw = make_rsrc(w_base + int64_t(c) * 32 * ldq, uint32_t(rows * ldq));
                 w[u][i][0] = __builtin_amdgcn_raw_buffer_load_b32(rw, int(w_off[i]), 0, 0);
             }
         }
+    };
+    auto load = [&](int u, int c) __attribute__((always_inline)) {
+        load_b(u, c, 32);
+        const uint8_t *const p = a_base + int64_t(c) * (DW ? 32 * lda_b : 64);
         if constexpr (DW) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) af[u][i] = __builtin_amdgcn_raw_buffer_load_b32(ra, int(a_off[i]), 0, 0);
+            for (int i = 0; i < 8; ++i) af[u][i] = *reinterpret_cast<const u32_any_mx *>(p + i * lda_b + a_off[0]);
         } else {
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const u32x4_t x = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ra, int(8 * grp < left ? a_off[m] : kOOB), 0, 0));
+                const u32x4_t x = *reinterpret_cast<const u32x4_any_mx *>(p + a_off[m]);
 #pragma unroll
                 for (int d = 0; d < 4; ++d) af[u][4 * m + d] = x[d];
+            }
+        }
+    };
+    // The step that K ends in, after `rows` of its 32: zeros past them.
+    auto load_cut = [&](int c, int rows) __attribute__((always_inline)) {
+        load_b(0, c, rows);
+        const uint8_t *const p = a_base + int64_t(c) * (DW ? 32 * lda_b : 64);
+        if constexpr (DW) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int past = 8 * grp + i - (rows - 1);
+                const uint32_t x = *reinterpret_cast<const u32_any_mx *>(p + int64_t(a_off[0]) + (i - (past > 0 ? past : 0)) * lda_b);
+                af[0][i] = past > 0 ? 0u : x;
+            }
+        } else {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                uint32_t x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int k = 8 * grp + e < rows ? e : rows - 1 - 8 * grp;      // may be before this lane's
+                    x[e] = *reinterpret_cast<const uint16_t *>(p + int64_t(a_off[m]) + 2 * k);
+                }
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    af[0][4 * m + d] = (8 * grp + 2 * d < rows ? x[2 * d] : 0u) | (8 * grp + 2 * d + 1 < rows ? x[2 * d + 1] << 16 : 0u);
             }
         }
     };
@@ -113,23 +149,22 @@ __global__ __attribute__((amdgpu_flat_work_group_size(64 * KW, 64 * KW), amdgpu_
         const uint32_t sel = half ? 0x07060302u : 0x05040100u;
         return u32x4_t{perm(v[1], v[0], sel), perm(v[3], v[2], sel), perm(v[5], v[4], sel), perm(v[7], v[6], sel)};
     };
+    // The halves of A's dwords (DW) that hold rows 2 i and 2 i + 1 of C: the row at the end of an odd M lies
+    // in the upper one, for its dword ends with it.
+    const uint32_t a_sel[2] = {DW && m0 + 2 * l16 == a_last + 1 ? 0x07060302u : 0x05040100u, 0x07060302u};
     f32x4_t acc[MT][8];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[m][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    auto multiply = [&](int u, int c) __attribute__((always_inline)) {
+    auto multiply = [&](int u) __attribute__((always_inline)) {
         u32x4_t fa[MT];
         if constexpr (DW) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) fa[m] = pairs(af[u], m);
+            for (int m = 0; m < MT; ++m)
+                fa[m] = u32x4_t{perm(af[u][1], af[u][0], a_sel[m]), perm(af[u][3], af[u][2], a_sel[m]),
+                                perm(af[u][5], af[u][4], a_sel[m]), perm(af[u][7], af[u][6], a_sel[m])};
         } else {
-            const int64_t left = k_end - (k0 + 32 * int64_t(c)) - 8 * grp;
-            if (k_end - (k0 + 32 * int64_t(c)) < 32) {        // what follows K in A's rows is not part of the sum
-#pragma unroll
-                for (int d = 0; d < 4 * MT; ++d)
-                    af[u][d] = 2 * (d % 4) + 1 < left ? af[u][d] : 2 * (d % 4) < left ? af[u][d] & 0xffffu : 0u;
-            }
 #pragma unroll
             for (int m = 0; m < MT; ++m) fa[m] = u32x4_t{af[u][4 * m], af[u][4 * m + 1], af[u][4 * m + 2], af[u][4 * m + 3]};
         }
@@ -179,18 +214,22 @@ __global__ __attribute__((amdgpu_flat_work_group_size(64 * KW, 64 * KW), amdgpu_
     for (; i + 2 * U <= n; i += U) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            multiply(u, i + u);
+            multiply(u);
             load(u, i + U + u);
         }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (i + u < n) multiply(u, i + u);
+        if (i + u < n) multiply(u);
         if (i + U + u < n) load(u, i + U + u);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (i + U + u < n) multiply(u, i + U + u);
+        if (i + U + u < n) multiply(u);
+    if (cut) {
+        load_cut(n, int(k_end - (k0 + 32 * int64_t(n))));
+        multiply(0);
+    }
 
     // Sum over the waves, 16 rows at a time, in a fixed order.  Piece v = 2 r + h of lane l holds columns
     // 32 g + 8 r + 4 h + 0..3; thread t then has columns 4 (t % 32) .. of row t / 32.  The pieces of

@@ -54,6 +54,8 @@ struct MxConfig {
 extern const MxConfig kMxConfigs[];
 extern const int32_t kMxNumConfigs;
 constexpr int32_t kMxDecode = 0, kMxDecode48 = 1;     // the decode kernel's rows
+// Whether a configuration reads an A that is not loadable (below) where it lies; else it is copied first.
+bool mx_direct_a(int32_t config, int64_t M, int64_t N, int64_t K);
 
 // Whether the tile kernels take an operand as it lies (its first row at p, rows `stride` bytes
 // apart) or have it copied first: they load 16 aligned bytes at a time straight into LDS, at
@@ -63,9 +65,10 @@ inline bool mx_loadable(const void *p, int64_t stride) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0 && stride <= kMxMostStride;
 }
 
-// The plan for a product, where `copied` bytes of its operands are not loadable.  config >= 0 and split > 0 say which one to evaluate instead.
+// The plan for a product, where `copied_a` and `copied_b` bytes of its operands are not loadable.
+// config >= 0 and split > 0 say which one to evaluate instead.
 // False where that configuration is not the operator's, or cannot hold the rows.
-bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied, int32_t config, int32_t split, MxPlan *out);
+bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, int32_t config, int32_t split, MxPlan *out);
 
 // Each queues its kernels on `stream` (a hipStream_t) and returns a LAUNCH_* value.
 int launch_mx_pack(const MxMatrixArgs &a, int bits, void *stream);

@@ -68,23 +68,23 @@ Forced g_forced[3];
 
 // The plans of this thread's latest shapes: choosing one evaluates a hundred or so.
 struct CachedPlan {
-    int64_t M, N, K, copied;   // M = 0: empty
+    int64_t M, N, K, copied_a, copied_b;   // M = 0: empty
     int32_t op;
     gemm::MxPlan plan;
 };
 thread_local CachedPlan t_plans[64];
 
-int plan_for(gemm::MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied, gemm::MxPlan *plan) {
+int plan_for(gemm::MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, gemm::MxPlan *plan) {
     if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX - 4096) return GEMM_ERR_UNSUPPORTED;    // 32-bit indices
     const int32_t config = g_forced[op].config, split = g_forced[op].split;
     if (config >= 0 || split > 0)
-        return gemm::mx_select(op, M, N, K, copied, config, split, plan) ? GEMM_OK : GEMM_ERR_UNSUPPORTED;
+        return gemm::mx_select(op, M, N, K, copied_a, copied_b, config, split, plan) ? GEMM_OK : GEMM_ERR_UNSUPPORTED;
     const uint64_t h = (uint64_t(M) * 0x9E3779B97F4A7C15u ^ uint64_t(N) * 0xC2B2AE3D27D4EB4Fu ^ uint64_t(K) * 0x165667B19E3779F9u) + uint64_t(op);
     CachedPlan &c = t_plans[(h ^ (h >> 32)) % 64];
-    if (c.M != M || c.N != N || c.K != K || c.copied != copied || c.op != op) {
+    if (c.M != M || c.N != N || c.K != K || c.copied_a != copied_a || c.copied_b != copied_b || c.op != op) {
         gemm::MxPlan p;
-        if (!gemm::mx_select(op, M, N, K, copied, -1, 0, &p)) return GEMM_ERR_UNSUPPORTED;
-        c = CachedPlan{M, N, K, copied, op, p};
+        if (!gemm::mx_select(op, M, N, K, copied_a, copied_b, -1, 0, &p)) return GEMM_ERR_UNSUPPORTED;
+        c = CachedPlan{M, N, K, copied_a, copied_b, op, p};
     }
     *plan = c.plan;
     return GEMM_OK;
@@ -104,9 +104,9 @@ int product(gemm::MxOp op, int64_t M, int64_t N, int64_t K, const uint16_t *A, i
     if (M == 0 || N == 0) return GEMM_OK;
     gemm::MxPlan plan;
     // What a tile kernel would have copied first.
-    const int64_t copied = K == 0 ? 0 : (gemm::mx_loadable(A, ra.stride) ? 0 : ra.rows * ra.used) +
-                                        (gemm::mx_loadable(codes, ldq) ? 0 : rq.rows * rq.used);
-    const int planned = plan_for(op, M, N, K, copied, &plan);
+    const int64_t copied_a = K == 0 || gemm::mx_loadable(A, ra.stride) ? 0 : ra.rows * ra.used;
+    const int64_t copied_b = K == 0 || gemm::mx_loadable(codes, ldq) ? 0 : rq.rows * rq.used;
+    const int planned = plan_for(op, M, N, K, copied_a, copied_b, &plan);
     if (planned != GEMM_OK) return planned;
     gemm::MxArgs a{};
     a.g.dtype = 1;      // bf16 operands on the MFMAs
@@ -186,7 +186,7 @@ int mx_plan(int op, int64_t M, int64_t N, int64_t K, mx_plan_info *out) {
     out->config = -1;
     if (M == 0 || N == 0) return GEMM_OK;
     gemm::MxPlan plan;
-    const int rc = plan_for(gemm::MxOp(op), M, N, K, 0, &plan);
+    const int rc = plan_for(gemm::MxOp(op), M, N, K, 0, 0, &plan);
     if (rc != GEMM_OK) return rc;
     const gemm::MxConfig &c = gemm::kMxConfigs[plan.config];
     out->config = plan.config;

@@ -64,7 +64,8 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const int64_t b_rows = op == MX_FWD ? a.g.N : a.g.K, b_cols = op == MX_FWD ? a.g.K : a.g.N;
     const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2;
     const int64_t s_used = (b_cols + kMxBlock - 1) / kMxBlock;
-    const bool copy_a = !decode && a.g.K > 0 && !mx_loadable(a.g.A, a.g.lda * 2);
+    const bool any_a = decode || (a.g.lda * 2 <= kMxMostStride && mx_direct_a(plan.config, a.g.M, a.g.N, a.g.K));
+    const bool copy_a = !any_a && a.g.K > 0 && !mx_loadable(a.g.A, a.g.lda * 2);
     const bool copy_b = !decode && a.g.K > 0 && !mx_loadable(a.g.B, a.g.ldb);
     // The gradient kernel offsets scale rows in 32 bits too; any alignment will do.
     const bool copy_s = op != MX_FWD && a.g.K > 0 && a.ld_scales > kMxMostStride;

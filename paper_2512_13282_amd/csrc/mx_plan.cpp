@@ -63,8 +63,21 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
     return out->split_k <= 65535 && int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX;
 }
 
+// Operands copied to aligned rows first: a launch and both ways through memory.
+double copy_us(int64_t bytes) { return 3.5 + 2.0 * double(bytes) / 4.5e6; }
+
+bool rows_dx(int32_t config) { return config >= 11 && config <= 13; }
+bool rows_dw(int32_t config) { return config == 19; }
+
+// What mx_rows_kernel loses to an A off 16-byte rows: its 16-byte pieces (DX), which every 128 columns of C
+// read again, touch two lines each (130 x 4097 x 4095: 17.1 -> 29.4 us, 37 x 2049 x 2051: 6.9 -> 7.7);
+// its dwords (DW) next to nothing (130 x 4097 x 4095: 22.0 -> 22.5).
+double unaligned_us(int32_t config, int64_t M, int64_t N, int64_t K) {
+    return rows_dx(config) ? 2.0 * double(M) * double(K) * double(ceil_div(N, 128)) / 2.9e6 : 0.0;
+}
+
 // Modelled microseconds of a plan, without the launch and what moves in any plan.
-double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p, int64_t copied) {
+double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p, int64_t copied_b, int64_t copied_a) {
     const MxConfig &c = kMxConfigs[p.config];
     if (p.config == kMxDecode || p.config == kMxDecode48) {
         // W at the rate it streams at, A once for every 16 columns at the rate of the L2s.
@@ -91,14 +104,25 @@ double modelled_us(MxOp op, int64_t M, int64_t N, int64_t K, const MxPlan &p, in
     // 1 x 28672 x 8192: 31.7 us, where the decode kernel takes 28.0).
     const double moved = 2.0 * double(M) * double(K) + double(N) * double(K) * (op == MX_DW ? 1.03 : 0.53) +
                          double(M) * double(N) * (op == MX_DW ? 4 : 2);
-    // Operands copied to aligned rows first: a launch and both ways through memory.
-    const double copy = copied > 0 ? 3.5 + 2.0 * double(copied) / 4.5e6 : 0.0;
+    double copy = 0;
+    if (copied_a > 0 && mx_direct_a(p.config, M, N, K)) {
+        copy = unaligned_us(p.config, M, N, K);
+        copied_a = 0;
+    }
+    if (copied_a + copied_b > 0) copy += copy_us(copied_a + copied_b);
     return (t > moved / 4.4e6 ? t : moved / 4.4e6) + copy;
 }
 
 }  // namespace
 
-bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied, int32_t config, int32_t split, MxPlan *out) {
+bool mx_direct_a(int32_t config, int64_t M, int64_t N, int64_t K) {
+    if (config == kMxDecode || config == kMxDecode48) return true;
+    if (rows_dw(config)) return M >= 2;                          // its dwords are two columns of A
+    return rows_dx(config) && unaligned_us(config, M, N, K) < copy_us(2 * M * K);
+}
+
+bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, int32_t config, int32_t split,
+               MxPlan *out) {
     if (config >= 0) return evaluate(op, M, K, config, split > 0 ? split : 1, out);
     static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
     double best = 0;
@@ -115,7 +139,7 @@ bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied, int32_t
             const double tiles = double(ceil_div(M, kMxConfigs[c].bm)) * double(ceil_div(N, kMxConfigs[c].bn));
             const double groups = tiles * p.split_k;
             if (split == 0 && p.split_k > 1 && kMxConfigs[c].bn > 16 && groups > 4 * kCUs) break;
-            const double t = modelled_us(op, M, N, K, p, copied);
+            const double t = modelled_us(op, M, N, K, p, copied_b, copied_a);
             if (!found || t < best) {
                 best = t;
                 *out = p;

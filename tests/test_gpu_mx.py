@@ -194,6 +194,17 @@ def test_products_with_strides_and_offsets(op, size, pads, offsets):
     check_product(op, *size, False, seed=sum(size), pads=pads, offsets=offsets)
 
 
+@pytest.mark.parametrize("op", ["dx", "dw"])
+@pytest.mark.parametrize("M", [1, 2, 3, 31, 33, 49, 130])
+@pytest.mark.parametrize("K", [1, 31, 33, 95, 260, 515])
+def test_gradients_of_an_activation_at_any_address(op, M, K):
+    """A off 16-byte rows, the packed matrix on them: A is read where it lies, up to its rows' ends."""
+    N = 70 if op == "dx" else 77
+    width = (N + 1) // 2 if op == "dx" else N
+    for pad in (0, 1):
+        check_product(op, M, N, K, False, seed=M + K, pads=(pad, -width % 16, 0, 0), offsets=(1, 0, 0, 0))
+
+
 @pytest.mark.parametrize("op", OPS)
 @pytest.mark.parametrize("M", [3, 40])
 def test_rows_far_apart(op, M):
