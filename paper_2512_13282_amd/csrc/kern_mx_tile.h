@@ -69,7 +69,7 @@ __device__ __forceinline__ void mx_sum_groups(f32x16_t (&acc)[TM][TN], uint8_t *
 // waves waiting 33 %, 1.85 rounds of 192 x 256 tiles); 16 x 4096 x 14336 12.7 us, of which the K loop
 // ends at 7.5 (46 GB/s per CU, what the load path gives) and the slices' sum takes 4.5.
 // Against it, at 2048 x 11008 x 4096: 128 x 256 tiles at four waves per SIMD 165 to 180 us (spills), stages
-// of 64 k 164; a stage's loads all at once cost a few per cent more.
+// of 64 k 158 (128 x 256) and 164; a stage's loads all at once a few per cent more.
 // ---------------------------------------------------------------------------
 template <int BM, int BN, int WM, int WN, int WK, int WAVES_PER_EU, int KS, int NS, int PANEL>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN * WK, 64 * WM * WN * WK),
