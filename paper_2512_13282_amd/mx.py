@@ -100,12 +100,13 @@ class MxMatrix(NamedTuple):
 # the stream's handle without a Stream object.
 
 def _ld(stride, rows, cols):
-    """The row stride of a matrix whose rows are contiguous (a single row or column has no
-    meaningful other one)."""
+    """The row stride of a matrix whose rows are contiguous (a column's elements are single, and a
+    single row or an empty matrix has no meaningful stride).  The entry points refuse one that is
+    shorter than a row: an expanded tensor's, say, which holds fewer elements than the matrix."""
     ld, step = stride
     if step != 1 and cols > 1:
         raise ValueError("rows must be contiguous")
-    return (ld if ld > cols else cols) if rows > 1 and cols else cols or 1
+    return ld if rows > 1 and cols else cols or 1
 
 
 def _packed(Q, bits, code_dtype, byte_dtype, device):
