@@ -30,8 +30,8 @@
  * call that needs it, grown the same way (to at least twice its size; the buffer
  * it replaces stays allocated, since a graph captured on the stream may use it),
  * and kept until the process ends or gemm_release_workspace.  Calls on one
- * stream run in order and share it safely; calls on different streams use
- * different workspaces.  A captured call uses the workspace of the stream it was
+ * stream run in order and share it safely, those of several host threads too;
+ * calls on different streams use different workspaces.  A captured call uses the workspace of the stream it was
  * captured on: its replays must be ordered with that stream's other calls.  A stream handle that is destroyed and re-created with
  * the same value while work of the old one is still running must not be used.
  *

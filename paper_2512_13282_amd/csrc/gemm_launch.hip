@@ -51,8 +51,13 @@ __global__ __launch_bounds__(256) void zero_u32_kernel(uint32_t *__restrict__ p,
 // current one's size.  Launches on one stream run in order and each launch
 // leaves every counter it touched at zero, which is what makes the counters
 // reusable; separate streams get separate workspaces.
+//
+// A call may take several launches (copies of operands, the product, a separate
+// reduction) that hand data on through the workspace.  `use` keeps another thread's call
+// on the same stream from queueing its own launches between them.
 namespace {
 struct Workspace {
+    std::mutex use;
     void *partials = nullptr;
     size_t partial_bytes = 0;
     uint32_t *counters = nullptr;
@@ -63,7 +68,7 @@ struct Workspace {
         if (p != nullptr) replaced[num_replaced++] = p;
     }
 };
-std::mutex g_ws_mu;
+std::mutex g_ws_mu;              // the map; never taken while a workspace is held
 std::map<std::pair<int, uintptr_t>, Workspace> g_ws;
 
 size_t grow(size_t need, size_t have, size_t quantum) {
@@ -102,12 +107,17 @@ static void *malloc_in_capture(size_t bytes) {
 // the counters do not grow (what zeroes them would run at each replay, not now), and the call
 // gets LAUNCH_NO_COUNTERS, before anything is queued.
 int acquire_workspace(void *stream_ptr, size_t partial_bytes, int64_t counter_words, void **partials,
-                      uint32_t **counters) {
+                      uint32_t **counters, WorkspaceHold &hold) {
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return LAUNCH_HIP_ERROR;
-    std::lock_guard<std::mutex> lk(g_ws_mu);
-    Workspace &w = g_ws[{dev, reinterpret_cast<uintptr_t>(stream)}];
+    Workspace *entry;
+    {
+        std::lock_guard<std::mutex> lk(g_ws_mu);
+        entry = &g_ws[{dev, reinterpret_cast<uintptr_t>(stream)}];     // stays there until release_workspaces
+    }
+    Workspace &w = *entry;
+    WorkspaceHold use(w.use);
     bool capturing = false;
     if (w.partial_bytes < partial_bytes || w.counter_cap < counter_words) {
         if (fail_workspace_for_test()) return LAUNCH_NO_MEMORY;
@@ -151,6 +161,7 @@ int acquire_workspace(void *stream_ptr, size_t partial_bytes, int64_t counter_wo
     }
     *partials = w.partials;
     *counters = w.counters;
+    hold = std::move(use);
     return LAUNCH_OK;
 }
 
@@ -170,7 +181,6 @@ int release_workspaces() {
         if (w.counters != nullptr && hipFree(w.counters) != hipSuccess) rc = LAUNCH_HIP_ERROR;
         for (int i = 0; i < w.num_replaced; ++i)
             if (hipFree(w.replaced[i]) != hipSuccess) rc = LAUNCH_HIP_ERROR;
-        w = Workspace{};
     }
     g_ws.clear();
     if (hipSetDevice(cur) != hipSuccess) rc = LAUNCH_HIP_ERROR;
@@ -223,6 +233,7 @@ int launch_gemm(const KernelArgs &a, int32_t cfg, int64_t grid, void *stream_ptr
     KernelArgs args = a;
     args.workspace = nullptr;
     args.counters = nullptr;
+    WorkspaceHold hold;
     if (args.split_k > 1 && args.reduce_in_kernel != REDUCE_ATOMIC) {
         const bool flag = args.reduce_in_kernel == REDUCE_ATOMIC_FLAG;
         if (flag && (args.dtype != DT_I8 || args.epilogue != EPI_NONE ||
@@ -249,12 +260,12 @@ int launch_gemm(const KernelArgs &a, int32_t cfg, int64_t grid, void *stream_ptr
                 if (hipGetLastError() != hipSuccess) return LAUNCH_HIP_ERROR;
             }
         } else {
-            int rc = acquire_workspace(stream, bytes, counter_words, &args.workspace, &args.counters);
+            int rc = acquire_workspace(stream, bytes, counter_words, &args.workspace, &args.counters, hold);
             if (rc == LAUNCH_NO_COUNTERS) {
                 // The reductions with one more launch and no counters: the same slices summed in
                 // the same order, or int32 adds in any, so the same bits.
                 args.reduce_in_kernel = flag ? REDUCE_ATOMIC : REDUCE_SEPARATE;
-                rc = flag ? LAUNCH_OK : acquire_workspace(stream, bytes, 0, &args.workspace, &args.counters);
+                rc = flag ? LAUNCH_OK : acquire_workspace(stream, bytes, 0, &args.workspace, &args.counters, hold);
             }
             if (rc != LAUNCH_OK) return rc;
         }

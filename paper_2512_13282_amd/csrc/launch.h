@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <mutex>
+
 namespace gemm {
 
 struct KernelArgs {
@@ -66,10 +68,13 @@ constexpr int64_t kScratchCounterBytes = int64_t(64) << 10;
 int launch_gemm(const KernelArgs &a, int32_t config, int64_t grid, void *stream, bool static_scratch = false);
 
 // The workspace of `stream` on the current device, grown where it is too small: at least
-// partial_bytes of scratch and counter_words arrival counters, zero between launches.
-// LAUNCH_NO_COUNTERS, and nothing queued, where the counters would have to grow while the
-// stream is being captured.
-int acquire_workspace(void *stream, size_t partial_bytes, int64_t counter_words, void **partials, uint32_t **counters);
+// partial_bytes of scratch and counter_words arrival counters, zero between launches.  With
+// LAUNCH_OK it is `hold`'s, which the caller keeps until the last launch that uses the
+// workspace is queued.  LAUNCH_NO_COUNTERS, and nothing queued, where the counters would have
+// to grow while the stream is being captured.
+using WorkspaceHold = std::unique_lock<std::mutex>;
+int acquire_workspace(void *stream, size_t partial_bytes, int64_t counter_words, void **partials, uint32_t **counters,
+                      WorkspaceHold &hold);
 
 // Frees every cached split-K workspace (all devices and streams) after
 // synchronising each device that holds one.

@@ -75,14 +75,15 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const int64_t s_bytes = copy_s ? b_rows * padded(s_used) : 0;
     if ((copy_a && padded(a_used) > kMxMostStride) || (copy_b && padded(b_used) > kMxMostStride) || (copy_s && padded(s_used) > kMxMostStride))
         return LAUNCH_UNSUPPORTED;
+    WorkspaceHold hold;                  // over the copies, the product and its separate reduction
     if (partial + a_bytes + b_bytes + s_bytes > 0) {
         void *ws = nullptr;
         uint32_t *counters = nullptr;
         const size_t bytes = size_t(partial + a_bytes + b_bytes + s_bytes);
-        int rc = acquire_workspace(stream_ptr, bytes, a.g.split_k > 1 ? tm * tn : 0, &ws, &counters);
+        int rc = acquire_workspace(stream_ptr, bytes, a.g.split_k > 1 ? tm * tn : 0, &ws, &counters, hold);
         if (rc == LAUNCH_NO_COUNTERS) {
             a.g.reduce_in_kernel = REDUCE_SEPARATE;     // the same sums in the same order
-            rc = acquire_workspace(stream_ptr, bytes, 0, &ws, &counters);
+            rc = acquire_workspace(stream_ptr, bytes, 0, &ws, &counters, hold);
         }
         if (rc != LAUNCH_OK) return rc;
         a.g.workspace = ws;
