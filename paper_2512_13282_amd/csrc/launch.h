@@ -52,7 +52,7 @@ enum { REDUCE_SEPARATE = 0, REDUCE_LAST_SLICE = 1, REDUCE_ATOMIC = 2, REDUCE_ATO
 // atomics behind each other (a GEMV with 32 slices per tile ran 1.9x slower).
 constexpr int kFlagCounterStride = 32;
 
-enum { LAUNCH_OK = 0, LAUNCH_HIP_ERROR = 1, LAUNCH_NO_MEMORY = 2, LAUNCH_SCRATCH_LIMIT = 3, LAUNCH_NO_COUNTERS = 4, LAUNCH_UNSUPPORTED = 5 };
+enum { LAUNCH_OK = 0, LAUNCH_HIP_ERROR = 1, LAUNCH_NO_MEMORY = 2, LAUNCH_SCRATCH_LIMIT = 3, LAUNCH_NO_COUNTERS = 4 };
 
 // The fixed split-K scratch of the entry point that allocates nothing: per device,
 // kScratchCounterBytes of per-tile arrival counters followed by the partial planes.

@@ -37,7 +37,7 @@ struct MxMatrixArgs {          // packing and unpacking
 struct MxPlan {
     int32_t config;
     int32_t split_k;
-    int64_t k_chunk;           // K of a slice, a multiple of 256
+    int64_t k_chunk;           // K of a slice, a multiple of 256 (the decode kernel's: of 128)
 };
 
 struct MxConfig {
@@ -65,9 +65,15 @@ inline bool mx_loadable(const void *p, int64_t stride) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0 && stride <= kMxMostStride;
 }
 
+// Bytes of a row of A and of B's codes, on to the next multiple of 16.
+inline int64_t mx_a_row(MxOp op, int64_t M, int64_t K) { return ((op == MX_DW ? M : K) * 2 + 15) / 16 * 16; }
+inline int64_t mx_b_row(MxOp op, int64_t N, int64_t K) {
+    return ((op == MX_FWD ? (K + 1) / 2 : op == MX_DX ? (N + 1) / 2 : N) + 15) / 16 * 16;
+}
+
 // The plan for a product, where `copied_a` and `copied_b` bytes of its operands are not loadable.
 // config >= 0 and split > 0 say which one to evaluate instead.
-// False where that configuration is not the operator's, or cannot hold the rows.
+// False where no configuration (the one named) is the operator's and takes the rows.
 bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, int32_t config, int32_t split, MxPlan *out);
 
 // Each queues its kernels on `stream` (a hipStream_t) and returns a LAUNCH_* value.

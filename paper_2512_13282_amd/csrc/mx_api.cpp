@@ -42,7 +42,6 @@ int status(int launched) {
     switch (launched) {
         case gemm::LAUNCH_OK: return GEMM_OK;
         case gemm::LAUNCH_NO_MEMORY: return GEMM_ERR_NO_MEMORY;
-        case gemm::LAUNCH_UNSUPPORTED: return GEMM_ERR_UNSUPPORTED;
         default: return GEMM_ERR_HIP;
     }
 }
@@ -186,7 +185,12 @@ int mx_plan(int op, int64_t M, int64_t N, int64_t K, mx_plan_info *out) {
     out->config = -1;
     if (M == 0 || N == 0) return GEMM_OK;
     gemm::MxPlan plan;
-    const int rc = plan_for(gemm::MxOp(op), M, N, K, 0, 0, &plan);
+    // Rows on 16 bytes, but of what is longer than the tile kernels can step over.
+    const gemm::MxOp o = gemm::MxOp(op);
+    const bool sizes = M <= INT32_MAX && N <= INT32_MAX && K <= INT32_MAX;       // else plan_for refuses
+    const int64_t a_row = sizes ? gemm::mx_a_row(o, M, K) : 0, b_row = sizes ? gemm::mx_b_row(o, N, K) : 0;
+    const int rc = plan_for(o, M, N, K, a_row > gemm::kMxMostStride ? a_row * (o == gemm::MX_DW ? K : M) : 0,
+                            b_row > gemm::kMxMostStride ? b_row * (o == gemm::MX_FWD ? N : K) : 0, &plan);
     if (rc != GEMM_OK) return rc;
     const gemm::MxConfig &c = gemm::kMxConfigs[plan.config];
     out->config = plan.config;

@@ -34,8 +34,6 @@ __global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
 }
 
 namespace {
-int64_t padded(int64_t bytes) { return (bytes + 15) / 16 * 16; }
-
 bool realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
     const int64_t n = (x.rows * (x.pitch / 16) + y.rows * (y.pitch / 16) + 255) / 256;
     hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream, x, y);
@@ -59,11 +57,12 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     a.g.group_m = 4;
     a.g.reduce_in_kernel = REDUCE_LAST_SLICE;
 
-    // Scratch: the K slices' partial sums, and aligned copies of operands that need one.
-    const int64_t a_rows = op == MX_DW ? a.g.K : a.g.M, a_used = (op == MX_DW ? a.g.M : a.g.K) * 2;
+    // Scratch: the K slices' partial sums, and aligned copies of operands that need one (their rows are
+    // no longer than kMxMostStride: mx_select).
+    const int64_t a_rows = op == MX_DW ? a.g.K : a.g.M, a_used = (op == MX_DW ? a.g.M : a.g.K) * 2, a_row = mx_a_row(op, a.g.M, a.g.K);
     const int64_t b_rows = op == MX_FWD ? a.g.N : a.g.K, b_cols = op == MX_FWD ? a.g.K : a.g.N;
-    const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2;
-    const int64_t s_used = (b_cols + kMxBlock - 1) / kMxBlock;
+    const int64_t b_used = op == MX_DW ? b_cols : (b_cols + 1) / 2, b_row = mx_b_row(op, a.g.N, a.g.K);
+    const int64_t s_used = (b_cols + kMxBlock - 1) / kMxBlock, s_row = (s_used + 15) / 16 * 16;
     const bool any_a = decode || (a.g.lda * 2 <= kMxMostStride && mx_direct_a(plan.config, a.g.M, a.g.N, a.g.K));
     const bool copy_a = !any_a && a.g.K > 0 && !mx_loadable(a.g.A, a.g.lda * 2);
     const bool copy_b = !decode && a.g.K > 0 && !mx_loadable(a.g.B, a.g.ldb);
@@ -71,10 +70,8 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const bool copy_s = op != MX_FWD && a.g.K > 0 && a.ld_scales > kMxMostStride;
     // Partial sums: whole tiles (the decode kernel's: 16 rows), at least the planes that the separate reduction reads.
     const int64_t partial = a.g.split_k > 1 ? a.g.split_k * tm * tn * c.bm * c.bn * 4 : 0;
-    const int64_t a_bytes = copy_a ? a_rows * padded(a_used) : 0, b_bytes = copy_b ? b_rows * padded(b_used) : 0;
-    const int64_t s_bytes = copy_s ? b_rows * padded(s_used) : 0;
-    if ((copy_a && padded(a_used) > kMxMostStride) || (copy_b && padded(b_used) > kMxMostStride) || (copy_s && padded(s_used) > kMxMostStride))
-        return LAUNCH_UNSUPPORTED;
+    const int64_t a_bytes = copy_a ? a_rows * a_row : 0, b_bytes = copy_b ? b_rows * b_row : 0;
+    const int64_t s_bytes = copy_s ? b_rows * s_row : 0;
     WorkspaceHold hold;                  // over the copies, the product and its separate reduction
     if (partial + a_bytes + b_bytes + s_bytes > 0) {
         void *ws = nullptr;
@@ -91,18 +88,18 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
         uint8_t *const copies = static_cast<uint8_t *>(ws) + partial;
         MxCopy x{}, y{};
         if (copy_a) {
-            x = MxCopy{static_cast<const uint8_t *>(a.g.A), copies, a.g.lda * 2, a_used, padded(a_used), a_rows};
+            x = MxCopy{static_cast<const uint8_t *>(a.g.A), copies, a.g.lda * 2, a_used, a_row, a_rows};
             a.g.A = x.dst;
             a.g.lda = x.pitch / 2;
         }
         if (copy_b) {
-            y = MxCopy{static_cast<const uint8_t *>(a.g.B), copies + a_bytes, a.g.ldb, b_used, padded(b_used), b_rows};
+            y = MxCopy{static_cast<const uint8_t *>(a.g.B), copies + a_bytes, a.g.ldb, b_used, b_row, b_rows};
             a.g.B = y.dst;
             a.g.ldb = y.pitch;
         }
         if ((copy_a || copy_b) && !realign(x, y, stream)) return LAUNCH_HIP_ERROR;
         if (copy_s) {
-            x = MxCopy{a.scales, copies + a_bytes + b_bytes, a.ld_scales, s_used, padded(s_used), b_rows};
+            x = MxCopy{a.scales, copies + a_bytes + b_bytes, a.ld_scales, s_used, s_row, b_rows};
             a.scales = x.dst;
             a.ld_scales = x.pitch;
             if (!realign(x, MxCopy{}, stream)) return LAUNCH_HIP_ERROR;

@@ -63,6 +63,13 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
     return out->split_k <= 65535 && int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX;
 }
 
+// Whether a configuration takes the operands, `copied_a` and `copied_b` bytes of which are not loadable: the
+// decode kernel reads any rows, the rest can have theirs copied where a row is no longer than a stride may be.
+bool holds(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, int32_t config) {
+    if (config == kMxDecode || config == kMxDecode48) return true;
+    return (copied_a == 0 || mx_a_row(op, M, K) <= kMxMostStride) && (copied_b == 0 || mx_b_row(op, N, K) <= kMxMostStride);
+}
+
 // Operands copied to aligned rows first: a launch and both ways through memory.
 double copy_us(int64_t bytes) { return 3.5 + 2.0 * double(bytes) / 4.5e6; }
 
@@ -123,12 +130,13 @@ bool mx_direct_a(int32_t config, int64_t M, int64_t N, int64_t K) {
 
 bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, int32_t config, int32_t split,
                MxPlan *out) {
-    if (config >= 0) return evaluate(op, M, K, config, split > 0 ? split : 1, out);
+    if (config >= 0)
+        return evaluate(op, M, K, config, split > 0 ? split : 1, out) && holds(op, M, N, K, copied_a, copied_b, config);
     static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
     double best = 0;
     bool found = false;
     for (int32_t c = 0; c < kMxNumConfigs; ++c) {
-        if (kMxConfigs[c].op != op) continue;
+        if (kMxConfigs[c].op != op || !holds(op, M, N, K, copied_a, copied_b, c)) continue;
         int32_t seen = 0;
         for (const int32_t s : kSplits) {
             MxPlan p;
