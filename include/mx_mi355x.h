@@ -31,7 +31,8 @@
  * GEMM_ERR_INVALID_VALUE is returned for a negative size, a stride that is too small,
  * a NULL pointer whose operand is non-empty, a bf16 or fp32 pointer that is not
  * aligned to its element size, and an output that overlaps an input or another output;
- * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more, or with rows of A,
+ * GEMM_ERR_UNSUPPORTED for a product with a size of 2^31 - 4096 or more, with more output
+ * tiles than a launch holds (2^23 workgroups of 512 threads), or with rows of A,
  * At or the codes longer than 4 MiB (up to 48 rows of A over W^T take K up to 1.1 * 10^8 / M).
  * Operands whose rows do not lie on 16-byte addresses are copied to rows that do, in the
  * stream's workspace, ahead of a product (but for a few rows of A over W^T, and A and At

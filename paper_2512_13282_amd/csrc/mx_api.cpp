@@ -74,7 +74,8 @@ struct CachedPlan {
 thread_local CachedPlan t_plans[64];
 
 int plan_for(gemm::MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, gemm::MxPlan *plan) {
-    if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX - 4096) return GEMM_ERR_UNSUPPORTED;    // 32-bit indices
+    constexpr int64_t kMost = INT32_MAX - 4096;      // 32-bit indices, up to the end of a tile or a stage
+    if (M > kMost || N > kMost || K > kMost) return GEMM_ERR_UNSUPPORTED;
     const int32_t config = g_forced[op].config, split = g_forced[op].split;
     if (config >= 0 || split > 0)
         return gemm::mx_select(op, M, N, K, copied_a, copied_b, config, split, plan) ? GEMM_OK : GEMM_ERR_UNSUPPORTED;

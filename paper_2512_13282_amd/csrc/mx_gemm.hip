@@ -49,7 +49,6 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
     const bool decode = plan.config == kMxDecode || plan.config == kMxDecode48;
     const int64_t tm = decode ? 1 : (a.g.M + c.bm - 1) / c.bm, tn = (a.g.N + c.bn - 1) / c.bn;
     const int64_t grid = tm * tn * plan.split_k;
-    if (grid > 0x7fffffff) return LAUNCH_HIP_ERROR;
     a.g.k_chunk = plan.k_chunk;
     a.g.split_k = plan.split_k;
     a.g.tiles_m = int32_t(tm);

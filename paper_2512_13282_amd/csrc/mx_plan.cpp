@@ -43,7 +43,7 @@ constexpr int kCUs = 256;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPlan *out) {
+bool evaluate(MxOp op, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, MxPlan *out) {
     if (config < 0 || config >= kMxNumConfigs || kMxConfigs[config].op != op) return false;
     const bool decode = config == kMxDecode || config == kMxDecode48;
     if (decode) {
@@ -58,9 +58,12 @@ bool evaluate(MxOp op, int64_t M, int64_t K, int32_t config, int32_t split, MxPl
     out->config = config;
     out->k_chunk = chunk;
     out->split_k = int32_t(K > 0 ? ceil_div(K, chunk) : 1);
-    // A tile's partial sums are addressed with 32 bits, and slices are a grid dimension.
+    // A tile's partial sums are addressed with 32 bits, the decode kernel's slices are a grid dimension of
+    // their own, and a dimension holds fewer than 2^32 threads.
     const MxConfig &c = kMxConfigs[config];
-    return out->split_k <= 65535 && int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX;
+    const int64_t tiles = (decode ? 1 : ceil_div(M, c.bm)) * ceil_div(N, c.bn);
+    const int64_t most = UINT32_MAX / (64 * c.waves) / (decode ? 1 : out->split_k);
+    return out->split_k <= 65535 && int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && tiles <= most;
 }
 
 // Whether a configuration takes the operands, `copied_a` and `copied_b` bytes of which are not loadable: the
@@ -131,7 +134,7 @@ bool mx_direct_a(int32_t config, int64_t M, int64_t N, int64_t K) {
 bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64_t copied_b, int32_t config, int32_t split,
                MxPlan *out) {
     if (config >= 0)
-        return evaluate(op, M, K, config, split > 0 ? split : 1, out) && holds(op, M, N, K, copied_a, copied_b, config);
+        return evaluate(op, M, N, K, config, split > 0 ? split : 1, out) && holds(op, M, N, K, copied_a, copied_b, config);
     static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
     double best = 0;
     bool found = false;
@@ -140,10 +143,10 @@ bool mx_select(MxOp op, int64_t M, int64_t N, int64_t K, int64_t copied_a, int64
         int32_t seen = 0;
         for (const int32_t s : kSplits) {
             MxPlan p;
-            if (!evaluate(op, M, K, c, split > 0 ? split : s, &p)) break;
+            if (!evaluate(op, M, N, K, c, split > 0 ? split : s, &p)) break;
             if (p.split_k == seen) continue;                     // the same slices again
             seen = p.split_k;
-            // Partial sums stay a fraction of the memory, and the grid a 32-bit number.
+            // Partial sums stay a fraction of the memory.
             const double tiles = double(ceil_div(M, kMxConfigs[c].bm)) * double(ceil_div(N, kMxConfigs[c].bn));
             const double groups = tiles * p.split_k;
             if (split == 0 && p.split_k > 1 && kMxConfigs[c].bn > 16 && groups > 4 * kCUs) break;
