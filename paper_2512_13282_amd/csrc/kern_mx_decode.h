@@ -156,8 +156,8 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
         if (i + U + u < n) multiply(u, i + U + u);
 
     // The end of K that is no whole chunk, by the wave whose part it ends: dwords of eight
-    // codes, and bytes within the last one.  Codes past the end meet A's zeros, under a
-    // scale that is no NaN.
+    // codes, and bytes within the last one.  Past the end codes are zeros under a scale that is
+    // no NaN, the unused half of an odd row's last byte too: it may stand for an infinity.
     if (chunks > whole && whole >= c0 && whole < end) {
         const int c = int(whole - c0);
         const int left = int(K - whole * 128) - 32 * grp;      // elements from this lane's block on
@@ -175,6 +175,7 @@ __global__ __launch_bounds__(64 * KW) void mx_decode_kernel(MxArgs a) {
             }
             w[0][t] = v;
         }
+        w[0] = mx4_first(w[0], left);
         multiply(0, c);
     }
 

@@ -242,12 +242,18 @@ void mx_fwd_kernel(MxArgs a) {
         constexpr int BUF = decltype(buf_c)::value;
         ring_barrier<(NS - 2) * LPS>();
         uint8_t *const st = lds[BUF];
-        if (kt == nk - 1 && (k_len & 7) != 0) {
-            // K ends inside a chunk: what follows it in A's row is not part of the sum.
+        if (kt == nk - 1 && (k_len & 31) != 0) {
+            // K ends inside a block: the codes that follow it may stand for infinities, which A's zeros
+            // would make NaN.  Inside a chunk: what follows it in A's row is not part of the sum.
             const int kl = k_len - kt * KS, part = kl / 64, c = (kl % 64) / 8;
-            for (int r = tid; r < BM; r += THREADS)
-                for (int e = kl & 7; e < 8; ++e)
-                    reinterpret_cast<uint16_t *>(st + part * A_PART + r * 128 + 16 * swz(c, r))[e] = 0;
+            for (int r = tid; r < BN; r += THREADS) {
+                u32x4_t *const w = reinterpret_cast<u32x4_t *>(st + A_STAGE + r * PITCH + 16 * ((kl / 32) ^ w_swz(r)));
+                *w = mx4_first(*w, kl % 32);
+            }
+            if ((kl & 7) != 0)
+                for (int r = tid; r < BM; r += THREADS)
+                    for (int e = kl & 7; e < 8; ++e)
+                        reinterpret_cast<uint16_t *>(st + part * A_PART + r * 128 + 16 * swz(c, r))[e] = 0;
             phase_barrier();
         }
         const int block0 = (kt * KS % PANEL) / kMxBlock + half;

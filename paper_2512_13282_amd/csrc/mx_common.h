@@ -36,6 +36,16 @@ __device__ __forceinline__ u32x4_t mx4_to_bf16(uint32_t codes, float scale) {
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 
+// The first n of a block's 32 codes, zeros after them.
+__device__ __forceinline__ u32x4_t mx4_first(u32x4_t codes, int n) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int left = n - 8 * t;
+        codes[t] &= left >= 8 ? ~0u : left > 0 ? (1u << (4 * left)) - 1u : 0u;
+    }
+    return codes;
+}
+
 // 2^(e - 127) as fp32; NaN for e = 255.
 __device__ __forceinline__ float mx_scale(uint32_t e) {
     return __builtin_bit_cast(float, e == 0u ? 0x00400000u : e == 255u ? 0x7fc00000u : e << 23);

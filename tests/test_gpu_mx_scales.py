@@ -93,6 +93,27 @@ def test_every_scale_byte(op):
 
 
 @pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("size", [(1, 33, 31), (5, 70, 95), (40, 130, 281), (150, 300, 517)], ids=lambda s: "x".join(map(str, s)))
+def test_codes_past_the_end_are_no_part_of_the_sum(op, size):
+    """Under bytes 253 and 254 the codes 4 and 6 are infinite.  The matrix holds none of them; what
+    surrounds it (and the unused half of a row's last byte) does."""
+    M, N, K = size
+    a, codes, scales, cols = operands(op, M, N, K, sum(size), (253, 254) if op != "dw" else (249, 250), -60)
+    if op == "dw":
+        codes = (codes.astype(np.int64) % 32).astype(np.int8)
+    else:
+        codes = (codes & 0x99) | np.where(codes & 0x20, 0x22, 0).astype(np.uint8) & 0x22     # magnitudes 0, 1 (0.5), 2 (1), 3 (1.5)
+        if cols % 2:
+            codes[:, -1] = codes[:, -1] & 0x0f | 0x70
+    want, magnitude = ref.product(op, ref.widen(a), ref.values(codes, scales, cols))
+    assert np.all(np.isfinite(want))
+    lim = ref.bound(K, magnitude, want, False)
+    for plan in over_configurations(op, M, N, K):
+        C = run_product(op, M, N, K, a, codes, scales, False)
+        assert np.all(np.abs(C - want) <= lim), (plan, np.argwhere(~(np.abs(C - want) <= lim))[:4].tolist())
+
+
+@pytest.mark.parametrize("op", OPS)
 @pytest.mark.parametrize("size", [(1, 96, 160), (20, 96, 200), (140, 260, 300)], ids=lambda s: "x".join(map(str, s)))
 def test_values_past_the_range_are_infinite(op, size):
     """One value past bf16's range makes the results that use it infinite, of the product's sign, and no
