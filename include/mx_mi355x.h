@@ -17,9 +17,12 @@
  *           8 bits: an element is a signed byte, written in [-127, 127]; row stride
  *           ldq, in bytes, at least cols.
  *
- * An element stands for (its code's value) * (its block's scale).  Every such value
- * is a bf16 number exactly, so the products below work on the stored values
- * themselves: products are exact and are accumulated in fp32, as gemm_bf16_f32's.
+ * An element stands for (its code's value) * (its block's scale).  Every such value is a
+ * bf16 number exactly, but for those past bf16's range, which count as infinities of
+ * their sign: code values of 2^(255 - e) and more (4 bits: under bytes 253 and 254; 8
+ * bits: from 248 on).  Packing makes none of them.
+ * The products below work on these values themselves: products are exact and are
+ * accumulated in fp32, as gemm_bf16_f32's.
  *
  * Ownership, workspaces, streams, capture and error codes are those of
  * gemm_mi355x.h: operands are caller-owned DEVICE pointers on the current device,
