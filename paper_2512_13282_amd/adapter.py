@@ -15,6 +15,19 @@ import torch
 from . import binding
 
 
+class _FirstDerivative(torch.autograd.Function):
+    """A gradient that came out of kernels which autograd does not see, as a function of the tensors behind it:
+    whoever differentiates it again is told so, instead of taking it for a constant."""
+
+    @staticmethod
+    def forward(ctx, gradient, *behind):
+        return gradient.view_as(gradient)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("AdapterLinear has first derivatives only")
+
+
 class _AdapterLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, A, B):
@@ -39,6 +52,8 @@ class _AdapterLinear(torch.autograd.Function):
             dx = binding.linear_mx4_dx(dy, ctx.W, out_dtype=torch.float32)   # dy . W
             dx += binding.mm_bf16_f32(dh, A)
             dx = dx.to(torch.bfloat16)
+        if torch.is_grad_enabled():                                          # create_graph=True
+            dx, dA, dB = (None if g is None else _FirstDerivative.apply(g, dy, A, B) for g in (dx, dA, dB))
         return dx, None, dA, dB
 
 
@@ -54,7 +69,8 @@ class AdapterLinear(torch.nn.Module):
         self.B = torch.nn.Parameter(torch.zeros(n_out, rank, device=dev, dtype=torch.bfloat16))
 
     def forward(self, x):
-        """x: tokens x n_in, bf16 (one token to a batch of prompts)."""
+        """x: tokens x n_in, bf16 (one token to a batch of prompts).  First derivatives only: a gradient of a
+        gradient raises."""
         if torch.is_grad_enabled():
             return _AdapterLinear.apply(x, self.weight, self.A, self.B)
         h = binding.mm_bf16_f32(x, self.A.t()).to(torch.bfloat16)
