@@ -57,16 +57,41 @@ class _AdapterLinear(torch.autograd.Function):
         return dx, None, dA, dB
 
 
+def _rows16(codes):
+    """Codes with their rows a multiple of 16 bytes apart, as packing lays them out: where they are not
+    (a module that is moved or loaded gets them one after the other), every product would copy them."""
+    rows, width = codes.shape
+    if rows < 2 or codes.stride(0) % 16 == 0 and codes.stride(1) == 1:
+        return codes
+    out = torch.empty_strided((rows, width), (-(-width // 16) * 16, 1), dtype=codes.dtype, device=codes.device)
+    return out.copy_(codes)
+
+
 class AdapterLinear(torch.nn.Module):
-    """``weight``: a bf16 matrix (n_out x n_in) on the GPU, packed to 4 bits here, or an ``MxMatrix``."""
+    """``weight``: a bf16 matrix (n_out x n_in) on the GPU, packed to 4 bits here, or an ``MxMatrix``.  Its parts are
+    buffers of the module, so that the adapter is saved, loaded and moved with the weight it was trained over."""
 
     def __init__(self, weight, rank: int):
         super().__init__()
-        self.weight = weight if isinstance(weight, binding.MxMatrix) else binding.pack_mx4(weight)
-        n_out, n_in = self.weight.codes.shape[0], self.weight.cols
-        dev = self.weight.codes.device
+        codes, scales, n_in = weight if isinstance(weight, binding.MxMatrix) else binding.pack_mx4(weight)
+        n_out, dev = codes.shape[0], codes.device
+        self.register_buffer("weight_codes", _rows16(codes))
+        self.register_buffer("weight_scales", scales)
         self.A = torch.nn.Parameter((torch.randn(rank, n_in, device=dev) / n_in ** 0.5).to(torch.bfloat16))
         self.B = torch.nn.Parameter(torch.zeros(n_out, rank, device=dev, dtype=torch.bfloat16))
+
+    @property
+    def weight(self) -> binding.MxMatrix:
+        return binding.MxMatrix(self.weight_codes, self.weight_scales, self.A.shape[1])
+
+    @weight.setter
+    def weight(self, W: binding.MxMatrix):
+        self.weight_codes, self.weight_scales = _rows16(W.codes), W.scales
+
+    def _apply(self, fn, *args, **kwargs):
+        super()._apply(fn, *args, **kwargs)
+        self.weight_codes = _rows16(self.weight_codes)
+        return self
 
     def forward(self, x):
         """x: tokens x n_in, bf16 (one token to a batch of prompts).  First derivatives only: a gradient of a

@@ -87,3 +87,51 @@ def test_a_gradient_that_is_a_constant_stays_one(plain):
     layer.B.requires_grad_(False)
     g, = torch.autograd.grad(layer(x).sum(), x, create_graph=True)
     assert not g.requires_grad
+
+
+def same(a, b):
+    return torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales) and a.cols == b.cols
+
+
+def test_a_saved_layer_holds_its_weight(plain, tmp_path):
+    layer, x = layer_and_input()
+    path = tmp_path / "layer.pt"
+    torch.save(layer.state_dict(), path)
+    other = adapter.AdapterLinear(base(seed=3), RANK)
+    assert not same(other.weight, layer.weight)
+    other.load_state_dict(torch.load(path, weights_only=True))
+    assert same(other.weight, layer.weight)
+    with torch.no_grad():
+        assert torch.equal(other(x), layer(x))
+    # An adapter alone, or one over a weight of another shape, is not taken for a layer.
+    with pytest.raises(RuntimeError):
+        other.load_state_dict({"A": layer.A, "B": layer.B})
+    with pytest.raises(RuntimeError):
+        adapter.AdapterLinear(base(n_in=38), RANK).load_state_dict(layer.state_dict())
+
+
+@pytest.mark.parametrize("move", [lambda m: m.to("meta"), lambda m: m.to_empty(device="meta"),
+                                  lambda m: torch.nn.Sequential(m).to("meta")[0]])
+def test_the_weight_moves_with_the_layer(move):
+    layer = move(adapter.AdapterLinear(base(), RANK))
+    assert {t.device.type for t in (*layer.weight[:2], layer.A, layer.B)} == {"meta"}
+    # Rows stay where the products read them as they lie.
+    assert layer.weight.codes.stride() == (32, 1) and layer.weight.cols == N_IN
+
+
+def test_rows_that_follow_each_other_are_laid_out_once():
+    Q = base()
+    layer = adapter.AdapterLinear(binding.MxMatrix(Q.codes.contiguous(), Q.scales, Q.cols), RANK)
+    assert layer.weight.codes.stride() == (32, 1) and same(layer.weight, Q)
+    layer.weight = binding.MxMatrix(base(seed=2).codes.contiguous(), base(seed=2).scales, N_IN)
+    assert layer.weight.codes.stride() == (32, 1) and same(layer.weight, base(seed=2))
+    layer.weight = Q
+    layer.load_state_dict({k: v.clone().contiguous() for k, v in layer.state_dict().items()}, assign=True)
+    assert same(layer.weight, Q)
+    assert same(adapter.AdapterLinear(base(n_in=1), 1).weight, base(n_in=1))
+
+
+def test_only_the_adapter_learns():
+    layer = adapter.AdapterLinear(base(), RANK)
+    assert [n for n, _ in layer.named_parameters()] == ["A", "B"]
+    assert not layer.weight.codes.requires_grad
