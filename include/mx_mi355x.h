@@ -39,7 +39,9 @@
  * At or the codes longer than 4 MiB (up to 48 rows of A over W^T take K up to 1.1 * 10^8 / M).
  * Operands whose rows do not lie on 16-byte addresses are copied to rows that do, in the
  * stream's workspace, ahead of a product (but for a few rows of A over W^T, and A and At
- * where the results have few rows).
+ * where the results have few rows).  The workspace keeps the size of the largest such
+ * copies, and while it grows the buffers that it replaces, until gemm_release_workspace:
+ * codes with ldq and their address multiples of 16 cost no memory.
  */
 #ifndef MX_MI355X_H
 #define MX_MI355X_H

@@ -65,8 +65,8 @@ __device__ __forceinline__ void mx_sum_groups(f32x16_t (&acc)[TM][TN], uint8_t *
 // for each other (LDS read, conversion, MFMA: 1000 clocks per 128 k with one wave per
 // SIMD); a second wave fills those waits without more K slices to sum.
 //
-// Measured: 2048 x 11008 x 4096 154 us (1200 TFLOP/s; the matrix unit busy 56 % of the clocks,
-// waves waiting 33 %, 1.85 rounds of 192 x 256 tiles); 16 x 4096 x 14336 12.7 us, of which the K loop
+// Measured: 2048 x 11008 x 4096 154 to 164 us (1130 to 1200 TFLOP/s; the matrix unit busy 51 % of the
+// clocks, the compute units 85 %: 1.85 rounds of 192 x 256 tiles; waves waiting 37 % of theirs); 16 x 4096 x 14336 12.7 us, of which the K loop
 // ends at 7.5 (46 GB/s per CU, what the load path gives) and the slices' sum takes 4.5.
 // Against it, at 2048 x 11008 x 4096: 128 x 256 tiles at four waves per SIMD 165 to 180 us (spills), stages
 // of 64 k 158 (128 x 256) and 164; a stage's loads all at once a few per cent more.
@@ -326,9 +326,10 @@ void mx_fwd_kernel(MxArgs a) {
 //
 // Few rows are mx_rows_kernel's.
 //
-// Measured: DX 2048 x 4096 x 11008 158 us (1170 TFLOP/s, the matrix unit busy 52 % of the clocks); DW
-// 11008 x 4096 x 2048 182 us (1010 TFLOP/s, 46 % busy; 2.69 rounds of tiles, 6.4 us of stores of C in
-// each).  Against it: A in a ring of three stages made no difference (64.3 and 64.8 us at
+// Measured: DX 2048 x 4096 x 11008 158 to 167 us (1110 to 1170 TFLOP/s; the matrix unit busy 48 % of the
+// clocks, LDS 48 %, a quarter of it bank conflicts; waves wait for LDS 20 % of their time); DW 11008 x
+// 4096 x 2048 178 to 185 us (1000 to 1040 TFLOP/s; matrix unit 46 %, LDS 29 %, compute units 83 %: 2.69
+// rounds of tiles, 6.4 us of stores of C in each).  Against it: A in a ring of three stages made no difference (64.3 and 64.8 us at
 // 2048 x 4096 x 4096); the loads in two halves 114 against 106 us (DX 2048 x 8192 x 4096); X unpacked to
 // bf16 by a launch of its own 180 against 183.5 us (DW 11008 x 4096 x 2048) but 74 against 69 (4096 x
 // 4096 x 2048).

@@ -10,6 +10,9 @@ current stream and call them:
 * ``linear_mx4_dx(dY, W)``: its input gradient dY . W over the same packed weight (``dY`` has
   the weight's rows as its columns);
 * ``linear_mx8_dw(dY, X)``: the weight gradient dY^T . X over a packed input X (tokens x in).
+
+Operands may be strided along their rows.  An expanded one (the gradient of a sum over tokens, say)
+is refused, as by the dense helpers: ``.contiguous()`` makes it one that is taken.
 """
 from __future__ import annotations
 
