@@ -313,14 +313,20 @@ def mm_bf16_f32(A, B, out=None):
     return _mm_bf16_f32(A, B, out)
 
 
-# ---------------------------------------------------------------- block-scaled operands
-_MX = ("MxMatrix", "linear_mx4", "linear_mx4_dx", "linear_mx8_dw", "pack_mx4", "pack_mx8", "unpack_mx")
+# ---------------------------------------------------------------- operators of modules that build on this one
+_BY_MODULE = {
+    "mx": ("MxMatrix", "linear_mx4", "linear_mx4_dx", "linear_mx8_dw", "pack_mx4", "pack_mx8", "unpack_mx"),
+    "ffn": ("gated_linear", "gated_linear_grad", "gated_linear_dx", "gated_linear_dw", "linear_dw"),
+    "adapters": ("Adapters", "linear_adapters", "linear_adapters_dx", "linear_adapters_dw"),
+}
 
 
 def __getattr__(name):
-    # The helpers of mx.py, which builds on this module, by the same names here.
-    if name in _MX:
-        from . import mx
-        globals().update((n, getattr(mx, n)) for n in _MX)
-        return globals()[name]
+    # The helpers of mx.py, ffn.py and adapters.py, by the same names here.
+    for module, names in _BY_MODULE.items():
+        if name in names:
+            import importlib
+            m = importlib.import_module("." + module, __package__)
+            globals().update((n, getattr(m, n)) for n in names)
+            return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

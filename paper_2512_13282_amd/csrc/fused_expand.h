@@ -1,0 +1,119 @@
+// fused_expand.h -- the adapters' second product, h Q_i, onto a wave's sums.
+#pragma once
+
+#include "fused_common.h"
+
+namespace gemm {
+
+typedef float f32x4_el_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned u32x4_el2_t __attribute__((ext_vector_type(4), aligned(2)));
+
+// Eight floats as bf16 parts whose sum they are: the upper 8 bits of each, the next 8, and the last 8 (24 bits
+// in all, so three parts are exact and two leave 2^-16).  An infinity or a NaN is its own first part.
+__device__ __forceinline__ void split_bf16(const float (&v)[8], u32x4_t (&part)[3]) {
+    uint32_t b[3][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t x = __builtin_bit_cast(uint32_t, v[e]);
+        const bool finite = (x & 0x7f800000u) != 0x7f800000u;
+        const float rest = finite ? v[e] - __builtin_bit_cast(float, x & 0xffff0000u) : 0.0f;
+        const uint32_t y = __builtin_bit_cast(uint32_t, rest);
+        b[0][e] = finite || (x & 0x007fffffu) == 0u ? x : x | 0x00400000u;
+        b[1][e] = y;
+        b[2][e] = __builtin_bit_cast(uint32_t, rest - __builtin_bit_cast(float, y & 0xffff0000u));
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) part[p][d] = perm(b[p][2 * d + 1], b[p][2 * d], 0x07060302u);
+}
+
+// Row t's h from element k on, the first `left` of eight, summed over its planes in their order.
+__device__ __forceinline__ void load_h(const FusedArgs &a, int64_t t, int k, int left, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    for (int p = 0; p < a.planes; ++p) {
+        const float *const src = a.h + p * a.h_plane + t * a.r + k;
+        if (left >= 8) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_el_t *>(src), y = *reinterpret_cast<const f32x4_el_t *>(src + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] += x[e];
+                v[4 + e] += y[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) v[e] += src[e];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// acc += h_t Q_i(t) for the wave's rows (TM x 32 from r0) and columns (32 from c0 and 32 from c0 + HALF).  QT: Q_i
+// is N x r, else r x N.
+//
+// The adapters that occur among a fragment's 32 rows are taken one after the other (most fragments of a prompt hold
+// one, and a decode batch's rows of weights have to be read for each of its requests anyway), each as
+// a product of all 32 rows, of which only the adapter's own take the result: rows are chosen, not multiplied
+// by zeros, so an infinity or a NaN in one request's adapter stays out of the others'.  h keeps
+// its fp32 value in two bf16 parts (2^-16 left out, a bf16 result's half step being 2^-9), three and so all of it
+// for an fp32 result.  Runs ahead of the K loop, while the first stages are on their way.
+// ---------------------------------------------------------------------------
+template <bool QT, int HALF, int TM, int TN>
+__device__ __forceinline__ void expand_adapters(const FusedArgs &a, f32x16_t (&acc)[TM][TN], int64_t r0, int64_t c0, int lane) {
+    if (a.n <= 0 || a.r <= 0) return;
+    const int l32 = lane & 31, half = lane >> 5;
+    const bool exact = a.g.epilogue != EPI_BF16;
+    const int64_t N = a.g.N;
+    int64_t col[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t c = c0 + HALF * j + l32;
+        col[j] = c < N ? c : N - 1;                              // not stored
+    }
+    static_for<0, TM>([&](auto i_c) __attribute__((always_inline)) {
+        constexpr int I = decltype(i_c)::value;
+        const int64_t t = r0 + 32 * I + l32;
+        const int own = t < a.g.M ? a.index[t] : -1;
+        const bool has = uint32_t(own) < uint32_t(a.n);
+        uint32_t pending = uint32_t(__ballot(has));
+        while (pending != 0u) {
+            const int cur = __builtin_amdgcn_readlane(own, __builtin_ctz(pending));
+            const uint32_t rows = uint32_t(__ballot(has && own == cur));
+            pending &= ~rows;
+            const uint16_t *const q = static_cast<const uint16_t *>(a.Q) + cur * a.sq;
+            f32x16_t sum[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) sum[j] = f32x16_t{};
+            for (int k = 0; k < a.r; k += 16) {
+                const int k0 = k + 8 * half, left = a.r - k0;
+                float v[8] = {};
+                if (has) load_h(a, t, k0, left, v);
+                u32x4_t part[3];
+                split_bf16(v, part);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    u32x4_t w{0u, 0u, 0u, 0u};
+                    if (QT && left >= 8) {
+                        w = *reinterpret_cast<const u32x4_el2_t *>(q + col[j] * a.ldq + k0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < left) w[e / 2] |= uint32_t(QT ? q[col[j] * a.ldq + k0 + e] : q[(k0 + e) * a.ldq + col[j]]) << (16 * (e & 1));
+                    }
+                    if (exact) sum[j] = mfma32<DT_BF16>(part[2], w, sum[j]);
+                    sum[j] = mfma32<DT_BF16>(part[1], w, sum[j]);
+                    sum[j] = mfma32<DT_BF16>(part[0], w, sum[j]);
+                }
+            }
+            const uint32_t mine = rows >> (4 * half);            // this lane's rows: 8 (e / 4) + 4 half + e % 4
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[I][j][e] += (mine >> (8 * (e >> 2) + (e & 3))) & 1u ? sum[j][e] : 0.0f;
+        }
+    });
+}
+
+}  // namespace gemm

@@ -1,0 +1,66 @@
+// fused_plan.cpp -- how the fused products choose their tile and K slices (host).
+#include "fused.h"
+
+namespace gemm {
+
+const FusedConfig kFusedConfigs[] = {
+    {64, 128, 4, 2, "fused_64x128_2x2"},
+};
+const int32_t kFusedNumConfigs = sizeof(kFusedConfigs) / sizeof(kFusedConfigs[0]);
+
+namespace {
+
+constexpr int kCUs = 256;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
+    if (config < 0 || config >= kFusedNumConfigs || !fused_has(op, config)) return false;
+    const FusedConfig &c = kFusedConfigs[config];
+    const int64_t stages = ceil_div(K, 64) * (op == FUSED_DX ? 2 : 1);
+    const int64_t chunk = stages > 0 ? ceil_div(stages, split) : 1;
+    out->config = config;
+    out->k_chunk = 64 * chunk;
+    out->split_k = int32_t(stages > 0 ? ceil_div(stages, chunk) : 1);
+    // A tile's partial sums are addressed with 32 bits, and a grid holds fewer than 2^32 threads.
+    const int64_t tiles = ceil_div(M, c.bm) * pairs * ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn);
+    return int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && tiles <= UINT32_MAX / (64 * c.waves) / out->split_k;
+}
+
+// Modelled microseconds of a plan, without the launch.
+double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t, const FusedPlan &p) {
+    const FusedConfig &c = kFusedConfigs[p.config];
+    const double tiles = double(ceil_div(M, c.bm)) * pairs * double(ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn));
+    const double groups = tiles * p.split_k, rounds = double(int64_t(groups / (kCUs * c.occupancy)) + 1);
+    return rounds * (2.0 + 0.4 * double(p.k_chunk) / 64) + (p.split_k > 1 ? 3.0 + 0.2 * p.split_k : 0.0);
+}
+
+}  // namespace
+
+bool fused_has(FusedOp op, int32_t config) { return op >= 0 && op < FUSED_OPS && config >= 0 && config < kFusedNumConfigs; }
+
+bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
+    if (config >= 0) return evaluate(op, pairs, M, N, K, config, split > 0 ? split : 1, out);
+    static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
+    double best = 0;
+    bool found = false;
+    for (int32_t c = 0; c < kFusedNumConfigs; ++c) {
+        int32_t seen = 0;
+        for (const int32_t s : kSplits) {
+            FusedPlan p;
+            if (!evaluate(op, pairs, M, N, K, c, split > 0 ? split : s, &p)) break;
+            if (p.split_k == seen) continue;                     // the same slices again
+            seen = p.split_k;
+            const double t = modelled_us(op, pairs, M, N, K, p);
+            if (!found || t < best) {
+                best = t;
+                *out = p;
+                found = true;
+            }
+            if (split > 0) break;
+        }
+    }
+    return found;
+}
+
+}  // namespace gemm

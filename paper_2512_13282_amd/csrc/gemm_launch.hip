@@ -165,6 +165,21 @@ int acquire_workspace(void *stream_ptr, size_t partial_bytes, int64_t counter_wo
     return LAUNCH_OK;
 }
 
+int acquire_counted(void *stream_ptr, size_t partial_bytes, int64_t counter_words, void **partials, uint32_t **counters,
+                    WorkspaceHold &hold) {
+    int rc = acquire_workspace(stream_ptr, partial_bytes, counter_words, partials, counters, hold);
+    if (rc != LAUNCH_NO_COUNTERS) return rc;
+    const size_t at = (partial_bytes + 255) / 256 * 256;
+    uint32_t *none = nullptr;
+    rc = acquire_workspace(stream_ptr, at + size_t(counter_words) * 4, 0, partials, &none, hold);
+    if (rc != LAUNCH_OK) return rc;
+    *counters = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(*partials) + at);
+    const int64_t blocks = (counter_words + 255) / 256;
+    hipLaunchKernelGGL(zero_u32_kernel, dim3(unsigned(blocks < 1024 ? blocks : 1024)), dim3(256), 0,
+                       static_cast<hipStream_t>(stream_ptr), *counters, counter_words);
+    return hipGetLastError() == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
+}
+
 int release_workspaces() {
     std::lock_guard<std::mutex> lk(g_ws_mu);
     int cur = 0;

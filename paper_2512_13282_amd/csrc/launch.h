@@ -76,6 +76,11 @@ using WorkspaceHold = std::unique_lock<std::mutex>;
 int acquire_workspace(void *stream, size_t partial_bytes, int64_t counter_words, void **partials, uint32_t **counters,
                       WorkspaceHold &hold);
 
+// The same for calls whose sums over K slices need counters in a capture too: where the stream holds too few
+// to lend, they follow the scratch in memory of their own, zeroed by a kernel of the capture.
+int acquire_counted(void *stream, size_t partial_bytes, int64_t counter_words, void **partials, uint32_t **counters,
+                    WorkspaceHold &hold);
+
 // Frees every cached split-K workspace (all devices and streams) after
 // synchronising each device that holds one.
 int release_workspaces();

@@ -4,15 +4,7 @@
 
 namespace gemm {
 
-// Rows of `used` bytes at any address and stride, copied to rows of `pitch` bytes (a multiple
-// of 16) on 16-byte addresses, zeros behind each row: what the tile kernels load straight into
-// LDS, 16 aligned bytes at a time.  Both operands in one launch, for the launch is what the
-// smaller copies cost.
-struct MxCopy {
-    const uint8_t *src;
-    uint8_t *dst;
-    int64_t stride, used, pitch, rows;     // rows 0: nothing to copy
-};
+// The copies that MxCopy describes, both in one launch, for the launch is what the smaller ones cost.
 __global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
     const int64_t x_total = x.rows * (x.pitch / 16), total = x_total + y.rows * (y.pitch / 16), step = int64_t(gridDim.x) * 256;
     for (int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x; id < total; id += step) {
@@ -33,14 +25,11 @@ __global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
     }
 }
 
-namespace {
-bool realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
+bool mx_realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
     const int64_t n = (x.rows * (x.pitch / 16) + y.rows * (y.pitch / 16) + 255) / 256;
     hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream, x, y);
     return hipGetLastError() == hipSuccess;
 }
-
-}  // namespace
 
 int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_ptr) {
     hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
@@ -96,12 +85,12 @@ int launch_mx_gemm(const MxArgs &a0, MxOp op, const MxPlan &plan, void *stream_p
             a.g.B = y.dst;
             a.g.ldb = y.pitch;
         }
-        if ((copy_a || copy_b) && !realign(x, y, stream)) return LAUNCH_HIP_ERROR;
+        if ((copy_a || copy_b) && !mx_realign(x, y, stream)) return LAUNCH_HIP_ERROR;
         if (copy_s) {
             x = MxCopy{a.scales, copies + a_bytes + b_bytes, a.ld_scales, s_used, s_row, b_rows};
             a.scales = x.dst;
             a.ld_scales = x.pitch;
-            if (!realign(x, MxCopy{}, stream)) return LAUNCH_HIP_ERROR;
+            if (!mx_realign(x, MxCopy{}, stream)) return LAUNCH_HIP_ERROR;
         }
     }
     hipError_t e = op == MX_FWD ? launch_mx_fwd(plan.config, a, grid, stream)
