@@ -50,6 +50,7 @@ struct FusedConfig {
     int32_t bm, bn;                  // output tile; GATED: bn / 2 columns of each product
     int32_t waves;                   // per workgroup
     int32_t occupancy;               // workgroups that a compute unit holds
+    int32_t most_slices;
     const char *name;
 };
 extern const FusedConfig kFusedConfigs[];

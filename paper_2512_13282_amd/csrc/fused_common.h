@@ -233,31 +233,40 @@ __device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
+    // The sums stay in their registers: several slices of a small tile are on the way at once, a slice of a large one
+    // in parts.
     auto add = [&](int s, auto n_c) __attribute__((always_inline)) {
-        constexpr int COUNT = decltype(n_c)::value;
-        f32x4_t v[COUNT][TM][TN][4];
+        constexpr int COUNT = decltype(n_c)::value, ROWS = TM * TN > 4 ? 1 : TM;
+        static_for<0, (TM + ROWS - 1) / ROWS>([&](auto b_c) __attribute__((always_inline)) {
+            constexpr int I0 = decltype(b_c)::value * ROWS, I1 = I0 + ROWS < TM ? I0 + ROWS : TM;
+            f32x4_t v[COUNT][ROWS][TN][4];
 #pragma unroll
-        for (int u = 0; u < COUNT; ++u)
+            for (int u = 0; u < COUNT; ++u)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = I0; i < I1; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+                    for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[u][i][j][q] = mx_load_part(parts, 32 * i + 8 * q < rows ? at(s + u, i, j, q) : kOOB);
+                        for (int q = 0; q < 4; ++q)
+                            v[u][i - I0][j][q] = mx_load_part(parts, 32 * i + 8 * q < rows ? at(s + u, i, j, q) : kOOB);
 #pragma unroll
-        for (int u = 0; u < COUNT; ++u)
+            for (int u = 0; u < COUNT; ++u)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = I0; i < I1; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+                    for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                        for (int q = 0; q < 4; ++q)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[u][i][j][q][e];
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[u][i - I0][j][q][e];
+            if constexpr (TM * TN > 4) __builtin_amdgcn_sched_barrier(0);
+        });
     };
     constexpr int G = TM * TN >= 4 ? 1 : 4 / (TM * TN);        // slices on the way at once
     int s = 0;
+#pragma unroll 1
     for (; s + G <= g.split_k; s += G) add(s, std::integral_constant<int, G>{});
+#pragma unroll 1
     for (; s < g.split_k; ++s) add(s, std::integral_constant<int, 1>{});
     mx_reset_counter(g, tile);
     return true;

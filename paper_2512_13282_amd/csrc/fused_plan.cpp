@@ -4,7 +4,10 @@
 namespace gemm {
 
 const FusedConfig kFusedConfigs[] = {
-    {64, 128, 4, 2, "fused_64x128_2x2"},
+    {64, 128, 4, 2, 4096, "fused_64x128_2x2"},
+    {128, 256, 8, 1, 4096, "fused_pingpong_128x256"},
+    {192, 256, 8, 1, 4096, "fused_pingpong_192x256"},
+    {256, 256, 8, 1, 1, "fused_pingpong_256x256"},
 };
 const int32_t kFusedNumConfigs = sizeof(kFusedConfigs) / sizeof(kFusedConfigs[0]);
 
@@ -17,6 +20,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
     if (config < 0 || config >= kFusedNumConfigs || !fused_has(op, config)) return false;
     const FusedConfig &c = kFusedConfigs[config];
+    if (split > c.most_slices) return false;
     const int64_t stages = ceil_div(K, 64) * (op == FUSED_DX ? 2 : 1);
     const int64_t chunk = stages > 0 ? ceil_div(stages, split) : 1;
     out->config = config;
