@@ -19,9 +19,12 @@ struct ShrinkArgs {
     bool qt;
     float *h;                    // the caller's (M x r), or null: the workspace's
     float *out;                  // where the kernel writes: planes of M x r
+    uint32_t *counters;          // of the token blocks and rank groups: the slices are added up into h; or null
     int64_t plane;
-    int32_t slices;              // of L, a plane each
+    int32_t slices;              // of L, a plane each, at most 8
+    int32_t blocks, groups;      // of tokens and of ranks
     int64_t chunk;               // L of a slice, a multiple of 32
+    int32_t parts;               // workgroups that share the adapters of a block
 };
 
 struct AdapterDwArgs {

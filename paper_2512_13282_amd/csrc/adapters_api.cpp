@@ -52,7 +52,8 @@ int product(int op, int64_t M, int64_t N, int64_t K, const uint16_t *X, int64_t 
     if (N > 0) {
         const int planned = gemm::fused_plan_for(fused, 1, M, N, K, g_forced[op], &plan);
         if (planned != GEMM_OK) return planned;
-        if (!gemm::fused_copyable(X, ldx, M, K, true) || !gemm::fused_copyable(W, ldw, forward ? N : K, forward ? K : N, forward))
+        if (!gemm::fused_any_address(plan.config) &&
+            (!gemm::fused_copyable(X, ldx, M, K, true) || !gemm::fused_copyable(W, ldw, forward ? N : K, forward ? K : N, forward)))
             return GEMM_ERR_UNSUPPORTED;
     }
     a.g.dtype = GEMM_DTYPE_BF16_F32;

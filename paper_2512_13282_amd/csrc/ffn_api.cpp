@@ -41,9 +41,9 @@ int launch(int op, FusedArgs &a, int64_t M, int64_t N, int64_t K, bool bf16_out,
     gemm::FusedPlan plan;
     const int planned = gemm::fused_plan_for(kOps[op], kPairs[op], M, N, K, g_forced[op], &plan);
     if (planned != GEMM_OK) return planned;
-    if (!gemm::fused_copyable(a.g.A, a.g.lda, a_rows, a_cols, !at) || !gemm::fused_copyable(a.g.B, a.g.ldb, b_rows, b_cols, bt) ||
+    if (!gemm::fused_any_address(plan.config) && (!gemm::fused_copyable(a.g.A, a.g.lda, a_rows, a_cols, !at) || !gemm::fused_copyable(a.g.B, a.g.ldb, b_rows, b_cols, bt) ||
         (a.A2 != nullptr && !gemm::fused_copyable(a.A2, a.lda2, a_rows, a_cols, !at)) ||
-        (a.B2 != nullptr && !gemm::fused_copyable(a.B2, a.ldb2, b_rows, b_cols, bt)))
+        (a.B2 != nullptr && !gemm::fused_copyable(a.B2, a.ldb2, b_rows, b_cols, bt))))
         return GEMM_ERR_UNSUPPORTED;
     a.g.dtype = GEMM_DTYPE_BF16_F32;
     a.g.M = M;

@@ -56,6 +56,12 @@ struct FusedConfig {
 extern const FusedConfig kFusedConfigs[];
 extern const int32_t kFusedNumConfigs;
 
+// The kernels for few rows of A, by rows: the one that takes its operands as they lie, and the one for operands on
+// 16-byte rows.
+constexpr int32_t kFusedDecode = 4, kFusedStream = 8;
+inline bool fused_few_rows(int32_t config) { return config >= kFusedDecode; }
+inline bool fused_any_address(int32_t config) { return config >= kFusedDecode && config < kFusedStream; }
+
 // Whether a configuration is built for an operator.
 bool fused_has(FusedOp op, int32_t config);
 

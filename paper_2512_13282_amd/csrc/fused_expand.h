@@ -8,6 +8,19 @@ namespace gemm {
 typedef float f32x4_el_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned u32x4_el2_t __attribute__((ext_vector_type(4), aligned(2)));
 
+// Eight bf16 values at any address, the first `left` of them, zeros after them.
+__device__ __forceinline__ u32x4_t load8_bf16(const uint16_t *p, int64_t left) {
+    u32x4_t v{0u, 0u, 0u, 0u};
+    if (left >= 8) {
+        v = *reinterpret_cast<const u32x4_el2_t *>(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) v[e / 2] |= uint32_t(p[e]) << (16 * (e & 1));
+    }
+    return v;
+}
+
 // Eight floats as bf16 parts whose sum they are: the upper 8 bits of each, the next 8, and the last 8 (24 bits
 // in all, so three parts are exact and two leave 2^-16).  An infinity or a NaN is its own first part.
 __device__ __forceinline__ void split_bf16(const float (&v)[8], u32x4_t (&part)[3]) {
@@ -49,6 +62,24 @@ __device__ __forceinline__ void load_h(const FusedArgs &a, int64_t t, int k, int
     }
 }
 
+// Eight bf16 values at any address, all of them inside the matrix.  ODD: the address may be off a dword, where a
+// 16-byte load takes 2.4 times as long (gated 37 x 2048 x 2049 against x 2050: 23.3 and 9.8 us): dwords from the
+// one that holds the first value, and one more, put together.
+template <bool ODD>
+__device__ __forceinline__ u32x4_t load8_any(const uint16_t *p) {
+    if constexpr (!ODD) {
+        return *reinterpret_cast<const u32x4_el2_t *>(p);
+    } else {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        const uint32_t *const q = reinterpret_cast<const uint32_t *>(at & ~uintptr_t(3));
+        const uint32_t shift = uint32_t(at & 2) * 8;
+        const u32x4_t v = *reinterpret_cast<const u32x4_el_t *>(q);
+        const uint32_t last = q[shift ? 4 : 3];
+        return u32x4_t{__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift),
+                       __builtin_amdgcn_alignbit(v[3], v[2], shift), __builtin_amdgcn_alignbit(last, v[3], shift)};
+    }
+}
+
 // ---------------------------------------------------------------------------
 // acc += h_t Q_i(t) for the wave's rows (TM x 32 from r0) and columns (32 from c0 and 32 from c0 + HALF).  QT: Q_i
 // is N x r, else r x N.
@@ -56,9 +87,11 @@ __device__ __forceinline__ void load_h(const FusedArgs &a, int64_t t, int k, int
 // The adapters that occur among a fragment's 32 rows are taken one after the other (most fragments of a prompt hold
 // one, and a decode batch's rows of weights have to be read for each of its requests anyway), each as
 // a product of all 32 rows, of which only the adapter's own take the result: rows are chosen, not multiplied
-// by zeros, so an infinity or a NaN in one request's adapter stays out of the others'.  h keeps
-// its fp32 value in two bf16 parts (2^-16 left out, a bf16 result's half step being 2^-9), three and so all of it
-// for an fp32 result.  Runs ahead of the K loop, while the first stages are on their way.
+// by zeros, so an infinity or a NaN in one request's adapter stays out of the others'.  h does not depend on the
+// adapter and is read once for every 16 ranks; the matrices of four adapters are on their way at once, for what
+// a batch of many requests waits for is their latency.  h keeps its fp32 value in two bf16 parts (2^-16 left
+// out, a bf16 result's half step being 2^-9), three and so all of it for an fp32 result.  Runs ahead of the
+// K loop, while the first stages are on their way.
 // ---------------------------------------------------------------------------
 template <bool QT, int HALF, int TM, int TN>
 __device__ __forceinline__ void expand_adapters(const FusedArgs &a, f32x16_t (&acc)[TM][TN], int64_t r0, int64_t c0, int lane) {
@@ -77,41 +110,54 @@ __device__ __forceinline__ void expand_adapters(const FusedArgs &a, f32x16_t (&a
         const int64_t t = r0 + 32 * I + l32;
         const int own = t < a.g.M ? a.index[t] : -1;
         const bool has = uint32_t(own) < uint32_t(a.n);
-        uint32_t pending = uint32_t(__ballot(has));
-        while (pending != 0u) {
-            const int cur = __builtin_amdgcn_readlane(own, __builtin_ctz(pending));
-            const uint32_t rows = uint32_t(__ballot(has && own == cur));
-            pending &= ~rows;
-            const uint16_t *const q = static_cast<const uint16_t *>(a.Q) + cur * a.sq;
-            f32x16_t sum[TN];
+        const uint32_t all = uint32_t(__ballot(has));
+        if (all == 0u) return;
+        for (int k = 0; k < a.r; k += 16) {
+            const int k0 = k + 8 * half, left = a.r - k0;
+            float v[8] = {};
+            if (has) load_h(a, t, k0, left, v);
+            u32x4_t part[3];
+            split_bf16(v, part);
+            constexpr int B = 4;                                 // adapters on the way at once
+            uint32_t pending = all;
+            while (pending != 0u) {
+                u32x4_t w[B][TN];
+                uint32_t rows[B];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) sum[j] = f32x16_t{};
-            for (int k = 0; k < a.r; k += 16) {
-                const int k0 = k + 8 * half, left = a.r - k0;
-                float v[8] = {};
-                if (has) load_h(a, t, k0, left, v);
-                u32x4_t part[3];
-                split_bf16(v, part);
+                for (int b = 0; b < B; ++b) {
+                    rows[b] = 0u;
+                    if (pending == 0u) continue;
+                    const int cur = __builtin_amdgcn_readlane(own, __builtin_ctz(pending));
+                    rows[b] = uint32_t(__ballot(has && own == cur));
+                    pending &= ~rows[b];
+                    const uint16_t *const q = static_cast<const uint16_t *>(a.Q) + cur * a.sq;
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    u32x4_t w{0u, 0u, 0u, 0u};
-                    if (QT && left >= 8) {
-                        w = *reinterpret_cast<const u32x4_el2_t *>(q + col[j] * a.ldq + k0);
-                    } else {
+                    for (int j = 0; j < TN; ++j) {
+                        if (QT) {
+                            w[b][j] = load8_bf16(q + col[j] * a.ldq + k0, left);
+                        } else {
+                            w[b][j] = u32x4_t{0u, 0u, 0u, 0u};
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e < left) w[e / 2] |= uint32_t(QT ? q[col[j] * a.ldq + k0 + e] : q[(k0 + e) * a.ldq + col[j]]) << (16 * (e & 1));
+                            for (int e = 0; e < 8; ++e)
+                                if (e < left) w[b][j][e / 2] |= uint32_t(q[(k0 + e) * a.ldq + col[j]]) << (16 * (e & 1));
+                        }
                     }
-                    if (exact) sum[j] = mfma32<DT_BF16>(part[2], w, sum[j]);
-                    sum[j] = mfma32<DT_BF16>(part[1], w, sum[j]);
-                    sum[j] = mfma32<DT_BF16>(part[0], w, sum[j]);
+                }
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    if (rows[b] == 0u) continue;
+                    const uint32_t mine = rows[b] >> (4 * half); // this lane's rows: 8 (e / 4) + 4 half + e % 4
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        f32x16_t sum{};
+                        if (exact) sum = mfma32<DT_BF16>(part[2], w[b][j], sum);
+                        sum = mfma32<DT_BF16>(part[1], w[b][j], sum);
+                        sum = mfma32<DT_BF16>(part[0], w[b][j], sum);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[I][j][e] += (mine >> (8 * (e >> 2) + (e & 3))) & 1u ? sum[e] : 0.0f;
+                    }
                 }
             }
-            const uint32_t mine = rows >> (4 * half);            // this lane's rows: 8 (e / 4) + 4 half + e % 4
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[I][j][e] += (mine >> (8 * (e >> 2) + (e & 3))) & 1u ? sum[j][e] : 0.0f;
         }
     });
 }

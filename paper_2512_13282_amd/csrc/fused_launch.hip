@@ -10,13 +10,24 @@ namespace {
 
 int64_t up16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
+// Tokens and ranks of a block (in sixteens).
+int shrink_rt(const ShrinkArgs &s) { return s.r <= 16 ? 1 : s.r <= 32 ? 2 : 4; }
+int shrink_mt(const ShrinkArgs &s) { return s.M <= 64 ? 1 : s.M <= 1024 || shrink_rt(s) == 4 ? 2 : 4; }
+
+template <bool QT, int MT>
+void queue_shrink_rows(const ShrinkArgs &s, dim3 grid, hipStream_t stream) {
+    const int rt = shrink_rt(s);
+    if (rt == 1) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 1, 8>), grid, dim3(512), 0, stream, s);
+    else if (rt == 2) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 2, 8>), grid, dim3(512), 0, stream, s);
+    else if constexpr (MT < 4) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 4, 8>), grid, dim3(512), 0, stream, s);
+}
 template <bool QT>
 hipError_t queue_shrink(const ShrinkArgs &s, hipStream_t stream) {
-    const int rt = s.r <= 16 ? 1 : s.r <= 32 ? 2 : 4;
-    const dim3 grid(unsigned((s.M + 15) / 16), unsigned(s.slices), unsigned((s.r + 16 * rt - 1) / (16 * rt)));
-    if (rt == 1) hipLaunchKernelGGL((adapters_shrink_kernel<QT, 1, 1, 8>), grid, dim3(512), 0, stream, s);
-    else if (rt == 2) hipLaunchKernelGGL((adapters_shrink_kernel<QT, 1, 2, 8>), grid, dim3(512), 0, stream, s);
-    else hipLaunchKernelGGL((adapters_shrink_kernel<QT, 1, 4, 8>), grid, dim3(512), 0, stream, s);
+    const dim3 grid(unsigned(s.blocks * s.parts), unsigned(s.slices), unsigned(s.groups));
+    const int mt = shrink_mt(s);
+    if (mt == 1) queue_shrink_rows<QT, 1>(s, grid, stream);
+    else if (mt == 2) queue_shrink_rows<QT, 2>(s, grid, stream);
+    else queue_shrink_rows<QT, 4>(s, grid, stream);
     return hipGetLastError();
 }
 
@@ -27,6 +38,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     FusedArgs a = a0;
     const FusedConfig &c = kFusedConfigs[plan.config];
     const int64_t cols = op == FUSED_GATED ? c.bn / 2 : c.bn;
+    const bool any = fused_any_address(plan.config);
     const int64_t tm = (a.g.M + c.bm - 1) / c.bm * (op == FUSED_DW ? a.pairs : 1), tn = (a.g.N + cols - 1) / cols;
     const int64_t grid = tm * tn * plan.split_k;
     a.g.k_chunk = plan.k_chunk;
@@ -49,16 +61,20 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     bool copy[4];
     for (int i = 0; i < 4; ++i) {
         const Operand &o = operands[i];
-        copy[i] = o.rows > 0 && o.cols > 0 && !fused_loadable(*o.p, *o.ld, o.along_k, o.cols);
+        copy[i] = !any && o.rows > 0 && o.cols > 0 && !fused_loadable(*o.p, *o.ld, o.along_k, o.cols);
         if (copy[i]) copied += o.rows * up16(2 * o.cols);
     }
-    const int64_t planes = shrink != nullptr && (shrink->h == nullptr || shrink->slices > 1) ? up16(shrink->slices * shrink->plane * 4) : 0;
+    // The kernels for few rows add h's planes up themselves; elsewhere and where the caller keeps h the slices meet in it.
+    const bool sum_h = shrink != nullptr && shrink->slices > 1 && (shrink->h != nullptr || !fused_few_rows(plan.config));
+    const bool own_h = shrink != nullptr && shrink->h == nullptr && sum_h;
+    const int64_t planes = shrink == nullptr || (shrink->h != nullptr && shrink->slices == 1) ? 0 : up16((shrink->slices + (own_h ? 1 : 0)) * shrink->plane * 4);
+    const int64_t counted = (a.g.split_k > 1 ? tm * tn : 0), h_counted = sum_h ? int64_t(shrink->blocks) * shrink->groups : 0;
 
     WorkspaceHold hold;                  // over the copies, the adapters' first product and the product
     if (partial + copied + planes > 0) {
         void *ws = nullptr;
         uint32_t *counters = nullptr;
-        const int rc = acquire_counted(stream_ptr, size_t(partial + copied + planes), a.g.split_k > 1 ? tm * tn : 0, &ws, &counters, hold);
+        const int rc = acquire_counted(stream_ptr, size_t(partial + copied + planes), counted + h_counted, &ws, &counters, hold);
         if (rc != LAUNCH_OK) return rc;
         a.g.workspace = ws;
         a.g.counters = counters;
@@ -80,19 +96,13 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     if (shrink != nullptr) {
         ShrinkArgs s = *shrink;
         float *const own = reinterpret_cast<float *>(static_cast<uint8_t *>(a.g.workspace) + partial);
-        s.out = s.h != nullptr && s.slices == 1 ? s.h : own;
+        s.out = planes > 0 ? own : s.h;
+        if (own_h) s.h = own + s.slices * s.plane;
+        s.counters = sum_h ? a.g.counters + counted : nullptr;
         if ((s.qt ? queue_shrink<true>(s, stream) : queue_shrink<false>(s, stream)) != hipSuccess) return LAUNCH_HIP_ERROR;
-        a.h = s.out;
+        a.h = sum_h ? s.h : s.out;
         a.h_plane = s.plane;
-        a.planes = s.slices;
-        if (s.h != nullptr && s.slices > 1) {
-            const int64_t total = s.M * s.r, blocks = (total + 255) / 256;
-            hipLaunchKernelGGL(adapters_sum_kernel, dim3(unsigned(blocks < 1024 ? blocks : 1024)), dim3(256), 0, stream, own, s.plane,
-                               s.slices, s.h, total);
-            if (hipGetLastError() != hipSuccess) return LAUNCH_HIP_ERROR;
-            a.h = s.h;
-            a.planes = 1;
-        }
+        a.planes = sum_h ? 1 : s.slices;
     }
     if (grid == 0) return LAUNCH_OK;      // h alone
     hipError_t e = hipErrorInvalidValue;
@@ -114,13 +124,20 @@ int launch_adapters(const FusedArgs &a, FusedOp op, const FusedPlan &plan, const
     if (s0.r == 0 || (s0.n == 0 && s0.h == nullptr)) return launch_fused_with(a, op, plan, nullptr, stream);
     ShrinkArgs s = s0;
     if (s.n == 0) s.L = 0;               // zeros
-    // Slices of at least 256 until the compute units have a workgroup each; every reader of h adds the planes up.
-    const int rt = s.r <= 16 ? 1 : s.r <= 32 ? 2 : 4;
-    const int64_t groups = (s.M + 15) / 16 * ((s.r + 16 * rt - 1) / (16 * rt));
-    int64_t slices = 256 / groups, most = (s.L + 255) / 256;
-    if (slices > most) slices = most;
+    // Slices of at least 512 of L until every compute unit has a workgroup; then the adapters of a block apart, of which
+    // few tokens have one each and many most often one.
+    s.blocks = int32_t((s.M + 16 * shrink_mt(s) - 1) / (16 * shrink_mt(s)));
+    s.groups = (s.r + 16 * shrink_rt(s) - 1) / (16 * shrink_rt(s));
+    const int64_t wanted = 256 / (int64_t(s.blocks) * s.groups), most = (s.L + 511) / 512;
+    int64_t slices = wanted < most ? wanted : most;
     if (slices > 8) slices = 8;
     if (slices < 1) slices = 1;
+    int64_t parts = 2 * wanted / slices;
+    if (parts > s.M) parts = s.M;
+    if (parts > s.n) parts = s.n;
+    if (parts > 16) parts = 16;
+    if (parts < 1) parts = 1;
+    s.parts = int32_t(parts);
     s.chunk = s.L > 0 ? ((s.L + slices - 1) / slices + 31) / 32 * 32 : 32;
     s.slices = int32_t(s.L > 0 ? (s.L + s.chunk - 1) / s.chunk : 1);
     s.plane = s.M * s.r;

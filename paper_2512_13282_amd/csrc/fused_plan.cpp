@@ -8,6 +8,12 @@ const FusedConfig kFusedConfigs[] = {
     {128, 256, 8, 1, 4096, "fused_pingpong_128x256"},
     {192, 256, 8, 1, 4096, "fused_pingpong_192x256"},
     {256, 256, 8, 1, 1, "fused_pingpong_256x256"},
+    {16, 16, 8, 2, 1, "fused_decode_16"},
+    {32, 16, 8, 2, 1, "fused_decode_32"},
+    {48, 16, 8, 2, 1, "fused_decode_48"},
+    {64, 16, 8, 2, 1, "fused_decode_64"},
+    {16, 16, 8, 1, 1, "fused_stream_16"},
+    {32, 16, 8, 1, 1, "fused_stream_32"},
 };
 const int32_t kFusedNumConfigs = sizeof(kFusedConfigs) / sizeof(kFusedConfigs[0]);
 
@@ -20,7 +26,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
     if (config < 0 || config >= kFusedNumConfigs || !fused_has(op, config)) return false;
     const FusedConfig &c = kFusedConfigs[config];
-    if (split > c.most_slices) return false;
+    if (split > c.most_slices || (fused_few_rows(config) && M > c.bm)) return false;
     const int64_t stages = ceil_div(K, 64) * (op == FUSED_DX ? 2 : 1);
     const int64_t chunk = stages > 0 ? ceil_div(stages, split) : 1;
     out->config = config;
@@ -41,7 +47,10 @@ double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t, con
 
 }  // namespace
 
-bool fused_has(FusedOp op, int32_t config) { return op >= 0 && op < FUSED_OPS && config >= 0 && config < kFusedNumConfigs; }
+bool fused_has(FusedOp op, int32_t config) {
+    if (op < 0 || op >= FUSED_OPS || config < 0 || config >= kFusedNumConfigs) return false;
+    return !fused_few_rows(config) || op == FUSED_GATED || op == FUSED_ADAPT;
+}
 
 bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
     if (config >= 0) return evaluate(op, pairs, M, N, K, config, split > 0 ? split : 1, out);

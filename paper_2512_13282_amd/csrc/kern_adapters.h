@@ -7,38 +7,36 @@
 
 namespace gemm {
 
-// Eight bf16 values at any address, the first `left` of them, zeros after them.
-__device__ __forceinline__ u32x4_t load8_bf16(const uint16_t *p, int64_t left) {
-    u32x4_t v{0u, 0u, 0u, 0u};
-    if (left >= 8) {
-        v = *reinterpret_cast<const u32x4_el2_t *>(p);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) v[e / 2] |= uint32_t(p[e]) << (16 * (e & 1));
-    }
-    return v;
-}
-
 // ---------------------------------------------------------------------------
 // h of 16 MT tokens and 16 RT ranks over a slice of L, KW waves with a part of the slice each (16 x 16 x 32 MFMAs, Q the
-// first operand: output register e of lane l is rank 4 (l / 16) + e of token l % 16).  Both operands go from memory to
-// registers, for every element is used by one wave alone.  The adapters that occur among the tokens are taken one after
-// the other over all rows, of which the adapter's own are written; the others' results are dropped.
-// Slices leave planes that whoever reads h adds up in their order.
+// first operand: output register e of lane l is rank 4 (l / 16) + e of token l % 16).  Every element is used by
+// one wave alone, so P, and Q where its rows lie along L, go from memory to registers, U chunks of 32 on the way; a Q
+// that lies across passes through LDS of the wave's own and is read back transposed.  The adapters that occur among the
+// tokens are taken one after the other over all rows, of which the adapter's own are written; the others' results are
+// dropped.  `parts` workgroups share the adapters of the same tokens, in turn.
+//
+// Slices leave planes.  Where `counters` is set the one that arrives last adds them up in their order (mx_common.h says
+// how the accesses are ordered), else whoever reads h does.
 // ---------------------------------------------------------------------------
 template <bool QT, int MT, int RT, int KW>
 __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) {
-    __shared__ __attribute__((aligned(16))) f32x4_t part[KW][MT * RT][64];
+    constexpr int PITCH = 32 * RT, CPR = 2 * RT;                 // bytes and 16-byte pieces of a row of Q across L
+    __shared__ __attribute__((aligned(1024))) f32x4_t part[KW][MT * RT][64];
+    static_assert(sizeof(part[0]) >= 32 * PITCH, "a wave's chunk of Q and its sums take turns");
+    __shared__ int flag;
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int l16 = lane & 15, grp = lane >> 4;
-    const int64_t t0 = int64_t(blockIdx.x) * (16 * MT);
+    const int block = int(blockIdx.x) / s.parts;
+    const int64_t t0 = int64_t(block) * (16 * MT);
+    int turn = int(blockIdx.x) % s.parts;                        // adapters until this workgroup's next
+    const bool zeros = turn == 0;
     const int j0 = int(blockIdx.z) * (16 * RT);
     float *const out = s.out + int64_t(blockIdx.y) * s.plane;
 
     const int64_t l_begin = int64_t(blockIdx.y) * s.chunk, l_end = l_begin + s.chunk < s.L ? l_begin + s.chunk : s.L;
-    const int chunks = int((l_end - l_begin + 31) / 32), per = (chunks + KW - 1) / KW;
+    const int length = int(l_end - l_begin), chunks = (length + 31) / 32, whole = length / 32, per = (chunks + KW - 1) / KW;
     const int c0 = wave * per, c1 = c0 + per < chunks ? c0 + per : chunks;
+    const int n = (c1 < whole ? c1 : whole) - c0;                // whole chunks; <= 0 for a wave without any
 
     int own[MT];
     bool has[MT];
@@ -50,14 +48,28 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
         own[m] = s.n > 0 ? s.index[safe] : -1;
         has[m] = t < s.M && uint32_t(own[m]) < uint32_t(s.n);
         pending[m] = uint32_t(__ballot(has[m])) & 0xffffu;
-        row[m] = static_cast<const uint16_t *>(s.P) + safe * s.ldp + l_begin + 8 * grp;
-        if (t < s.M && !has[m] && wave == m % KW) {              // none: zeros
+        row[m] = static_cast<const uint16_t *>(s.P) + safe * s.ldp + l_begin + 32 * c0 + 8 * grp;
+    }
+    auto store = [&](int m, int j, int64_t t, f32x4_t v) __attribute__((always_inline)) {
+        float *const dst = out + t * s.r + j;
+        if (s.counters != nullptr) {
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int e = 0; e < 4; ++e)
+                if (j + e < s.r) store_coherent(dst + e, v[e]);
+        } else if (j + 4 <= s.r) {
+            *reinterpret_cast<f32x4_el_t *>(dst) = v;
+        } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j0 + 16 * rt + 4 * grp + e < s.r) out[t * s.r + j0 + 16 * rt + 4 * grp + e] = 0.0f;
+            for (int e = 0; e < 4; ++e)
+                if (j + e < s.r) dst[e] = v[e];
         }
+    };
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int64_t t = t0 + 16 * m + l16;
+        if (zeros && t < s.M && !has[m] && wave == m % KW)       // none: zeros
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) store(m, j0 + 16 * rt + 4 * grp, t, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
     }
     for (;;) {
         int cur = -1;
@@ -67,93 +79,133 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
         if (cur < 0) break;
 #pragma unroll
         for (int m = 0; m < MT; ++m) pending[m] &= ~uint32_t(__ballot(has[m] && own[m] == cur));
+        if (turn-- > 0) continue;
+        turn = s.parts - 1;
+        const float scale = s.scale != nullptr ? s.scale[cur] : 1.0f;
 
         const uint16_t *const q = static_cast<const uint16_t *>(s.Q) + cur * s.sq;
+        // Along L: rank l16 of tile rt.  Across: piece (lane % CPR) of row lane / CPR of each 64 / CPR rows.
         const uint16_t *qp[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const int j = j0 + 16 * rt + l16 < s.r ? j0 + 16 * rt + l16 : s.r - 1;      // past r: not written
-            qp[rt] = QT ? q + j * s.ldq + l_begin + 8 * grp : q + (l_begin + 8 * grp) * s.ldq + j;
+            if constexpr (QT) {
+                const int j = j0 + 16 * rt + l16 < s.r ? j0 + 16 * rt + l16 : s.r - 1;      // past r: not written
+                qp[rt] = q + j * s.ldq + l_begin + 32 * c0 + 8 * grp;
+            } else {
+                qp[rt] = q + (l_begin + 32 * c0 + rt * (64 / CPR) + lane / CPR) * s.ldq + j0 + 8 * (lane % CPR);
+            }
         }
+        const int ranks = s.r - j0 - 8 * (lane % CPR);           // of this lane's piece
+        uint8_t *const mine = reinterpret_cast<uint8_t *>(part[wave]);
+
         f32x4_t acc[MT][RT];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) acc[m][rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        auto load = [&](int c, u32x4_t (&x)[MT], u32x4_t (&w)[RT], int64_t left) __attribute__((always_inline)) {
+        constexpr int U = MT * RT >= 8 ? 2 : MT * RT >= 4 ? 3 : 4;
+        u32x4_t x[U][MT], w[U][RT];
+        // Chunk c of this wave; rows of L past `left` are zeros.
+        auto load = [&](int u, int c, bool all) __attribute__((always_inline)) {
+            const int left = length - 32 * (c0 + c);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) x[m] = load8_bf16(row[m] + 32 * c, left);
+            for (int m = 0; m < MT; ++m) x[u][m] = load8_bf16(row[m] + 32 * c, all ? 8 : left - 8 * grp);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                if constexpr (QT) {
-                    w[rt] = load8_bf16(qp[rt] + 32 * c, left);
-                } else {
-                    w[rt] = u32x4_t{0u, 0u, 0u, 0u};
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < left) w[rt][e / 2] |= uint32_t(qp[rt][(32 * c + e) * s.ldq]) << (16 * (e & 1));
-                }
+                if constexpr (QT) w[u][rt] = load8_bf16(qp[rt] + 32 * c, all ? 8 : left - 8 * grp);
+                else w[u][rt] = load8_bf16(qp[rt] + 32 * c * s.ldq, all || rt * (64 / CPR) + lane / CPR < left ? ranks : 0);
             }
         };
-        auto multiply = [&](const u32x4_t (&x)[MT], const u32x4_t (&w)[RT]) __attribute__((always_inline)) {
+        auto multiply = [&](int u) __attribute__((always_inline)) {
+            u32x4_t f[RT];
+            if constexpr (QT) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) f[rt] = w[u][rt];
+            } else {
+                auto swz_row = [](int r) { return RT == 4 ? ring_bswz<DT_BF16, 8>(r) : 0; };
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const int r = rt * (64 / CPR) + lane / CPR;
+                    *reinterpret_cast<u32x4_t *>(mine + r * PITCH + (((lane % CPR) ^ swz_row(r)) << 4)) = w[u][rt];
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // lanes read what others of the wave wrote
+                const int r = 8 * grp + (l16 >> 2);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const int colb = 32 * rt + 8 * (l16 & 3);
+                    const uint8_t *const p = mine + r * PITCH + ((((colb >> 4) ^ swz_row(r)) << 4) | (colb & 15));
+                    const u32x2_t lo = lds_read_tr<DT_BF16>(p), hi = lds_read_tr<DT_BF16>(p + 4 * PITCH);
+                    f[rt] = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) acc[m][rt] = mfma16_bf16(w[rt], x[m], acc[m][rt]);
+                for (int rt = 0; rt < RT; ++rt) acc[m][rt] = mfma16_bf16(f[rt], x[u][m], acc[m][rt]);
         };
-        constexpr int U = RT >= 4 ? 2 : 4;                       // chunks on the way at once
-        const int64_t mine = l_end - l_begin - 8 * grp;         // from this lane's first element on
-        int c = c0;
-        for (; c + U <= c1 && 32 * int64_t(c + U) <= l_end - l_begin; c += U) {
-            u32x4_t x[U][MT], w[U][RT];
 #pragma unroll
-            for (int u = 0; u < U; ++u) load(c + u, x[u], w[u], 8);
+        for (int u = 0; u < U; ++u)
+            if (u < n) load(u, u, true);
+        int i = 0;
+        for (; i + 2 * U <= n; i += U) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) multiply(x[u], w[u]);
+            for (int u = 0; u < U; ++u) {
+                multiply(u);
+                load(u, i + U + u, true);
+            }
         }
-        for (; c < c1; ++c) {
-            u32x4_t x[MT], w[RT];
-            load(c, x, w, mine - 32 * int64_t(c));
-            multiply(x, w);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u < n) multiply(u);
+            if (i + U + u < n) load(u, i + U + u, true);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + U + u < n) multiply(u);
+        if (chunks > whole && whole >= c0 && whole < c1) {       // the end of L that is no whole chunk
+            load(0, whole - c0, false);
+            multiply(0);
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) part[wave][m * RT + rt][lane] = acc[m][rt];
-        __syncthreads();
-        const float scale = s.scale != nullptr ? s.scale[cur] : 1.0f;
-        for (int i = wave; i < MT * RT; i += KW) {
-            f32x4_t sum = part[0][i][lane];
+        phase_barrier();
+        for (int k = wave; k < MT * RT; k += KW) {
+            f32x4_t sum = part[0][k][lane];
 #pragma unroll
-            for (int k = 1; k < KW; ++k) sum += part[k][i][lane];
-            const int m = i / RT, j = j0 + 16 * (i % RT) + 4 * grp;
-            const int64_t t = t0 + 16 * m + l16;
+            for (int v = 1; v < KW; ++v) sum += part[v][k][lane];
+            const int m = k / RT;
             bool take = false;
 #pragma unroll
             for (int v = 0; v < MT; ++v)
                 if (v == m) take = has[v] && own[v] == cur;
-            if (take) {
-                float *const dst = out + t * s.r + j;
-                if (j + 4 <= s.r) {
-                    *reinterpret_cast<f32x4_el_t *>(dst) = sum * scale;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (j + e < s.r) dst[e] = sum[e] * scale;
-                }
-            }
+            if (take) store(m, j0 + 16 * (k % RT) + 4 * grp, t0 + 16 * m + l16, sum * scale);
         }
-        __syncthreads();
+        phase_barrier();
     }
-}
-
-// h = the sum of its planes, where the caller keeps it.
-__global__ __launch_bounds__(256) void adapters_sum_kernel(const float *__restrict__ parts, int64_t plane, int slices, float *__restrict__ h, int64_t total) {
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-        float v = 0.0f;
-        for (int p = 0; p < slices; ++p) v += parts[p * plane + i];
-        h[i] = v;
+    if (s.counters == nullptr) return;
+    // The last of the block's slices and parts adds the planes up.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int counter = block * int(gridDim.z) + int(blockIdx.z);
+    if (threadIdx.x == 0)
+        flag = __hip_atomic_fetch_add(&s.counters[counter], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == unsigned(s.slices * s.parts - 1);
+    __syncthreads();
+    if (flag == 0) return;
+    const int rows = int(s.M - t0 < 16 * MT ? s.M - t0 : 16 * MT), ranks = s.r - j0 < 16 * RT ? s.r - j0 : 16 * RT;
+    for (int i = int(threadIdx.x); i < rows * ranks; i += 64 * KW) {
+        const int64_t at = (t0 + i / ranks) * s.r + j0 + i % ranks;
+        float v[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) v[p] = p < s.slices ? load_coherent(s.out + p * s.plane + at) : 0.0f;
+        float sum = v[0];
+#pragma unroll
+        for (int p = 1; p < 8; ++p) sum += v[p];
+        s.h[at] = sum;
     }
+    if (threadIdx.x == 0) __hip_atomic_store(&s.counters[counter], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // ---------------------------------------------------------------------------
