@@ -29,6 +29,7 @@ struct FusedArgs {
     int64_t ldg, ldu;
     int32_t act;                     // FFN_* of ffn_mi355x.h
     int32_t pairs;                   // DW: 1 or 2 matrices A
+    int32_t whole;                   // tiles with all of K, ahead of those cut into slices
     // ADAPT: row t's h is the sum over `planes` of h[plane][t][0 .. r), its adapter index[t] in [0, n), any other
     // value for none; adapter i's matrix starts sq elements after the one before it, rows ldq apart.
     const float *h;
@@ -43,6 +44,7 @@ struct FusedArgs {
 struct FusedPlan {
     int32_t config;
     int32_t split_k;
+    int32_t whole;                   // tiles with all of K, the rest are cut into slices
     int64_t k_chunk;                 // K of a slice, a multiple of 64 (DX: of both products' K one after the other)
 };
 

@@ -134,7 +134,7 @@ __device__ __forceinline__ void store_gated(const FusedArgs &a, const f32x16_t (
     });
 }
 
-// GRAD: the sums are dH; G and U are read where dG, dU and H are written, the next fragment's ahead of
+// GRAD: the sums are dH; G and U are read where dG, dU and H are written, the next fragments' ahead of
 // this one's stores.  Each result is rounded once, from G and U as they were kept.
 template <int ACT, int HALF, int TM, int TN>
 __device__ __forceinline__ void store_grad_as(const FusedArgs &a, const f32x16_t (&acc)[TM][TN], int64_t r0, int64_t c0, int lane) {
@@ -145,24 +145,25 @@ __device__ __forceinline__ void store_grad_as(const FusedArgs &a, const f32x16_t
     auto column = [&](int j) __attribute__((always_inline)) {
         return c0 + (lane & 28) + 32 * (j % (TN / 2)) + HALF * (j / (TN / 2));
     };
-    u32x2_t kept[2][4][2];
+    constexpr int AHEAD = TM * TN <= 4 ? TM * TN : TM * TN <= 6 ? 5 : 4;      // fragments of G and U on their way
+    u32x2_t kept[AHEAD][4][2];
     auto fetch = [&](auto f_c) __attribute__((always_inline)) {
         constexpr int F = decltype(f_c)::value, J = F / TM, I = F % TM;
         const int64_t col = column(J), left = a.g.N - col;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int dr = 32 * I + 8 * q;
-            kept[F % 2][q][0] = kept[F % 2][q][1] = u32x2_t{0u, 0u};
+            kept[F % AHEAD][q][0] = kept[F % AHEAD][q][1] = u32x2_t{0u, 0u};
             if (dr < rows_left) {
-                kept[F % 2][q][0] = load4_bf16(gs + (row0 + dr) * a.ldg + col, left);
-                kept[F % 2][q][1] = load4_bf16(us + (row0 + dr) * a.ldu + col, left);
+                kept[F % AHEAD][q][0] = load4_bf16(gs + (row0 + dr) * a.ldg + col, left);
+                kept[F % AHEAD][q][1] = load4_bf16(us + (row0 + dr) * a.ldu + col, left);
             }
         }
     };
-    fetch(std::integral_constant<int, 0>{});
+    static_for<0, AHEAD>([&](auto f_c) __attribute__((always_inline)) { fetch(f_c); });
+    __builtin_amdgcn_sched_barrier(0);
     static_for<0, TM * TN>([&](auto f_c) __attribute__((always_inline)) {
         constexpr int F = decltype(f_c)::value, J = F / TM, I = F % TM;
-        if constexpr (F + 1 < TM * TN) fetch(std::integral_constant<int, F + 1>{});
         const int64_t col = column(J), left = a.g.N - col;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -177,8 +178,8 @@ __device__ __forceinline__ void store_grad_as(const FusedArgs &a, const f32x16_t
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float d = __builtin_bit_cast(float, x[k]);
-                const float g = bf16_to_f32((kept[F % 2][q][0][k / 2] >> (16 * (k & 1))) & 0xffffu);
-                const float u = bf16_to_f32((kept[F % 2][q][1][k / 2] >> (16 * (k & 1))) & 0xffffu);
+                const float g = bf16_to_f32((kept[F % AHEAD][q][0][k / 2] >> (16 * (k & 1))) & 0xffffu);
+                const float u = bf16_to_f32((kept[F % AHEAD][q][1][k / 2] >> (16 * (k & 1))) & 0xffffu);
                 float value, slope;
                 act_both<ACT>(g, value, slope);
                 ga[k] = d * u * slope;
@@ -192,6 +193,7 @@ __device__ __forceinline__ void store_grad_as(const FusedArgs &a, const f32x16_t
                 if (h != nullptr) store4_bf16(h + (row0 + dr) * a.ldc3 + col, left, pack_bf16(ha[0], ha[1]), pack_bf16(ha[2], ha[3]));
             }
         }
+        if constexpr (F + AHEAD < TM * TN) fetch(std::integral_constant<int, F + AHEAD>{});
         __builtin_amdgcn_sched_barrier(0);
     });
 }
@@ -205,17 +207,48 @@ __device__ __forceinline__ void store_plain(const KernelArgs &g, const f32x16_t 
 }
 
 // ---------------------------------------------------------------------------
+// Which tile and K slice a workgroup has.  The first `whole` workgroups have a tile each with all of K, the rest a slice of
+// one of the tiles after those: a last round of tiles that leaves compute units idle is cut along K instead (344 tiles
+// of 256 x 256 are 256 whole ones and 88 in three slices).  As in map_tile, each XCD has a contiguous range of either
+// part, and tiles are walked in groups of rows.  first and count: the stages of 64 k (of `all`).
+// ---------------------------------------------------------------------------
+struct FusedWork {
+    int tm, tn, slot, slice;     // slot: the tile's place among those cut along K
+    int first, count;
+    bool cut;
+};
+__device__ __forceinline__ FusedWork fused_work(const KernelArgs &g, int whole, int all) {
+    const bool tail = int(blockIdx.x) >= whole;
+    const int total = tail ? int(gridDim.x) - whole : whole, hw = tail ? int(blockIdx.x) - whole : int(blockIdx.x);
+    const int per = total / 8, rem = total % 8, xcd = hw % 8, local = hw / 8;
+    const int id = xcd < rem ? xcd * (per + 1) + local : rem * (per + 1) + (xcd - rem) * per + local;
+    const int after = g.tiles_m * g.tiles_n - whole;
+    FusedWork w;
+    w.cut = tail && g.split_k > 1;
+    w.slice = tail ? id / after : 0;
+    w.slot = tail ? id % after : 0;
+    const int t = tail ? whole + w.slot : id;
+    const int width = g.group_m * g.tiles_n, first_m = t / width * g.group_m;
+    const int rows = g.tiles_m - first_m < g.group_m ? g.tiles_m - first_m : g.group_m;
+    w.tm = first_m + t % width % rows;
+    w.tn = t % width / rows;
+    const int chunk = int(g.k_chunk / 64);
+    w.first = w.cut ? w.slice * chunk : 0;
+    w.count = w.cut && w.first + chunk < all ? chunk : all - w.first;
+    return w;
+}
+
+// ---------------------------------------------------------------------------
 // K slices: every slice leaves its sums in the workspace as its registers hold them and the one that
-// arrives last adds them up in their order (mx_common.h says how the accesses are ordered).
-// True in every thread of the workgroup that holds the whole sums.
+// arrives last adds the others' to its own, all in the order of the slices, whichever it is (mx_common.h says how
+// the accesses are ordered).  True in every thread of the workgroup that holds the whole sums.
 // ---------------------------------------------------------------------------
 template <int THREADS, int TM, int TN>
-__device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[TM][TN], int tile, int slice, int64_t rows, int &flag) {
-    if (g.split_k == 1) return true;
+__device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[TM][TN], int slot, int slice, int64_t rows, int &flag) {
     constexpr uint32_t SLICE = uint32_t(TM * TN * 16 * 4) * THREADS;
-    const __amdgpu_buffer_rsrc_t parts = mx_parts(g, tile, SLICE);
+    const __amdgpu_buffer_rsrc_t parts = mx_parts(g, slot, SLICE);
     const uint32_t off = threadIdx.x * 16;
-    // Slot q of fragment row i: rows 32 i + 8 q .. + 7 of the wave's; past M nothing is left or fetched.
+    // Register group q of fragment row i: rows 32 i + 8 q .. + 7 of the wave's; past M nothing is left or fetched.
     auto at = [&](int s, int i, int j, int q) __attribute__((always_inline)) {
         return uint32_t(s) * SLICE + off + uint32_t(((i * TN + j) * 4 + q) * THREADS) * 16;
     };
@@ -228,47 +261,56 @@ __device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[
                 if (32 * i + 8 * q < rows)
                     mx_store_part(parts, at(slice, i, j, q),
                                   f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
-    if (!mx_last_slice(g, tile, flag)) return false;
+    if (!mx_last_slice(g, slot, flag)) return false;
+    // ((part 0 + part 1) + ...) + own + ... : own stays in its registers, what comes before it is added up beside them.
+    // FRAGMENTS fragments of WAYS slices on the way at once, as many registers as a tile of that size leaves.
+    constexpr int F = TM * TN;
+    auto pass = [&](auto f0_c, auto count_c, auto ways_c, int begin, int end, auto &&into) __attribute__((always_inline)) {
+        constexpr int F0 = decltype(f0_c)::value, COUNT = decltype(count_c)::value, WAYS = decltype(ways_c)::value;
+#pragma unroll 1
+        for (int s = begin; s < end; s += WAYS) {
+            f32x4_t v[WAYS][COUNT][4];
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+            for (int u = 0; u < WAYS; ++u)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
-    // The sums stay in their registers: several slices of a small tile are on the way at once, a slice of a large one
-    // in parts.
-    auto add = [&](int s, auto n_c) __attribute__((always_inline)) {
-        constexpr int COUNT = decltype(n_c)::value, ROWS = TM * TN > 4 ? 1 : TM;
-        static_for<0, (TM + ROWS - 1) / ROWS>([&](auto b_c) __attribute__((always_inline)) {
-            constexpr int I0 = decltype(b_c)::value * ROWS, I1 = I0 + ROWS < TM ? I0 + ROWS : TM;
-            f32x4_t v[COUNT][ROWS][TN][4];
+                for (int f = 0; f < COUNT; ++f)
 #pragma unroll
-            for (int u = 0; u < COUNT; ++u)
+                    for (int q = 0; q < 4; ++q)              // past the end zeros, which change nothing
+                        v[u][f][q] = mx_load_part(parts, s + u < end && 32 * ((F0 + f) / TN) + 8 * q < rows ? at(s + u, (F0 + f) / TN, (F0 + f) % TN, q) : kOOB);
 #pragma unroll
-                for (int i = I0; i < I1; ++i)
+            for (int u = 0; u < WAYS; ++u)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
+                for (int f = 0; f < COUNT; ++f)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            v[u][i - I0][j][q] = mx_load_part(parts, 32 * i + 8 * q < rows ? at(s + u, i, j, q) : kOOB);
-#pragma unroll
-            for (int u = 0; u < COUNT; ++u)
-#pragma unroll
-                for (int i = I0; i < I1; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += v[u][i - I0][j][q][e];
-            if constexpr (TM * TN > 4) __builtin_amdgcn_sched_barrier(0);
-        });
+                    for (int q = 0; q < 4; ++q) into(f, q, v[u][f][q]);
+        }
     };
-    constexpr int G = TM * TN >= 4 ? 1 : 4 / (TM * TN);        // slices on the way at once
-    int s = 0;
-#pragma unroll 1
-    for (; s + G <= g.split_k; s += G) add(s, std::integral_constant<int, G>{});
-#pragma unroll 1
-    for (; s < g.split_k; ++s) add(s, std::integral_constant<int, 1>{});
-    mx_reset_counter(g, tile);
+    auto group = [&](auto f0_c, auto count_c, auto ways_c) __attribute__((always_inline)) {
+        constexpr int F0 = decltype(f0_c)::value, COUNT = decltype(count_c)::value;
+        auto add = [&](int f, int q, f32x4_t v) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[(F0 + f) / TN][(F0 + f) % TN][4 * q + e] += v[e];
+        };
+        if (slice > 1) {
+            f32x4_t sum[COUNT][4] = {};
+            pass(f0_c, count_c, ways_c, 0, slice, [&](int f, int q, f32x4_t v) __attribute__((always_inline)) { sum[f][q] += v; });
+#pragma unroll
+            for (int f = 0; f < COUNT; ++f)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) add(f, q, sum[f][q]);
+        } else {
+            pass(f0_c, count_c, std::integral_constant<int, 1>{}, 0, slice, add);
+        }
+        pass(f0_c, count_c, ways_c, slice + 1, g.split_k, add);
+    };
+    constexpr int FRAGMENTS = F <= 4 ? F : 2, WAYS = F <= 2 ? 4 : 1;
+    static_assert(F % FRAGMENTS == 0, "whole groups");
+    static_for<0, F / FRAGMENTS>([&](auto k) __attribute__((always_inline)) {
+        group(std::integral_constant<int, decltype(k)::value * FRAGMENTS>{}, std::integral_constant<int, FRAGMENTS>{},
+              std::integral_constant<int, WAYS>{});
+        if constexpr (F > 4) __builtin_amdgcn_sched_barrier(0);
+    });
+    mx_reset_counter(g, slot);
     return true;
 }
 

@@ -45,7 +45,7 @@ __device__ __forceinline__ void split_bf16(const float (&v)[8], u32x4_t (&part)[
 __device__ __forceinline__ void load_h(const FusedArgs &a, int64_t t, int k, int left, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-    for (int p = 0; p < a.planes; ++p) {
+    for (int p = 0; p < a.planes; ++p) {                         // one, but for few rows
         const float *const src = a.h + p * a.h_plane + t * a.r + k;
         if (left >= 8) {
             const f32x4_t x = *reinterpret_cast<const f32x4_el_t *>(src), y = *reinterpret_cast<const f32x4_el_t *>(src + 4);
@@ -84,9 +84,9 @@ __device__ __forceinline__ u32x4_t load8_any(const uint16_t *p) {
 // acc += h_t Q_i(t) for the wave's rows (TM x 32 from r0) and columns (32 from c0 and 32 from c0 + HALF).  QT: Q_i
 // is N x r, else r x N.
 //
-// The adapters that occur among a fragment's 32 rows are taken one after the other (most fragments of a prompt hold
-// one, and a decode batch's rows of weights have to be read for each of its requests anyway), each as
-// a product of all 32 rows, of which only the adapter's own take the result: rows are chosen, not multiplied
+// Rows of one adapter take its product straight onto their sums.  Among others the adapters that occur in 32 rows are
+// taken one after the other (a decode batch's rows of weights have to be read for each of its requests anyway), each as
+// a product of the 32 rows, of which only the adapter's own take the result: rows are chosen, not multiplied
 // by zeros, so an infinity or a NaN in one request's adapter stays out of the others'.  h does not depend on the
 // adapter and is read once for every 16 ranks; the matrices of four adapters are on their way at once, for what
 // a batch of many requests waits for is their latency.  h keeps its fp32 value in two bf16 parts (2^-16 left
@@ -105,21 +105,67 @@ __device__ __forceinline__ void expand_adapters(const FusedArgs &a, f32x16_t (&a
         const int64_t c = c0 + HALF * j + l32;
         col[j] = c < N ? c : N - 1;                              // not stored
     }
+    // Eight of column c's values from rank k0 on.
+    auto weights = [&](const uint16_t *q, int64_t c, int k0, int left) __attribute__((always_inline)) {
+        if (QT) return load8_bf16(q + c * a.ldq + k0, left);
+        u32x4_t w{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) w[e / 2] |= uint32_t(q[(k0 + e) * a.ldq + c]) << (16 * (e & 1));
+        return w;
+    };
+    int own[TM];
+    uint32_t all[TM];
+    int common = -1;                                             // the adapter of all rows, if it is one
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t t = r0 + 32 * i + l32;
+        own[i] = t < a.g.M ? a.index[t] : -1;
+        if (uint32_t(own[i]) >= uint32_t(a.n)) own[i] = -1;
+        all[i] = uint32_t(__ballot(own[i] >= 0));
+        if (all[i] != 0u && common < 0) common = __builtin_amdgcn_readlane(own[i], __builtin_ctz(all[i]));
+    }
+    if (common < 0) return;
+    uint32_t others = 0u;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) others |= uint32_t(__ballot(r0 + 32 * i + l32 < a.g.M && own[i] != common));
+    if (others == 0u) {
+        // One for all rows: straight onto the sums, its matrix read once.
+        const uint16_t *const q = static_cast<const uint16_t *>(a.Q) + common * a.sq;
+        for (int k = 0; k < a.r; k += 16) {
+            const int k0 = k + 8 * half, left = a.r - k0;
+            u32x4_t w[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) w[j] = weights(q, col[j], k0, left);
+            float v[TM][8] = {};
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                if (own[i] >= 0) load_h(a, r0 + 32 * i + l32, k0, left, v[i]);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                u32x4_t part[3];
+                split_bf16(v[i], part);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    if (exact) acc[i][j] = mfma32<DT_BF16>(part[2], w[j], acc[i][j]);
+                    acc[i][j] = mfma32<DT_BF16>(part[1], w[j], acc[i][j]);
+                    acc[i][j] = mfma32<DT_BF16>(part[0], w[j], acc[i][j]);
+                }
+            }
+        }
+        return;
+    }
     static_for<0, TM>([&](auto i_c) __attribute__((always_inline)) {
         constexpr int I = decltype(i_c)::value;
-        const int64_t t = r0 + 32 * I + l32;
-        const int own = t < a.g.M ? a.index[t] : -1;
-        const bool has = uint32_t(own) < uint32_t(a.n);
-        const uint32_t all = uint32_t(__ballot(has));
-        if (all == 0u) return;
+        if (all[I] == 0u) return;
         for (int k = 0; k < a.r; k += 16) {
             const int k0 = k + 8 * half, left = a.r - k0;
             float v[8] = {};
-            if (has) load_h(a, t, k0, left, v);
+            if (own[I] >= 0) load_h(a, r0 + 32 * I + l32, k0, left, v);
             u32x4_t part[3];
             split_bf16(v, part);
             constexpr int B = 4;                                 // adapters on the way at once
-            uint32_t pending = all;
+            uint32_t pending = all[I];
             while (pending != 0u) {
                 u32x4_t w[B][TN];
                 uint32_t rows[B];
@@ -127,21 +173,12 @@ __device__ __forceinline__ void expand_adapters(const FusedArgs &a, f32x16_t (&a
                 for (int b = 0; b < B; ++b) {
                     rows[b] = 0u;
                     if (pending == 0u) continue;
-                    const int cur = __builtin_amdgcn_readlane(own, __builtin_ctz(pending));
-                    rows[b] = uint32_t(__ballot(has && own == cur));
+                    const int cur = __builtin_amdgcn_readlane(own[I], __builtin_ctz(pending));
+                    rows[b] = uint32_t(__ballot(own[I] == cur));
                     pending &= ~rows[b];
                     const uint16_t *const q = static_cast<const uint16_t *>(a.Q) + cur * a.sq;
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        if (QT) {
-                            w[b][j] = load8_bf16(q + col[j] * a.ldq + k0, left);
-                        } else {
-                            w[b][j] = u32x4_t{0u, 0u, 0u, 0u};
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (e < left) w[b][j][e / 2] |= uint32_t(q[(k0 + e) * a.ldq + col[j]]) << (16 * (e & 1));
-                        }
-                    }
+                    for (int j = 0; j < TN; ++j) w[b][j] = weights(q, col[j], k0, left);
                 }
 #pragma unroll
                 for (int b = 0; b < B; ++b) {

@@ -12,14 +12,14 @@ int64_t up16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
 // Tokens and ranks of a block (in sixteens).
 int shrink_rt(const ShrinkArgs &s) { return s.r <= 16 ? 1 : s.r <= 32 ? 2 : 4; }
-int shrink_mt(const ShrinkArgs &s) { return s.M <= 64 ? 1 : s.M <= 1024 || shrink_rt(s) == 4 ? 2 : 4; }
+int shrink_mt(const ShrinkArgs &s) { return s.M <= 64 ? 1 : s.M <= 512 || (shrink_rt(s) == 4 && !s.qt) ? 2 : 4; }
 
 template <bool QT, int MT>
 void queue_shrink_rows(const ShrinkArgs &s, dim3 grid, hipStream_t stream) {
     const int rt = shrink_rt(s);
-    if (rt == 1) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 1, 8>), grid, dim3(512), 0, stream, s);
+    if (rt == 1) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 1, MT == 1 ? 16 : 8>), grid, dim3(MT == 1 ? 1024 : 512), 0, stream, s);
     else if (rt == 2) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 2, 8>), grid, dim3(512), 0, stream, s);
-    else if constexpr (MT < 4) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 4, 8>), grid, dim3(512), 0, stream, s);
+    else if constexpr (QT || MT < 4) hipLaunchKernelGGL((adapters_shrink_kernel<QT, MT, 4, 8>), grid, dim3(512), 0, stream, s);
 }
 template <bool QT>
 hipError_t queue_shrink(const ShrinkArgs &s, hipStream_t stream) {
@@ -40,16 +40,17 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     const int64_t cols = op == FUSED_GATED ? c.bn / 2 : c.bn;
     const bool any = fused_any_address(plan.config);
     const int64_t tm = (a.g.M + c.bm - 1) / c.bm * (op == FUSED_DW ? a.pairs : 1), tn = (a.g.N + cols - 1) / cols;
-    const int64_t grid = tm * tn * plan.split_k;
+    const int64_t cut = tm * tn - plan.whole, grid = plan.whole + cut * plan.split_k;
     a.g.k_chunk = plan.k_chunk;
     a.g.split_k = plan.split_k;
+    a.whole = plan.whole;
     a.g.tiles_m = int32_t(tm);
     a.g.tiles_n = int32_t(tn);
     a.g.group_m = 4;
     a.g.reduce_in_kernel = REDUCE_LAST_SLICE;
 
     // Scratch: the K slices' sums, the planes of h, and aligned copies of operands that need one.
-    const int64_t partial = a.g.split_k > 1 ? grid * c.bm * c.bn * 4 : 0;
+    const int64_t partial = a.g.split_k > 1 ? cut * plan.split_k * c.bm * c.bn * 4 : 0;
     const bool at = op == FUSED_DW, bt = op == FUSED_GATED || op == FUSED_ADAPT;
     const int64_t a_rows = at ? a.g.K : a.g.M, a_cols = at ? a.g.M : a.g.K;
     const int64_t b_rows = bt ? a.g.N : a.g.K, b_cols = bt ? a.g.K : a.g.N;
@@ -68,7 +69,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     const bool sum_h = shrink != nullptr && shrink->slices > 1 && (shrink->h != nullptr || !fused_few_rows(plan.config));
     const bool own_h = shrink != nullptr && shrink->h == nullptr && sum_h;
     const int64_t planes = shrink == nullptr || (shrink->h != nullptr && shrink->slices == 1) ? 0 : up16((shrink->slices + (own_h ? 1 : 0)) * shrink->plane * 4);
-    const int64_t counted = (a.g.split_k > 1 ? tm * tn : 0), h_counted = sum_h ? int64_t(shrink->blocks) * shrink->groups : 0;
+    const int64_t counted = a.g.split_k > 1 ? cut : 0, h_counted = sum_h ? int64_t(shrink->blocks) * shrink->groups : 0;
 
     WorkspaceHold hold;                  // over the copies, the adapters' first product and the product
     if (partial + copied + planes > 0) {

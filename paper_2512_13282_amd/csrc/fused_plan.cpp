@@ -7,7 +7,7 @@ const FusedConfig kFusedConfigs[] = {
     {64, 128, 4, 2, 4096, "fused_64x128_2x2"},
     {128, 256, 8, 1, 4096, "fused_pingpong_128x256"},
     {192, 256, 8, 1, 4096, "fused_pingpong_192x256"},
-    {256, 256, 8, 1, 1, "fused_pingpong_256x256"},
+    {256, 256, 8, 1, 16, "fused_pingpong_256x256"},
     {16, 16, 8, 2, 1, "fused_decode_16"},
     {32, 16, 8, 2, 1, "fused_decode_32"},
     {48, 16, 8, 2, 1, "fused_decode_48"},
@@ -28,13 +28,18 @@ bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_
     const FusedConfig &c = kFusedConfigs[config];
     if (split > c.most_slices || (fused_few_rows(config) && M > c.bm)) return false;
     const int64_t stages = ceil_div(K, 64) * (op == FUSED_DX ? 2 : 1);
-    const int64_t chunk = stages > 0 ? ceil_div(stages, split) : 1;
+    const int64_t tiles = ceil_div(M, c.bm) * pairs * ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn);
+    // Tiles that fill whole rounds of the compute units keep all of K; slices are for the rest.
+    const int64_t slots = int64_t(kCUs) * c.occupancy, rest = tiles % slots;
+    const int64_t chunk = stages > 0 && rest > 0 ? ceil_div(stages, split) : stages > 0 ? stages : 1;
     out->config = config;
     out->k_chunk = 64 * chunk;
     out->split_k = int32_t(stages > 0 ? ceil_div(stages, chunk) : 1);
+    const int64_t cut = out->split_k > 1 ? rest : 0;
+    if (tiles > INT32_MAX) return false;
+    out->whole = int32_t(tiles - cut);
     // A tile's partial sums are addressed with 32 bits, and a grid holds fewer than 2^32 threads.
-    const int64_t tiles = ceil_div(M, c.bm) * pairs * ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn);
-    return int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && tiles <= UINT32_MAX / (64 * c.waves) / out->split_k;
+    return int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && tiles - cut + cut * out->split_k <= UINT32_MAX / (64 * c.waves);
 }
 
 // Modelled microseconds of a plan, without the launch.

@@ -106,14 +106,20 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
         constexpr int U = MT * RT >= 8 ? 2 : MT * RT >= 4 ? 3 : 4;
         u32x4_t x[U][MT], w[U][RT];
         // Chunk c of this wave; rows of L past `left` are zeros.
-        auto load = [&](int u, int c, bool all) __attribute__((always_inline)) {
+        const bool pieces = s.r % 8 == 0;                        // Q across: whole pieces of ranks; those past r are not written
+        if constexpr (!QT) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                if (pieces && ranks <= 0) qp[rt] -= 8 * (lane % CPR);
+        }
+        auto load = [&](int u, int c, bool all, bool eight) __attribute__((always_inline)) {
             const int left = length - 32 * (c0 + c);
 #pragma unroll
             for (int m = 0; m < MT; ++m) x[u][m] = load8_bf16(row[m] + 32 * c, all ? 8 : left - 8 * grp);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 if constexpr (QT) w[u][rt] = load8_bf16(qp[rt] + 32 * c, all ? 8 : left - 8 * grp);
-                else w[u][rt] = load8_bf16(qp[rt] + 32 * c * s.ldq, all || rt * (64 / CPR) + lane / CPR < left ? ranks : 0);
+                else w[u][rt] = load8_bf16(qp[rt] + 32 * c * s.ldq, all || rt * (64 / CPR) + lane / CPR < left ? (eight ? 8 : ranks) : 0);
             }
         };
         auto multiply = [&](int u) __attribute__((always_inline)) {
@@ -144,27 +150,32 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) acc[m][rt] = mfma16_bf16(f[rt], x[u][m], acc[m][rt]);
         };
+        auto walk = [&](auto eight_c) __attribute__((always_inline)) {
+            constexpr bool EIGHT = decltype(eight_c)::value;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < n) load(u, u, true);
-        int i = 0;
-        for (; i + 2 * U <= n; i += U) {
+            for (int u = 0; u < U; ++u)
+                if (u < n) load(u, u, true, EIGHT);
+            int i = 0;
+            for (; i + 2 * U <= n; i += U) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    multiply(u);
+                    load(u, i + U + u, true, EIGHT);
+                }
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                multiply(u);
-                load(u, i + U + u, true);
+                if (i + u < n) multiply(u);
+                if (i + U + u < n) load(u, i + U + u, true, EIGHT);
             }
-        }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (i + u < n) multiply(u);
-            if (i + U + u < n) load(u, i + U + u, true);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + U + u < n) multiply(u);
+            for (int u = 0; u < U; ++u)
+                if (i + U + u < n) multiply(u);
+        };
+        if (QT || pieces) walk(std::true_type{});
+        else walk(std::false_type{});
         if (chunks > whole && whole >= c0 && whole < c1) {       // the end of L that is no whole chunk
-            load(0, whole - c0, false);
+            load(0, whole - c0, false, false);
             multiply(0);
         }
 #pragma unroll

@@ -24,8 +24,13 @@ __device__ __forceinline__ void few_rows_adapters(const FusedArgs &a, float (&hs
         for (int i = tid; i < TOKENS * kFewRanks; i += THREADS) {
             const int t = i / kFewRanks, j = i % kFewRanks;
             float v = 0.0f;
-            if (t < M && j < ranks)
-                for (int p = 0; p < a.planes; ++p) v += a.h[p * a.h_plane + int64_t(t) * a.r + j0 + j];
+            if (t < M && j < ranks) {
+                float parts[8];                                           // all of them on the way at once
+#pragma unroll
+                for (int p = 0; p < 8; ++p) parts[p] = p < a.planes ? a.h[p * a.h_plane + int64_t(t) * a.r + j0 + j] : 0.0f;
+#pragma unroll
+                for (int p = 0; p < 8; ++p) v += parts[p];
+            }
             hs[t][j] = v;
         }
         phase_barrier();

@@ -36,17 +36,14 @@ void fused_pingpong_kernel(FusedArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = wave >> 2, wave_n = wave & 3;
 
-    int tm, tn, slice;
-    map_tile(a.g, tm, tn, slice);
-    const int tile = tm * a.g.tiles_n + tn;
+    const int K = int(a.g.K), one = (K + BK - 1) / BK;      // stages of one product
+    const FusedWork work = fused_work(a.g, a.whole, OP == FUSED_DX ? 2 * one : one);
+    int tm = work.tm;
+    const int tn = work.tn, first = work.first, ns = work.count;
     const int which = OP == FUSED_DW && tm >= a.g.tiles_m / a.pairs;
     if (which) tm -= a.g.tiles_m / a.pairs;
     const int64_t M = a.g.M, N = a.g.N;
-    const int K = int(a.g.K);
     const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * COLS;
-    const int one = (K + BK - 1) / BK, all = OP == FUSED_DX ? 2 * one : one;
-    const int first = slice * int(a.g.k_chunk / BK);
-    const int ns = first + int(a.g.k_chunk / BK) < all ? int(a.g.k_chunk / BK) : all - first;
 
     const uint8_t *const a_src = static_cast<const uint8_t *>(which ? a.A2 : a.g.A);
     const int lda_b = int(which ? a.lda2 : a.g.lda) * 2, lda2_b = int(a.lda2) * 2;       // at most 4 MiB
@@ -249,7 +246,7 @@ void fused_pingpong_kernel(FusedArgs a) {
         });
     }
     if constexpr (L::EXPAND)
-        if (slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + grp * (32 * TM), n0 + wave_n * 32, lane);
+        if (work.slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + grp * (32 * TM), n0 + wave_n * 32, lane);
     if (ns > 0) {
         // B0 and A0 of stage 0 have landed: all but the other six units.
         ring_barrier<3 * LB + H0 + 2 * H1>();
@@ -265,8 +262,7 @@ void fused_pingpong_kernel(FusedArgs a) {
         if (grp == 0) asm volatile("s_barrier" ::: "memory");
     }
     stage_barrier();                                       // drains the loads past the end, by every wave
-    if constexpr (TM < 4)                                  // with 256 rows the last slice's sums in flight would spill
-        if (!sum_slices<512>(a.g, acc, tile, slice, M - (m0 + grp * (32 * TM)), *reinterpret_cast<int *>(lds[0]))) return;
+    if (work.cut && !sum_slices<512>(a.g, acc, work.slot, work.slice, M - (m0 + grp * (32 * TM)), *reinterpret_cast<int *>(lds[0]))) return;
     store_fused<OP, 512, HALF>(a, acc, which, m0 + grp * (32 * TM), n0 + wave_n * 32, lane);
 }
 

@@ -64,18 +64,15 @@ void fused_tile_kernel(FusedArgs a) {
     const int tid = int(threadIdx.x), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wave_m = wave / WN, wave_n = wave % WN;
-    int tm, tn, slice;
-    map_tile(a.g, tm, tn, slice);
-    const int tile = tm * a.g.tiles_n + tn;
+    const int one = int((a.g.K + BK - 1) / BK);                 // stages of one product
+    const FusedWork work = fused_work(a.g, a.whole, OP == FUSED_DX ? 2 * one : one);
+    int tm = work.tm;
+    const int tn = work.tn, first = work.first, nk = work.count;
     const int which = OP == FUSED_DW && tm >= a.g.tiles_m / a.pairs;
     if (which) tm -= a.g.tiles_m / a.pairs;
     const int64_t M = a.g.M, N = a.g.N, K = a.g.K;
     constexpr int COLS = BN / L::HALVES;                         // output columns of a tile
     const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * COLS;
-    const int one = int((K + BK - 1) / BK);                     // stages of one product
-    const int first = int(slice * (a.g.k_chunk / BK));
-    const int all = OP == FUSED_DX ? 2 * one : one;
-    const int nk = first + int(a.g.k_chunk / BK) < all ? int(a.g.k_chunk / BK) : all - first;
 
     const uint8_t *const a_src = static_cast<const uint8_t *>(which ? a.A2 : a.g.A);
     const int64_t lda_b = (which ? a.lda2 : a.g.lda) * 2, lda2_b = a.lda2 * 2;
@@ -226,17 +223,17 @@ void fused_tile_kernel(FusedArgs a) {
     if (nk > 0) {
         static_for<0, NS - 1>([&](auto u) { load_stage(decltype(u)::value, u); });
         if constexpr (L::EXPAND)
-            if (slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + wrow0, n0 + wcol0, lane);
+            if (work.slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + wrow0, n0 + wcol0, lane);
         for (int kt = 0; kt < nk; kt += NS) {
             static_for<0, NS>([&](auto u) {
                 if (kt + decltype(u)::value < nk) iteration(kt + decltype(u)::value, u);
             });
         }
     } else if constexpr (L::EXPAND) {
-        if (slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + wrow0, n0 + wcol0, lane);
+        if (work.slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + wrow0, n0 + wcol0, lane);
     }
     stage_barrier();       // drains the loads past the end before sum_slices borrows a word of the buffers
-    if (!sum_slices<THREADS>(a.g, acc, tile, slice, M - (m0 + wrow0), *reinterpret_cast<int *>(lds[0]))) return;
+    if (work.cut && !sum_slices<THREADS>(a.g, acc, work.slot, work.slice, M - (m0 + wrow0), *reinterpret_cast<int *>(lds[0]))) return;
     store_fused<OP, THREADS, HALF>(a, acc, which, m0 + wrow0, n0 + wcol0, lane);
 }
 

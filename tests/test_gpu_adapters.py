@@ -13,7 +13,9 @@ pytestmark = pytest.mark.gpu
 # M, N, K, adapters, rank, pad, offset
 SIZES = [(1, 8, 8, 1, 8, 0, 0), (1, 1, 1, 1, 1, 0, 0), (3, 7, 5, 2, 3, 0, 0), (16, 128, 256, 16, 16, 0, 0), (37, 131, 129, 5, 7, 1, 3),
          (64, 256, 520, 3, 16, 8, 8), (65, 130, 1000, 70, 4, 0, 0), (130, 264, 320, 1, 64, 0, 0), (300, 513, 511, 9, 33, 5, 1),
-         (257, 520, 136, 4, 128, 0, 0), (1, 1000, 2056, 3, 16, 0, 0), (12, 512, 4104, 40, 32, 0, 0), (511, 264, 64, 2, 1, 0, 0)]
+         (257, 520, 136, 4, 128, 0, 0), (1, 1000, 2056, 3, 16, 0, 0), (12, 512, 4104, 40, 32, 0, 0), (511, 264, 64, 2, 1, 0, 0),
+         # More tiles than compute units: whole ones, and slices of the rest.
+         (1100, 4200, 200, 6, 16, 0, 0), (4340, 4100, 264, 7, 24, 0, 4)]
 
 
 def indices(gen, M, n):
@@ -240,3 +242,19 @@ def test_results_leave_their_padding():
     assert rc == b.GEMM_OK
     assert torch.equal(dA[:, :5, :96], want[0]) and torch.equal(dB[:, :133, :5], want[1])
     assert torch.all(dA[:, 5:] == 7) and torch.all(dA[:, :, 96:] == 7) and torch.all(dB[:, 133:] == 7) and torch.all(dB[:, :, 5:] == 7)
+
+
+@pytest.mark.parametrize("none", [range(0, 40), range(64, 128), range(96, 300), range(0, 1)])
+def test_rows_without_an_adapter_beside_one_of_nan(none):
+    """Rows that share a tile with one adapter's rows and have none keep their bits whatever the adapter holds."""
+    gen = generator("none beside", none.start, none.stop)
+    M, N, K, r = 300, 270, 136, 20
+    x, w, v = matrix(gen, M, K), matrix(gen, N, K), matrix(gen, K, N)
+    index = torch.zeros(M, dtype=torch.int32)
+    index[list(none)] = -1
+    rows, index = (index < 0).to(DEV), index.to(DEV)
+    bad = torch.full((1, r, max(N, K)), float("nan"), dtype=BF16, device=DEV)
+    for op, fn, weight, n_in, n_out in ((0, b.linear_adapters, w, K, N), (1, b.linear_adapters_dx, v, N, K)):
+        held = ad.Adapters(bad[:, :, :n_in], bad[:, :, :n_out].transpose(1, 2).contiguous())
+        for plan, y in plans(op, lambda: fn(x, weight, held, index)):
+            assert torch.all(torch.isfinite(y[rows])) and torch.all(torch.isnan(y[~rows])), plan

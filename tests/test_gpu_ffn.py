@@ -31,7 +31,9 @@ def generator(*key):
 # M, N, K, pad, offset of the operands (elements)
 SIZES = [(1, 8, 8, 0, 0), (1, 1, 1, 0, 0), (3, 7, 5, 0, 0), (17, 33, 65, 0, 0), (64, 128, 64, 0, 0), (65, 129, 72, 8, 8), (37, 131, 129, 1, 3),
          (100, 264, 320, 0, 0), (130, 250, 1000, 8, 0), (257, 520, 136, 0, 0), (300, 513, 511, 5, 1), (1, 1000, 2048, 0, 0),
-         (16, 512, 4104, 0, 0), (511, 264, 64, 0, 0)]
+         (16, 512, 4104, 0, 0), (511, 264, 64, 0, 0),
+         # More tiles than compute units: whole ones, and slices of the rest.
+         (1100, 2200, 328, 0, 0), (4340, 4100, 264, 0, 4)]
 ids = dict(ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else str(v))
 
 
