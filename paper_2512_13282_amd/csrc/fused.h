@@ -29,7 +29,12 @@ struct FusedArgs {
     int64_t ldg, ldu;
     int32_t act;                     // FFN_* of ffn_mi355x.h
     int32_t pairs;                   // DW: 1 or 2 matrices A
-    int32_t whole;                   // tiles with all of K, ahead of those cut into slices
+    int32_t whole;                   // workgroups with a tile and all of K, ahead of the rest
+    int32_t half;                    // DW: tile rows of the first matrix
+    struct Tail {                    // the lower tiles, where the plan has some: from row `row` and column `col` on
+        int64_t row, col;
+        int32_t tiles_m, tiles_n, half;
+    } tail;
     // ADAPT: row t's h is the sum over `planes` of h[plane][t][0 .. r), its adapter index[t] in [0, n), any other
     // value for none; adapter i's matrix starts sq elements after the one before it, rows ldq apart.
     const float *h;
@@ -43,8 +48,10 @@ struct FusedArgs {
 // How a product runs: a row of kFusedConfigs and the number of K slices.
 struct FusedPlan {
     int32_t config;
-    int32_t split_k;
-    int32_t whole;                   // tiles with all of K, the rest are cut into slices
+    int32_t split_k;                 // slices of each tile after the first `whole`
+    int32_t whole;
+    int32_t tail_rows, tail_cols;    // else the tile rows and columns that tiles of the whole height have, where lower
+                                     // ones have the rest (0, 0: none)
     int64_t k_chunk;                 // K of a slice, a multiple of 64 (DX: of both products' K one after the other)
 };
 
@@ -53,14 +60,21 @@ struct FusedConfig {
     int32_t waves;                   // per workgroup
     int32_t occupancy;               // workgroups that a compute unit holds
     int32_t most_slices;
+    int32_t low;                     // rows of the lower tiles of a last round, 0: none
     const char *name;
 };
 extern const FusedConfig kFusedConfigs[];
 extern const int32_t kFusedNumConfigs;
 
+// The region that a plan's lower tiles cover: from a row (of the matrix that the others leave off in) or a column on.
+struct FusedTail {
+    int64_t row, col, tiles_m, tiles_n, tiles, half;         // half: tile rows of the first matrix
+};
+FusedTail fused_tail(FusedOp op, int32_t pairs, int64_t M, int64_t N, const FusedPlan &p);
+
 // The kernels for few rows of A, by rows: the one that takes its operands as they lie, and the one for operands on
 // 16-byte rows.
-constexpr int32_t kFusedDecode = 4, kFusedStream = 8;
+constexpr int32_t kFusedDecode = 6, kFusedStream = 10;
 inline bool fused_few_rows(int32_t config) { return config >= kFusedDecode; }
 inline bool fused_any_address(int32_t config) { return config >= kFusedDecode && config < kFusedStream; }
 

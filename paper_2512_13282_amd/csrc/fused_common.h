@@ -207,34 +207,47 @@ __device__ __forceinline__ void store_plain(const KernelArgs &g, const f32x16_t 
 }
 
 // ---------------------------------------------------------------------------
-// Which tile and K slice a workgroup has.  The first `whole` workgroups have a tile each with all of K, the rest a slice of
-// one of the tiles after those: a last round of tiles that leaves compute units idle is cut along K instead (344 tiles
-// of 256 x 256 are 256 whole ones and 88 in three slices).  As in map_tile, each XCD has a contiguous range of either
-// part, and tiles are walked in groups of rows.  first and count: the stages of 64 k (of `all`).
+// What a workgroup computes.  The first `whole` workgroups have an output tile each with all of K.  The rest fill a last
+// round that would leave compute units idle: with slices of K of the tiles after those, or (`tail`) with lower tiles over the
+// rows or columns after those, which end sooner (gated 2048 x 11008: 512 tiles of 256 rows in two rounds, then 242 of
+// 192 rows in place of 176).  As in map_tile, each XCD has a contiguous range of either part, and tiles are walked in
+// groups of rows.
 // ---------------------------------------------------------------------------
 struct FusedWork {
-    int tm, tn, slot, slice;     // slot: the tile's place among those cut along K
-    int first, count;
-    bool cut;
+    int64_t m0, n0;              // of the tile
+    int which;                   // DW: the second matrix
+    int first, count;            // stages of 64 k
+    int slot, slice, slices;     // the tile's place among those in slices, this slice of it and how many there are
+    bool low;                    // one of the lower tiles
 };
-__device__ __forceinline__ FusedWork fused_work(const KernelArgs &g, int whole, int all) {
-    const bool tail = int(blockIdx.x) >= whole;
-    const int total = tail ? int(gridDim.x) - whole : whole, hw = tail ? int(blockIdx.x) - whole : int(blockIdx.x);
+template <int BM, int LOW, int COLS>
+__device__ __forceinline__ FusedWork fused_work(const FusedArgs &a, int all) {
+    const KernelArgs &g = a.g;
+    const bool rest = int(blockIdx.x) >= a.whole;
+    const int total = rest ? int(gridDim.x) - a.whole : a.whole, hw = rest ? int(blockIdx.x) - a.whole : int(blockIdx.x);
     const int per = total / 8, rem = total % 8, xcd = hw % 8, local = hw / 8;
     const int id = xcd < rem ? xcd * (per + 1) + local : rem * (per + 1) + (xcd - rem) * per + local;
-    const int after = g.tiles_m * g.tiles_n - whole;
     FusedWork w;
-    w.cut = tail && g.split_k > 1;
-    w.slice = tail ? id / after : 0;
-    w.slot = tail ? id % after : 0;
-    const int t = tail ? whole + w.slot : id;
-    const int width = g.group_m * g.tiles_n, first_m = t / width * g.group_m;
-    const int rows = g.tiles_m - first_m < g.group_m ? g.tiles_m - first_m : g.group_m;
-    w.tm = first_m + t % width % rows;
-    w.tn = t % width / rows;
+    w.low = LOW > 0 && rest;
+    const int tiles_m = w.low ? a.tail.tiles_m : g.tiles_m, tiles_n = w.low ? a.tail.tiles_n : g.tiles_n;
+    const int sliced = w.low ? 1 : rest ? tiles_m * tiles_n - a.whole : 1;
+    w.slice = w.low || !rest ? 0 : id / sliced;
+    w.slot = w.low || !rest ? 0 : id % sliced;
+    w.slices = w.low || !rest ? 1 : g.split_k;
+    const int t = w.low || !rest ? id : a.whole + w.slot;
+    const int width = g.group_m * tiles_n, first_m = t / width * g.group_m;
+    const int rows = tiles_m - first_m < g.group_m ? tiles_m - first_m : g.group_m;
+    const int tm = first_m + t % width % rows, tn = t % width / rows;
+    // DW: tile rows from `half` on are the second matrix's.  The lower tiles begin at a row of the matrix that the
+    // others leave off in, and at the first row of a matrix after it.
+    const int half = w.low ? a.tail.half : a.half;
+    w.which = tm >= half;
+    const int64_t row0 = w.low && !(w.which && half > 0) ? a.tail.row : 0;
+    w.m0 = row0 + int64_t(w.which ? tm - half : tm) * (w.low ? LOW : BM);
+    w.n0 = (w.low ? a.tail.col : 0) + int64_t(tn) * COLS;
     const int chunk = int(g.k_chunk / 64);
-    w.first = w.cut ? w.slice * chunk : 0;
-    w.count = w.cut && w.first + chunk < all ? chunk : all - w.first;
+    w.first = w.slices > 1 ? w.slice * chunk : 0;
+    w.count = w.slices > 1 && w.first + chunk < all ? chunk : all - w.first;
     return w;
 }
 
@@ -244,7 +257,7 @@ __device__ __forceinline__ FusedWork fused_work(const KernelArgs &g, int whole, 
 // the accesses are ordered).  True in every thread of the workgroup that holds the whole sums.
 // ---------------------------------------------------------------------------
 template <int THREADS, int TM, int TN>
-__device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[TM][TN], int slot, int slice, int64_t rows, int &flag) {
+__device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[TM][TN], int slot, int slice, int slices, int64_t rows, int &flag) {
     constexpr uint32_t SLICE = uint32_t(TM * TN * 16 * 4) * THREADS;
     const __amdgpu_buffer_rsrc_t parts = mx_parts(g, slot, SLICE);
     const uint32_t off = threadIdx.x * 16;
@@ -261,7 +274,12 @@ __device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[
                 if (32 * i + 8 * q < rows)
                     mx_store_part(parts, at(slice, i, j, q),
                                   f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
-    if (!mx_last_slice(g, slot, flag)) return false;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        flag = __hip_atomic_fetch_add(&g.counters[slot], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == unsigned(slices - 1);
+    __syncthreads();
+    if (flag == 0) return false;
     // ((part 0 + part 1) + ...) + own + ... : own stays in its registers, what comes before it is added up beside them.
     // FRAGMENTS fragments of WAYS slices on the way at once, as many registers as a tile of that size leaves.
     constexpr int F = TM * TN;
@@ -301,7 +319,7 @@ __device__ __forceinline__ bool sum_slices(const KernelArgs &g, f32x16_t (&acc)[
         } else {
             pass(f0_c, count_c, std::integral_constant<int, 1>{}, 0, slice, add);
         }
-        pass(f0_c, count_c, ways_c, slice + 1, g.split_k, add);
+        pass(f0_c, count_c, ways_c, slice + 1, slices, add);
     };
     constexpr int FRAGMENTS = F <= 4 ? F : 2, WAYS = F <= 2 ? 4 : 1;
     static_assert(F % FRAGMENTS == 0, "whole groups");

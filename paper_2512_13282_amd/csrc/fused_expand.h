@@ -88,7 +88,7 @@ __device__ __forceinline__ u32x4_t load8_any(const uint16_t *p) {
 // taken one after the other (a decode batch's rows of weights have to be read for each of its requests anyway), each as
 // a product of the 32 rows, of which only the adapter's own take the result: rows are chosen, not multiplied
 // by zeros, so an infinity or a NaN in one request's adapter stays out of the others'.  h does not depend on the
-// adapter and is read once for every 16 ranks; the matrices of four adapters are on their way at once, for what
+// adapter and is read once for every 16 ranks; the matrices of two to four adapters are on their way at once, for what
 // a batch of many requests waits for is their latency.  h keeps its fp32 value in two bf16 parts (2^-16 left
 // out, a bf16 result's half step being 2^-9), three and so all of it for an fp32 result.  Runs ahead of the
 // K loop, while the first stages are on their way.
@@ -164,7 +164,7 @@ __device__ __forceinline__ void expand_adapters(const FusedArgs &a, f32x16_t (&a
             if (own[I] >= 0) load_h(a, r0 + 32 * I + l32, k0, left, v);
             u32x4_t part[3];
             split_bf16(v, part);
-            constexpr int B = 4;                                 // adapters on the way at once
+            constexpr int B = TM > 3 ? 2 : 4;                    // adapters on the way at once
             uint32_t pending = all[I];
             while (pending != 0u) {
                 u32x4_t w[B][TN];

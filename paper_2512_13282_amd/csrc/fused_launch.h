@@ -26,9 +26,11 @@ hipError_t launch_fused_op(int32_t cfg, const FusedArgs &a, int64_t grid, hipStr
     const dim3 g{unsigned(grid)};
     switch (cfg) {
         case 0: hipLaunchKernelGGL((fused_tile_kernel<OP, 64, 128, 2, 2, 2, 3>), g, dim3(256), 0, s, a); break;
-        case 1: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 1, 1>), g, dim3(512), 0, s, a); break;
-        case 2: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 2, 1>), g, dim3(512), 0, s, a); break;
-        case 3: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 2, 2>), g, dim3(512), 0, s, a); break;
+        case 1: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 1, 1, 0, 0>), g, dim3(512), 0, s, a); break;
+        case 2: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 2, 1, 0, 0>), g, dim3(512), 0, s, a); break;
+        case 3: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 2, 2, 0, 0>), g, dim3(512), 0, s, a); break;
+        case 4: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 2, 2, 2, 1>), g, dim3(512), 0, s, a); break;
+        case 5: hipLaunchKernelGGL((fused_pingpong_kernel<OP, 2, 2, 1, 1>), g, dim3(512), 0, s, a); break;
         default:
             if constexpr (OP == FUSED_GATED || OP == FUSED_ADAPT) {
                 // Whether any 16 bytes of a row may lie off a dword.

@@ -40,17 +40,24 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     const int64_t cols = op == FUSED_GATED ? c.bn / 2 : c.bn;
     const bool any = fused_any_address(plan.config);
     const int64_t tm = (a.g.M + c.bm - 1) / c.bm * (op == FUSED_DW ? a.pairs : 1), tn = (a.g.N + cols - 1) / cols;
-    const int64_t cut = tm * tn - plan.whole, grid = plan.whole + cut * plan.split_k;
+    const int64_t sliced = plan.split_k > 1 ? tm * tn - plan.whole : 0;
+    int64_t grid = plan.whole + sliced * plan.split_k;
     a.g.k_chunk = plan.k_chunk;
     a.g.split_k = plan.split_k;
     a.whole = plan.whole;
-    a.g.tiles_m = int32_t(tm);
-    a.g.tiles_n = int32_t(tn);
+    a.half = op == FUSED_DW ? int32_t((a.g.M + c.bm - 1) / c.bm) : INT32_MAX;
+    if (c.low > 0) {
+        const FusedTail t = fused_tail(op, a.pairs, a.g.M, a.g.N, plan);
+        a.tail = FusedArgs::Tail{t.row, t.col, int32_t(t.tiles_m), int32_t(t.tiles_n), op == FUSED_DW ? int32_t(t.half) : INT32_MAX};
+        grid += t.tiles;
+    }
+    a.g.tiles_m = int32_t(plan.tail_rows > 0 ? plan.tail_rows : tm);
+    a.g.tiles_n = int32_t(plan.tail_cols > 0 ? plan.tail_cols : tn);
     a.g.group_m = 4;
     a.g.reduce_in_kernel = REDUCE_LAST_SLICE;
 
     // Scratch: the K slices' sums, the planes of h, and aligned copies of operands that need one.
-    const int64_t partial = a.g.split_k > 1 ? cut * plan.split_k * c.bm * c.bn * 4 : 0;
+    const int64_t partial = a.g.split_k > 1 ? sliced * plan.split_k * c.bm * c.bn * 4 : 0;
     const bool at = op == FUSED_DW, bt = op == FUSED_GATED || op == FUSED_ADAPT;
     const int64_t a_rows = at ? a.g.K : a.g.M, a_cols = at ? a.g.M : a.g.K;
     const int64_t b_rows = bt ? a.g.N : a.g.K, b_cols = bt ? a.g.K : a.g.N;
@@ -69,7 +76,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     const bool sum_h = shrink != nullptr && shrink->slices > 1 && (shrink->h != nullptr || !fused_few_rows(plan.config));
     const bool own_h = shrink != nullptr && shrink->h == nullptr && sum_h;
     const int64_t planes = shrink == nullptr || (shrink->h != nullptr && shrink->slices == 1) ? 0 : up16((shrink->slices + (own_h ? 1 : 0)) * shrink->plane * 4);
-    const int64_t counted = a.g.split_k > 1 ? cut : 0, h_counted = sum_h ? int64_t(shrink->blocks) * shrink->groups : 0;
+    const int64_t counted = sliced, h_counted = sum_h ? int64_t(shrink->blocks) * shrink->groups : 0;
 
     WorkspaceHold hold;                  // over the copies, the adapters' first product and the product
     if (partial + copied + planes > 0) {

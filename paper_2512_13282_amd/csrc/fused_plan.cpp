@@ -4,16 +4,18 @@
 namespace gemm {
 
 const FusedConfig kFusedConfigs[] = {
-    {64, 128, 4, 2, 4096, "fused_64x128_2x2"},
-    {128, 256, 8, 1, 4096, "fused_pingpong_128x256"},
-    {192, 256, 8, 1, 4096, "fused_pingpong_192x256"},
-    {256, 256, 8, 1, 16, "fused_pingpong_256x256"},
-    {16, 16, 8, 2, 1, "fused_decode_16"},
-    {32, 16, 8, 2, 1, "fused_decode_32"},
-    {48, 16, 8, 2, 1, "fused_decode_48"},
-    {64, 16, 8, 2, 1, "fused_decode_64"},
-    {16, 16, 8, 1, 1, "fused_stream_16"},
-    {32, 16, 8, 1, 1, "fused_stream_32"},
+    {64, 128, 4, 2, 4096, 0, "fused_64x128_2x2"},
+    {128, 256, 8, 1, 4096, 0, "fused_pingpong_128x256"},
+    {192, 256, 8, 1, 4096, 0, "fused_pingpong_192x256"},
+    {256, 256, 8, 1, 16, 0, "fused_pingpong_256x256"},
+    {256, 256, 8, 1, 1, 192, "fused_pingpong_256x256_192"},
+    {256, 256, 8, 1, 1, 128, "fused_pingpong_256x256_128"},
+    {16, 16, 8, 2, 1, 0, "fused_decode_16"},
+    {32, 16, 8, 2, 1, 0, "fused_decode_32"},
+    {48, 16, 8, 2, 1, 0, "fused_decode_48"},
+    {64, 16, 8, 2, 1, 0, "fused_decode_64"},
+    {16, 16, 8, 1, 1, 0, "fused_stream_16"},
+    {32, 16, 8, 1, 1, 0, "fused_stream_32"},
 };
 const int32_t kFusedNumConfigs = sizeof(kFusedConfigs) / sizeof(kFusedConfigs[0]);
 
@@ -28,18 +30,29 @@ bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_
     const FusedConfig &c = kFusedConfigs[config];
     if (split > c.most_slices || (fused_few_rows(config) && M > c.bm)) return false;
     const int64_t stages = ceil_div(K, 64) * (op == FUSED_DX ? 2 : 1);
-    const int64_t tiles = ceil_div(M, c.bm) * pairs * ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn);
-    // Tiles that fill whole rounds of the compute units keep all of K; slices are for the rest.
+    const int64_t tm = ceil_div(M, c.bm) * pairs, tn = ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn), tiles = tm * tn;
+    if (tiles > INT32_MAX) return false;
+    // Tiles that fill whole rounds of the compute units keep all of K.
     const int64_t slots = int64_t(kCUs) * c.occupancy, rest = tiles % slots;
     const int64_t chunk = stages > 0 && rest > 0 ? ceil_div(stages, split) : stages > 0 ? stages : 1;
     out->config = config;
     out->k_chunk = 64 * chunk;
     out->split_k = int32_t(stages > 0 ? ceil_div(stages, chunk) : 1);
-    const int64_t cut = out->split_k > 1 ? rest : 0;
-    if (tiles > INT32_MAX) return false;
-    out->whole = int32_t(tiles - cut);
+    out->tail_rows = out->tail_cols = 0;
+    const int64_t sliced = out->split_k > 1 ? rest : 0;
+    int64_t groups = tiles - sliced + sliced * out->split_k;
+    out->whole = int32_t(tiles - sliced);
+    if (c.low > 0) {
+        // The tile columns or rows that fill whole rounds, whichever wastes less; lower tiles over the others.
+        const int64_t full = tiles - rest, cols = full / tm, rows = full / tn;
+        if (full == 0 || rest == 0) return false;
+        if (cols * tm >= rows * tn) out->tail_cols = int32_t(cols);
+        else out->tail_rows = int32_t(rows);
+        out->whole = int32_t(out->tail_cols > 0 ? cols * tm : rows * tn);
+        groups = out->whole + fused_tail(op, pairs, M, N, *out).tiles;
+    }
     // A tile's partial sums are addressed with 32 bits, and a grid holds fewer than 2^32 threads.
-    return int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && tiles - cut + cut * out->split_k <= UINT32_MAX / (64 * c.waves);
+    return int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && groups <= UINT32_MAX / (64 * c.waves);
 }
 
 // Modelled microseconds of a plan, without the launch.
@@ -51,6 +64,27 @@ double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t, con
 }
 
 }  // namespace
+
+FusedTail fused_tail(FusedOp op, int32_t pairs, int64_t M, int64_t N, const FusedPlan &p) {
+    const FusedConfig &c = kFusedConfigs[p.config];
+    const int64_t width = op == FUSED_GATED ? c.bn / 2 : c.bn, per = ceil_div(M, c.bm), tn = ceil_div(N, width);
+    FusedTail t{};
+    if (p.tail_cols > 0) {
+        t.col = p.tail_cols * width;
+        t.half = ceil_div(M, c.low);
+        t.tiles_m = t.half * pairs;
+        t.tiles_n = tn - p.tail_cols;
+    } else {
+        const bool second = p.tail_rows >= per;                  // the rows left are all the second matrix's
+        t.row = (second ? p.tail_rows - per : p.tail_rows) * c.bm;
+        const int64_t left = ceil_div(M - t.row, c.low);
+        t.half = second ? 0 : left;
+        t.tiles_m = second ? left : left + (pairs == 2 ? ceil_div(M, c.low) : 0);
+        t.tiles_n = tn;
+    }
+    t.tiles = t.tiles_m * t.tiles_n;
+    return t;
+}
 
 bool fused_has(FusedOp op, int32_t config) {
     if (op < 0 || op >= FUSED_OPS || config < 0 || config >= kFusedNumConfigs) return false;

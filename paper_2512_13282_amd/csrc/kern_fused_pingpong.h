@@ -18,8 +18,7 @@ namespace gemm {
 // B's, and of A0 and A1 two and one or one and two.
 // ---------------------------------------------------------------------------
 template <int OP, int H0, int H1>
-__global__ __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_waves_per_eu(2, 2)))
-void fused_pingpong_kernel(FusedArgs a) {
+__device__ __forceinline__ void fused_pingpong_tile(const FusedArgs &a, const FusedWork &work, uint8_t *buffers, int wave, int lane) {
     using L = FusedLayout<OP>;
     constexpr int BK = 64, WAVES = 8, TM = H0 + H1, TN = 2, BM = 64 * TM, BN = 256, HALF = 128;
     constexpr int A0_BYTES = 64 * H0 * 128, A1_BYTES = 64 * H1 * 128, B_BYTES = HALF * 128;
@@ -30,21 +29,12 @@ void fused_pingpong_kernel(FusedArgs a) {
     enum { U_B0, U_A0, U_B1, U_A1 };                       // units of a stage, in load order
     constexpr int AT_B0 = 0, AT_A0 = B_BYTES, AT_B1 = AT_A0 + A0_BYTES, AT_A1 = AT_B1 + B_BYTES;
 
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][STAGE];
 
-    const int tid = int(threadIdx.x), lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint8_t *const lds[2] = {buffers, buffers + STAGE};
     const int grp = wave >> 2, wave_n = wave & 3;
-
+    const int64_t M = a.g.M, N = a.g.N, m0 = work.m0, n0 = work.n0;
     const int K = int(a.g.K), one = (K + BK - 1) / BK;      // stages of one product
-    const FusedWork work = fused_work(a.g, a.whole, OP == FUSED_DX ? 2 * one : one);
-    int tm = work.tm;
-    const int tn = work.tn, first = work.first, ns = work.count;
-    const int which = OP == FUSED_DW && tm >= a.g.tiles_m / a.pairs;
-    if (which) tm -= a.g.tiles_m / a.pairs;
-    const int64_t M = a.g.M, N = a.g.N;
-    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * COLS;
-
+    const int which = work.which, first = work.first, ns = work.count;
     const uint8_t *const a_src = static_cast<const uint8_t *>(which ? a.A2 : a.g.A);
     const int lda_b = int(which ? a.lda2 : a.g.lda) * 2, lda2_b = int(a.lda2) * 2;       // at most 4 MiB
     const int ldb_b = int(a.g.ldb) * 2, ldb2_b = int(a.ldb2) * 2;
@@ -262,8 +252,27 @@ void fused_pingpong_kernel(FusedArgs a) {
         if (grp == 0) asm volatile("s_barrier" ::: "memory");
     }
     stage_barrier();                                       // drains the loads past the end, by every wave
-    if (work.cut && !sum_slices<512>(a.g, acc, work.slot, work.slice, M - (m0 + grp * (32 * TM)), *reinterpret_cast<int *>(lds[0]))) return;
+    if (work.slices > 1 &&
+        !sum_slices<512>(a.g, acc, work.slot, work.slice, work.slices, M - (m0 + grp * (32 * TM)), *reinterpret_cast<int *>(lds[0])))
+        return;
     store_fused<OP, 512, HALF>(a, acc, which, m0 + grp * (32 * TM), n0 + wave_n * 32, lane);
+}
+
+// Tiles of 64 (H0 + H1) rows, and where L0 > 0 lower ones of 64 (L0 + L1) rows in a last round.
+template <int OP, int H0, int H1, int L0, int L1>
+__global__ __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_waves_per_eu(2, 2)))
+void fused_pingpong_kernel(FusedArgs a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t buffers[2 * (64 * (H0 + H1) + 256) * 128];
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), lane = int(threadIdx.x) & 63;
+    const int one = (int(a.g.K) + 63) / 64;
+    const FusedWork work = fused_work<64 * (H0 + H1), 64 * (L0 + L1), 256 / FusedLayout<OP>::HALVES>(a, OP == FUSED_DX ? 2 * one : one);
+    if constexpr (L0 > 0) {
+        if (work.low) {
+            fused_pingpong_tile<OP, L0, L1>(a, work, buffers, wave, lane);
+            return;
+        }
+    }
+    fused_pingpong_tile<OP, H0, H1>(a, work, buffers, wave, lane);
 }
 
 }  // namespace gemm

@@ -64,16 +64,12 @@ void fused_tile_kernel(FusedArgs a) {
     const int tid = int(threadIdx.x), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wave_m = wave / WN, wave_n = wave % WN;
-    const int one = int((a.g.K + BK - 1) / BK);                 // stages of one product
-    const FusedWork work = fused_work(a.g, a.whole, OP == FUSED_DX ? 2 * one : one);
-    int tm = work.tm;
-    const int tn = work.tn, first = work.first, nk = work.count;
-    const int which = OP == FUSED_DW && tm >= a.g.tiles_m / a.pairs;
-    if (which) tm -= a.g.tiles_m / a.pairs;
-    const int64_t M = a.g.M, N = a.g.N, K = a.g.K;
     constexpr int COLS = BN / L::HALVES;                         // output columns of a tile
-    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * COLS;
-
+    const int64_t M = a.g.M, N = a.g.N, K = a.g.K;
+    const int one = int((K + BK - 1) / BK);                     // stages of one product
+    const FusedWork work = fused_work<BM, 0, COLS>(a, OP == FUSED_DX ? 2 * one : one);
+    const int64_t m0 = work.m0, n0 = work.n0;
+    const int which = work.which, first = work.first, nk = work.count;
     const uint8_t *const a_src = static_cast<const uint8_t *>(which ? a.A2 : a.g.A);
     const int64_t lda_b = (which ? a.lda2 : a.g.lda) * 2, lda2_b = a.lda2 * 2;
     const int64_t ldb_b = a.g.ldb * 2, ldb2_b = a.ldb2 * 2;
@@ -233,7 +229,9 @@ void fused_tile_kernel(FusedArgs a) {
         if (work.slice == 0) expand_adapters<OP == FUSED_ADAPT, HALF>(a, acc, m0 + wrow0, n0 + wcol0, lane);
     }
     stage_barrier();       // drains the loads past the end before sum_slices borrows a word of the buffers
-    if (work.cut && !sum_slices<THREADS>(a.g, acc, work.slot, work.slice, M - (m0 + wrow0), *reinterpret_cast<int *>(lds[0]))) return;
+    if (work.slices > 1 &&
+        !sum_slices<THREADS>(a.g, acc, work.slot, work.slice, work.slices, M - (m0 + wrow0), *reinterpret_cast<int *>(lds[0])))
+        return;
     store_fused<OP, THREADS, HALF>(a, acc, which, m0 + wrow0, n0 + wcol0, lane);
 }
 

@@ -33,7 +33,7 @@ SIZES = [(1, 8, 8, 0, 0), (1, 1, 1, 0, 0), (3, 7, 5, 0, 0), (17, 33, 65, 0, 0), 
          (100, 264, 320, 0, 0), (130, 250, 1000, 8, 0), (257, 520, 136, 0, 0), (300, 513, 511, 5, 1), (1, 1000, 2048, 0, 0),
          (16, 512, 4104, 0, 0), (511, 264, 64, 0, 0),
          # More tiles than compute units: whole ones, and slices of the rest.
-         (1100, 2200, 328, 0, 0), (4340, 4100, 264, 0, 4)]
+         (1100, 2200, 328, 0, 0), (4340, 4100, 264, 0, 4), (2100, 8200, 72, 0, 0), (72, 4100, 4340, 0, 0)]
 ids = dict(ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else str(v))
 
 
