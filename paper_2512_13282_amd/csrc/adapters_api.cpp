@@ -49,8 +49,10 @@ int product(int op, int64_t M, int64_t N, int64_t K, const uint16_t *X, int64_t 
     gemm::FusedPlan plan{};
     const gemm::FusedOp fused = forward ? gemm::FUSED_ADAPT : gemm::FUSED_ADAPT_DX;
     if (K > gemm::kFusedMostSize) return GEMM_ERR_UNSUPPORTED;
+    if (N > gemm::kFusedMostSize) return GEMM_ERR_UNSUPPORTED;
     if (N > 0) {
-        const int planned = gemm::fused_plan_for(fused, 1, M, N, K, g_forced[op], &plan);
+        const int64_t copied = gemm::fused_copied(X, ldx, M, K, true) + gemm::fused_copied(W, ldw, forward ? N : K, forward ? K : N, forward);
+        const int planned = gemm::fused_plan_for(fused, 1, M, N, K, copied, g_forced[op], &plan);
         if (planned != GEMM_OK) return planned;
         if (!gemm::fused_any_address(plan.config) &&
             (!gemm::fused_copyable(X, ldx, M, K, true) || !gemm::fused_copyable(W, ldw, forward ? N : K, forward ? K : N, forward)))

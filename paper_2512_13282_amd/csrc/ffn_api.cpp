@@ -38,8 +38,12 @@ bool sound(const Region (&in)[I], const Region (&out)[O]) {
 int launch(int op, FusedArgs &a, int64_t M, int64_t N, int64_t K, bool bf16_out, void *stream) {
     const bool at = kOps[op] == gemm::FUSED_DW, bt = kOps[op] == gemm::FUSED_GATED;
     const int64_t a_rows = at ? K : M, a_cols = at ? M : K, b_rows = bt ? N : K, b_cols = bt ? K : N;
+    if (M > gemm::kFusedMostSize || N > gemm::kFusedMostSize || K > gemm::kFusedMostSize) return GEMM_ERR_UNSUPPORTED;
+    const int64_t copied = gemm::fused_copied(a.g.A, a.g.lda, a_rows, a_cols, !at) + gemm::fused_copied(a.g.B, a.g.ldb, b_rows, b_cols, bt) +
+                           (a.A2 != nullptr ? gemm::fused_copied(a.A2, a.lda2, a_rows, a_cols, !at) : 0) +
+                           (a.B2 != nullptr ? gemm::fused_copied(a.B2, a.ldb2, b_rows, b_cols, bt) : 0);
     gemm::FusedPlan plan;
-    const int planned = gemm::fused_plan_for(kOps[op], kPairs[op], M, N, K, g_forced[op], &plan);
+    const int planned = gemm::fused_plan_for(kOps[op], kPairs[op], M, N, K, copied, g_forced[op], &plan);
     if (planned != GEMM_OK) return planned;
     if (!gemm::fused_any_address(plan.config) && (!gemm::fused_copyable(a.g.A, a.g.lda, a_rows, a_cols, !at) || !gemm::fused_copyable(a.g.B, a.g.ldb, b_rows, b_cols, bt) ||
         (a.A2 != nullptr && !gemm::fused_copyable(a.A2, a.lda2, a_rows, a_cols, !at)) ||
@@ -172,7 +176,7 @@ int ffn_plan(int op, int64_t M, int64_t N, int64_t K, ffn_plan_info *out) {
     out->config = -1;
     if (M == 0 || N == 0) return GEMM_OK;
     gemm::FusedPlan plan;
-    const int rc = gemm::fused_plan_for(kOps[op], kPairs[op], M, N, K, g_forced[op], &plan);
+    const int rc = gemm::fused_plan_for(kOps[op], kPairs[op], M, N, K, 0, g_forced[op], &plan);
     if (rc != GEMM_OK) return rc;
     const gemm::FusedConfig &c = gemm::kFusedConfigs[plan.config];
     out->config = plan.config;

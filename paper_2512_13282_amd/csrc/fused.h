@@ -81,9 +81,9 @@ inline bool fused_any_address(int32_t config) { return config >= kFusedDecode &&
 // Whether a configuration is built for an operator.
 bool fused_has(FusedOp op, int32_t config);
 
-// The plan for a product; config >= 0 and split > 0 say which one to take instead.  False where
-// none (the one named does not) takes the sizes.
-bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out);
+// The plan for a product, where `copied` bytes of its operands are not loadable (below); config >= 0 and split > 0 say which
+// one to take instead.  False where none (the one named does not) takes the sizes.
+bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int64_t copied, int32_t config, int32_t split, FusedPlan *out);
 
 // The tile kernels load 16 aligned bytes at a time straight into LDS, at 32-bit offsets within a
 // tile: an operand whose rows lie otherwise is copied first.  Along the sum a row is whole pieces,

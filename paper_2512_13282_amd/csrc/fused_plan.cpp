@@ -22,8 +22,42 @@ const int32_t kFusedNumConfigs = sizeof(kFusedConfigs) / sizeof(kFusedConfigs[0]
 namespace {
 
 constexpr int kCUs = 256;
+constexpr int32_t kFused128 = 1, kFused192 = 2, kFused256 = 3;     // rows of kFusedConfigs that the lower tiles' plans use too
+
+// The model's figures: a least-squares fit of modelled_us to the logarithms of the times of every configuration and number
+// of slices at 840 drawn shapes (rows 1 to 4096, widths of 64 to 14336, every operator).  They are to be fitted again where a
+// kernel changes.
+struct FusedFigures {
+    // Microseconds: a workgroup's start and end, a stage of 64 k of its tile alone on its compute unit and with the unit
+    // full, a last slice's sum and its share per 100 KB of partial sums.
+    double start_us, part_us, part_full_us, sum_us, sum_slice_us;
+};
+constexpr FusedFigures kFigures[] = {
+    {1.115, 0.335, 0.602, 3.846, 0.941},
+    {2.811, 0.670, 0.670, 4.436, 0.760},
+    {4.102, 0.885, 0.885, 4.870, 0.556},
+    {4.757, 1.104, 1.104, 4.369, 0.413},
+};
+// A stage's time by operator, over GATED's.
+constexpr double kPart[FUSED_OPS][4] = {
+    {1.000, 1.000, 1.000, 1.000}, {1.140, 1.184, 1.164, 1.190}, {1.000, 0.957, 0.906, 0.882},
+    {0.978, 1.071, 1.066, 1.102}, {0.932, 0.826, 0.827, 0.929}, {0.865, 0.779, 0.778, 0.797},
+};
+constexpr double kStore[FUSED_OPS] = {0.432, 0.376, 0.448, 0.090, 0.228, 0.471};   // a megabyte of results (GRAD: and of G and U)
+constexpr double kLaunch = 3.1, kRate = 4.0;                                       // megabytes in a microsecond
+// The kernels for few rows: the start, a megabyte of weights and of A, 100 KB of both through one compute unit, 1000 k.
+struct FewFigures { double start_us, weights_us, x_us, own_us, k_us; };
+constexpr FewFigures kFew[] = {
+    {4.195, 0.167, 0.066, 2.425, 0.000}, {3.644, 0.162, 0.128, 2.434, 0.251}, {3.559, 0.201, 0.107, 2.488, 0.423},
+    {3.455, 0.261, 0.073, 2.772, 0.474}, {4.959, 0.168, 0.000, 0.733, 0.000}, {4.742, 0.187, 0.039, 0.998, 0.000},
+};
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+double out_mb(FusedOp op, int32_t pairs, int64_t M, int64_t N) {
+    static constexpr int kBytes[FUSED_OPS] = {6, 10, 2, 4, 2, 2};
+    return double(kBytes[op]) * pairs * double(M) * double(N) / 1e6;
+}
 
 bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
     if (config < 0 || config >= kFusedNumConfigs || !fused_has(op, config)) return false;
@@ -55,12 +89,52 @@ bool evaluate(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_
     return int64_t(out->split_k) * c.bm * c.bn * 4 <= INT32_MAX && groups <= UINT32_MAX / (64 * c.waves);
 }
 
-// Modelled microseconds of a plan, without the launch.
-double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t, const FusedPlan &p) {
+double moved_mb(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K) {
+    const double m = double(M), n = double(N), k = double(K), two = op == FUSED_DX ? 2.0 : double(pairs);
+    return (2.0 * two * m * k + 2.0 * (op == FUSED_GATED || op == FUSED_DX ? 2.0 : 1.0) * n * k) / 1e6 + out_mb(op, pairs, M, N);
+}
+
+// Rounds of `groups` workgroups with `stages` stages each.
+double rounds_us(FusedOp op, int32_t config, double groups, double stages) {
+    const FusedConfig &c = kFusedConfigs[config];
+    const FusedFigures &f = kFigures[config];
+    const double slots = double(kCUs) * c.occupancy, full = double(int64_t(groups / slots)), rest = groups - full * slots;
+    const double part = kPart[op][config];
+    const double alone = f.start_us + f.part_us * part * stages, shared = f.start_us + f.part_full_us * part * stages;
+    double t = full * (c.occupancy > 1 ? shared : alone);
+    if (rest > 0) {
+        const double per_cu = double(ceil_div(int64_t(rest), kCUs));     // on the fullest
+        t += per_cu <= 1 ? alone : alone + (shared - alone) * (per_cu - 1) / (c.occupancy - 1);
+    }
+    return t;
+}
+
+// Modelled microseconds of a plan, where `copied` bytes of the operands are not loadable.
+double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, const FusedPlan &p, int64_t copied) {
     const FusedConfig &c = kFusedConfigs[p.config];
-    const double tiles = double(ceil_div(M, c.bm)) * pairs * double(ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn));
-    const double groups = tiles * p.split_k, rounds = double(int64_t(groups / (kCUs * c.occupancy)) + 1);
-    return rounds * (2.0 + 0.4 * double(p.k_chunk) / 64) + (p.split_k > 1 ? 3.0 + 0.2 * p.split_k : 0.0);
+    // Operands copied to aligned rows first: a launch and both ways through memory.
+    const double copy = copied > 0 && !fused_any_address(p.config) ? 3.5 + 2.0 * double(copied) / 4.5e6 : 0.0;
+    if (fused_few_rows(p.config)) {
+        const FewFigures &f = kFew[p.config - kFusedDecode];
+        const double rows = double(N) * (op == FUSED_GATED ? 2 : 1), groups = double(ceil_div(int64_t(rows), 16));
+        const double tokens = double(M < c.bm ? M : c.bm), weights = 2.0 * rows * double(K) / 1e6, x = groups * tokens * double(K) * 2 / 1e6;
+        const double per_cu = double(ceil_div(int64_t(groups), kCUs)), own = per_cu * 2.0 * (16 + tokens) * double(K) / 1e5;
+        const double all = f.weights_us * weights + f.x_us * x, one = f.own_us * own;
+        return f.start_us + (all > one ? all : one) + f.k_us * double(K) / 1e3 + copy;
+    }
+    const double stages = double(ceil_div(K, 64)) * (op == FUSED_DX ? 2 : 1), chunk = double(p.k_chunk) / 64;
+    const int64_t tiles = ceil_div(M, c.bm) * pairs * ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn);
+    const int32_t as = c.low > 0 ? kFused256 : p.config;
+    double t = rounds_us(op, as, double(p.whole), stages) + kStore[op] * out_mb(op, pairs, M, N);
+    if (c.low > 0) t += rounds_us(op, c.low == 192 ? kFused192 : kFused128, double(fused_tail(op, pairs, M, N, p).tiles), stages);
+    if (p.split_k > 1) {
+        // The slices, the last one's sum, and every slice's partial sums out and back.
+        const FusedFigures &f = kFigures[as];
+        const double groups = double(tiles - p.whole) * p.split_k, rows = M < 8 ? 8 : M < c.bm ? double(M) : double(c.bm);
+        t += rounds_us(op, as, groups, chunk) + f.sum_us + f.sum_slice_us * p.split_k * rows * c.bn * 4 / 1e5 + groups * rows * c.bn * 8 / 4.5e6;
+    }
+    const double memory = moved_mb(op, pairs, M, N, K) / kRate;
+    return kLaunch + (t > memory ? t : memory) + copy;
 }
 
 }  // namespace
@@ -91,7 +165,7 @@ bool fused_has(FusedOp op, int32_t config) {
     return !fused_few_rows(config) || op == FUSED_GATED || op == FUSED_ADAPT;
 }
 
-bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int32_t config, int32_t split, FusedPlan *out) {
+bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, int64_t copied, int32_t config, int32_t split, FusedPlan *out) {
     if (config >= 0) return evaluate(op, pairs, M, N, K, config, split > 0 ? split : 1, out);
     static const int32_t kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
     double best = 0;
@@ -103,7 +177,7 @@ bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, in
             if (!evaluate(op, pairs, M, N, K, c, split > 0 ? split : s, &p)) break;
             if (p.split_k == seen) continue;                     // the same slices again
             seen = p.split_k;
-            const double t = modelled_us(op, pairs, M, N, K, p);
+            const double t = modelled_us(op, pairs, M, N, K, p, copied);
             if (!found || t < best) {
                 best = t;
                 *out = p;
