@@ -55,6 +55,11 @@ int ffn_gated_grad_bf16(int64_t M, int64_t N, int64_t K, const uint16_t *dY, int
                         const uint16_t *G, int64_t ldg, const uint16_t *U, int64_t ldu, int act,
                         uint16_t *dG, int64_t lddg, uint16_t *dU, int64_t lddu, uint16_t *H, int64_t ldh, void *stream);
 
+/* The same from the gradient dH of H itself (M x N, bf16), where something else than a projection follows:
+ * dG = dH * U * act'(G), dU = dH * act(G), for any dH. */
+int ffn_gated_bwd_bf16(int64_t M, int64_t N, const uint16_t *dH, int64_t lddh, const uint16_t *G, int64_t ldg,
+                       const uint16_t *U, int64_t ldu, int act, uint16_t *dG, int64_t lddg, uint16_t *dU, int64_t lddu, void *stream);
+
 /* dX (M x N) = dG Wg + dU Wu, dG and dU M x K, Wg and Wu K x N: both products in one sum. */
 int ffn_gated_dx_f32(int64_t M, int64_t N, int64_t K, const uint16_t *dG, int64_t lddg, const uint16_t *Wg, int64_t ldwg,
                      const uint16_t *dU, int64_t lddu, const uint16_t *Wu, int64_t ldwu, float *dX, int64_t lddx, void *stream);

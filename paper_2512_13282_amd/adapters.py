@@ -11,7 +11,8 @@ addresses.  The torch helpers read addresses, strides and the current stream and
 * ``linear_adapters_dw(x, dy, h, dh, index, n)``: every adapter's gradients, from what the two above leave with
   ``keep=True``.
 
-``Adapters`` holds n adapters of one rank; one of a lower rank has zeros behind its own.
+``Adapters`` holds n adapters of one rank; one of a lower rank has zeros behind its own.  ``AdaptersLinear``
+(feedforward.py) is the projection as a module.
 """
 from __future__ import annotations
 
@@ -99,6 +100,17 @@ class _Helpers:
         backward = {f32: fns["adapters_linear_f32"], bf16: fns["adapters_linear_bf16"]}
         dws = {f32: fns["adapters_dw_f32"], bf16: fns["adapters_dw_bf16"]}
 
+        current, device_of = torch._C._cuda_getDevice, torch.cuda.device
+
+        def call(device, fn, *args):
+            if current() == device:
+                rc = fn(*args, raw_stream(device))
+            else:                                           # the entry points work on the current device
+                with device_of(device):
+                    rc = fn(*args, raw_stream(device))
+            if rc != ok:
+                raise _b.GemmError(rc)
+
         def matrix(x, device=None):
             if x.dtype != bf16:
                 raise TypeError("expected bfloat16 operands")
@@ -147,10 +159,8 @@ class _Helpers:
             H = empty(M, r, dtype=f32, device=X.device) if keep else None
             held = AdaptersSet(n, r, A.data_ptr() or None, *_stack(A, n, r, n_in), B.data_ptr() or None, *_stack(B, n, n_out, r),
                                None if scale is None else scale.data_ptr() or None)
-            rc = table[dtype](M, N, K, X.data_ptr(), _ld(X.stride(), M, K), W.data_ptr(), _ld(W.stride(), n_out, n_in), held, where,
-                              out.data_ptr(), ldy, H.data_ptr() if keep else None, raw_stream(device))
-            if rc != ok:
-                raise _b.GemmError(rc)
+            call(device, table[dtype], M, N, K, X.data_ptr(), _ld(X.stride(), M, K), W.data_ptr(), _ld(W.stride(), n_out, n_in), held, where,
+                 out.data_ptr(), ldy, H.data_ptr() if keep else None)
             return (out, H) if keep else out
 
         def weight_gradients(x, dy, h, dh, index, n, out_dtype):
@@ -171,10 +181,8 @@ class _Helpers:
             if dtype not in dws:
                 raise TypeError("results are bfloat16 or float32")
             dA, dB = empty(n, r, K, dtype=dtype, device=x.device), empty(n, N, r, dtype=dtype, device=x.device)
-            rc = dws[dtype](M, N, K, n, r, x.data_ptr(), _ld(x.stride(), M, K), dy.data_ptr(), _ld(dy.stride(), M, N), h.data_ptr(),
-                            dh.data_ptr(), where, dA.data_ptr(), K or 1, r * K or 1, dB.data_ptr(), r or 1, N * r or 1, raw_stream(device))
-            if rc != ok:
-                raise _b.GemmError(rc)
+            call(device, dws[dtype], M, N, K, n, r, x.data_ptr(), _ld(x.stride(), M, K), dy.data_ptr(), _ld(dy.stride(), M, N), h.data_ptr(),
+                 dh.data_ptr(), where, dA.data_ptr(), K or 1, r * K or 1, dB.data_ptr(), r or 1, N * r or 1)
             return dA, dB
 
         self.forward = lambda *args: linear(forward, True, *args)
@@ -214,6 +222,5 @@ def __getattr__(name):
     # The module, which needs torch at its definition.
     if name == "AdaptersLinear":
         from .feedforward import AdaptersLinear
-        globals()[name] = AdaptersLinear
         return AdaptersLinear
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

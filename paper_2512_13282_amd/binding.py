@@ -316,7 +316,7 @@ def mm_bf16_f32(A, B, out=None):
 # ---------------------------------------------------------------- operators of modules that build on this one
 _BY_MODULE = {
     "mx": ("MxMatrix", "linear_mx4", "linear_mx4_dx", "linear_mx8_dw", "pack_mx4", "pack_mx8", "unpack_mx"),
-    "ffn": ("gated_linear", "gated_linear_grad", "gated_linear_dx", "gated_linear_dw", "linear_dw"),
+    "ffn": ("gated_linear", "gated_linear_grad", "gated_linear_bwd", "gated_linear_dx", "gated_linear_dw", "linear_dw"),
     "adapters": ("Adapters", "linear_adapters", "linear_adapters_dx", "linear_adapters_dw"),
 }
 

@@ -140,6 +140,16 @@ int ffn_gated_grad_bf16(int64_t M, int64_t N, int64_t K, const uint16_t *dY, int
     return launch(FFN_OP_GRAD, a, M, N, K, true, stream);
 }
 
+int ffn_gated_bwd_bf16(int64_t M, int64_t N, const uint16_t *dH, int64_t lddh, const uint16_t *G, int64_t ldg, const uint16_t *U, int64_t ldu,
+                       int act, uint16_t *dG, int64_t lddg, uint16_t *dU, int64_t lddu, void *stream) {
+    if (M < 0 || N < 0 || !known(act)) return GEMM_ERR_INVALID_VALUE;
+    const Region in[] = {region(dH, M, N, lddh, 2), region(G, M, N, ldg, 2), region(U, M, N, ldu, 2)};
+    const Region out[] = {region(dG, M, N, lddg, 2), region(dU, M, N, lddu, 2)};
+    if (!sound(in, out)) return GEMM_ERR_INVALID_VALUE;
+    if (M == 0 || N == 0) return GEMM_OK;
+    return gemm::fused_status(gemm::launch_gated_bwd({M, N, dH, G, U, dG, dU, lddh, ldg, ldu, lddg, lddu, act}, stream));
+}
+
 int ffn_gated_dx_f32(int64_t M, int64_t N, int64_t K, const uint16_t *dG, int64_t lddg, const uint16_t *Wg, int64_t ldwg, const uint16_t *dU,
                      int64_t lddu, const uint16_t *Wu, int64_t ldwu, float *dX, int64_t lddx, void *stream) {
     return gated_dx(M, N, K, dG, lddg, Wg, ldwg, dU, lddu, Wu, ldwu, dX, lddx, false, stream);

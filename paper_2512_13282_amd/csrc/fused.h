@@ -94,7 +94,17 @@ inline bool fused_loadable(const void *p, int64_t ld, bool along_k, int64_t cols
            (!along_k || cols % 8 == 0);
 }
 
+// dG and dU of M x N from dH, G and U.
+struct GatedBwdArgs {
+    int64_t M, N;
+    const void *dH, *G, *U;
+    void *dG, *dU;
+    int64_t lddh, ldg, ldu, lddg, lddu;
+    int32_t act;
+};
+
 // Each queues its kernels on `stream` (a hipStream_t) and returns a LAUNCH_* value.
+int launch_gated_bwd(const GatedBwdArgs &a, void *stream);
 int launch_fused(const FusedArgs &a, FusedOp op, const FusedPlan &plan, void *stream);
 
 }  // namespace gemm

@@ -21,24 +21,26 @@ __device__ __forceinline__ u32x4_t load8_bf16(const uint16_t *p, int64_t left) {
     return v;
 }
 
-// Eight floats as bf16 parts whose sum they are: the upper 8 bits of each, the next 8, and the last 8 (24 bits
-// in all, so three parts are exact and two leave 2^-16).  An infinity or a NaN is its own first part.
+// Eight floats as bf16 parts whose sum they are: the upper 8 bits of each, what is left rounded to 8 bits, and what that leaves
+// (24 bits in all, so three parts are exact; two leave half a step of the second, 2^-16).  An infinity or a NaN is its own
+// first part.
 __device__ __forceinline__ void split_bf16(const float (&v)[8], u32x4_t (&part)[3]) {
-    uint32_t b[3][8];
+    uint32_t b[8];
+    float rest[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const uint32_t x = __builtin_bit_cast(uint32_t, v[e]);
         const bool finite = (x & 0x7f800000u) != 0x7f800000u;
-        const float rest = finite ? v[e] - __builtin_bit_cast(float, x & 0xffff0000u) : 0.0f;
-        const uint32_t y = __builtin_bit_cast(uint32_t, rest);
-        b[0][e] = finite || (x & 0x007fffffu) == 0u ? x : x | 0x00400000u;
-        b[1][e] = y;
-        b[2][e] = __builtin_bit_cast(uint32_t, rest - __builtin_bit_cast(float, y & 0xffff0000u));
+        b[e] = finite || (x & 0x007fffffu) == 0u ? x : x | 0x00400000u;
+        rest[e] = finite ? v[e] - __builtin_bit_cast(float, x & 0xffff0000u) : 0.0f;
     }
 #pragma unroll
-    for (int p = 0; p < 3; ++p)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) part[p][d] = perm(b[p][2 * d + 1], b[p][2 * d], 0x07060302u);
+    for (int d = 0; d < 4; ++d) {
+        const uint32_t second = pack_bf16(rest[2 * d], rest[2 * d + 1]);
+        part[0][d] = perm(b[2 * d + 1], b[2 * d], 0x07060302u);
+        part[1][d] = second;
+        part[2][d] = pack_bf16(rest[2 * d] - bf16_to_f32(second & 0xffffu), rest[2 * d + 1] - bf16_to_f32(second >> 16));
+    }
 }
 
 // Row t's h from element k on, the first `left` of eight, summed over its planes in their order.

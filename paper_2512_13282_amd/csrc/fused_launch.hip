@@ -126,6 +126,40 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     return e == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
 }
 
+// Eight columns of a row to a thread, at any address and stride.  Bound by memory: ten bytes an element.
+__global__ __launch_bounds__(256) void gated_bwd_kernel(GatedBwdArgs a) {
+    const int64_t pieces = (a.N + 7) / 8, total = a.M * pieces;
+    with_act(a.act, [&](auto act) __attribute__((always_inline)) {
+        constexpr int ACT = decltype(act)::value;
+        for (int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x; id < total; id += int64_t(gridDim.x) * 256) {
+            const int64_t row = (id | pieces) >> 32 == 0 ? uint32_t(id) / uint32_t(pieces) : id / pieces, col = 8 * (id - row * pieces), left = a.N - col;
+            const u32x4_t d = load8_bf16(static_cast<const uint16_t *>(a.dH) + row * a.lddh + col, left);
+            const u32x4_t g = load8_bf16(static_cast<const uint16_t *>(a.G) + row * a.ldg + col, left);
+            const u32x4_t u = load8_bf16(static_cast<const uint16_t *>(a.U) + row * a.ldu + col, left);
+            float dg[8], du[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                auto value = [&](const u32x4_t &v) __attribute__((always_inline)) { return bf16_to_f32((v[e / 2] >> (16 * (e & 1))) & 0xffffu); };
+                float val, slope;
+                act_both<ACT>(value(g), val, slope);
+                dg[e] = value(d) * value(u) * slope;
+                du[e] = value(d) * val;
+            }
+            uint16_t *const og = static_cast<uint16_t *>(a.dG) + row * a.lddg + col, *const ou = static_cast<uint16_t *>(a.dU) + row * a.lddu + col;
+            store4_bf16(og, left, pack_bf16(dg[0], dg[1]), pack_bf16(dg[2], dg[3]));
+            store4_bf16(ou, left, pack_bf16(du[0], du[1]), pack_bf16(du[2], du[3]));
+            store4_bf16(og + 4, left - 4, pack_bf16(dg[4], dg[5]), pack_bf16(dg[6], dg[7]));
+            store4_bf16(ou + 4, left - 4, pack_bf16(du[4], du[5]), pack_bf16(du[6], du[7]));
+        }
+    });
+}
+
+int launch_gated_bwd(const GatedBwdArgs &a, void *stream) {
+    const int64_t blocks = (a.M * ((a.N + 7) / 8) + 255) / 256;
+    hipLaunchKernelGGL(gated_bwd_kernel, dim3(unsigned(blocks < 16384 ? blocks : 16384)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    return hipGetLastError() == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
+}
+
 int launch_fused(const FusedArgs &a, FusedOp op, const FusedPlan &plan, void *stream) { return launch_fused_with(a, op, plan, nullptr, stream); }
 
 int launch_adapters(const FusedArgs &a, FusedOp op, const FusedPlan &plan, const ShrinkArgs &s0, void *stream) {

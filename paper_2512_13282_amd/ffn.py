@@ -6,9 +6,11 @@ current stream and call them:
 
 * ``gated_linear(X, Wg, Wu)``: H, and with ``keep=True`` the bf16 G and U that the backward pass takes;
 * ``gated_linear_grad(dY, Wd, G, U)``: the gradients of G and U, and H again, from the block's output gradient;
+* ``gated_linear_bwd(dH, G, U)``: the gradients of G and U from that of H, where something else follows;
 * ``gated_linear_dx(dG, Wg, dU, Wu)``: the input gradient;
 * ``gated_linear_dw(dG, dU, X)``: both weight gradients, and ``linear_dw(dY, X)`` one projection's;
-* ``GatedFeedForward``: the block as a module, with all of them behind autograd.
+* ``GatedLinear`` and ``GatedFeedForward`` (feedforward.py): H and the whole block as modules, with all of them behind
+  autograd.
 
 Weights are laid out as torch's linear layers have them (outputs x inputs).  Operands are bf16
 matrices, which may be strided along their rows; an expanded one is refused, as by the dense helpers.
@@ -20,7 +22,7 @@ import ctypes
 from . import binding as _b
 from .mx import _ld
 
-EXPORTED = ("ffn_gated_bf16_bt", "ffn_gated_grad_bf16", "ffn_gated_dx_f32", "ffn_gated_dx_bf16", "ffn_gated_dw_f32",
+EXPORTED = ("ffn_gated_bf16_bt", "ffn_gated_grad_bf16", "ffn_gated_bwd_bf16", "ffn_gated_dx_f32", "ffn_gated_dx_bf16", "ffn_gated_dw_f32",
             "ffn_gated_dw_bf16", "ffn_dw_f32", "ffn_dw_bf16", "ffn_plan", "ffn_force_plan")
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 FFN_OP_GATED, FFN_OP_GRAD, FFN_OP_DX, FFN_OP_GATED_DW, FFN_OP_DW = range(5)
@@ -37,6 +39,7 @@ class PlanInfo(ctypes.Structure):
 _ARGS = {
     "ffn_gated_bf16_bt": [_i64] * 3 + _matrix * 3 + [_int] + _matrix * 3 + [_p],
     "ffn_gated_grad_bf16": [_i64] * 3 + _matrix * 4 + [_int] + _matrix * 3 + [_p],
+    "ffn_gated_bwd_bf16": [_i64] * 2 + _matrix * 3 + [_int] + _matrix * 2 + [_p],
     **{f"ffn_gated_dx_{t}": [_i64] * 3 + _matrix * 5 + [_p] for t in ("f32", "bf16")},
     **{f"ffn_gated_dw_{t}": [_i64] * 3 + _matrix * 5 + [_p] for t in ("f32", "bf16")},
     **{f"ffn_dw_{t}": [_i64] * 3 + _matrix * 3 + [_p] for t in ("f32", "bf16")},
@@ -69,8 +72,8 @@ def _entry(name):
     return call
 
 
-(ffn_gated_bf16_bt, ffn_gated_grad_bf16, ffn_gated_dx_f32, ffn_gated_dx_bf16, ffn_gated_dw_f32, ffn_gated_dw_bf16,
- ffn_dw_f32, ffn_dw_bf16) = map(_entry, EXPORTED[:8])
+(ffn_gated_bf16_bt, ffn_gated_grad_bf16, ffn_gated_bwd_bf16, ffn_gated_dx_f32, ffn_gated_dx_bf16, ffn_gated_dw_f32, ffn_gated_dw_bf16,
+ ffn_dw_f32, ffn_dw_bf16) = map(_entry, EXPORTED[:9])
 
 
 def ffn_plan(op, M, N, K) -> dict:
@@ -136,8 +139,14 @@ class _Helpers:
                 raise TypeError("results are bfloat16 or float32")
             return out_dtype
 
-        def call(fn, *args):
-            rc = fn(*args)
+        current, device_of = torch._C._cuda_getDevice, torch.cuda.device
+
+        def call(dev, fn, *args):
+            if current() == dev:
+                rc = fn(*args, raw_stream(dev))
+            else:                                           # the entry points work on the current device
+                with device_of(dev):
+                    rc = fn(*args, raw_stream(dev))
             if rc != ok:
                 raise _b.GemmError(rc)
 
@@ -152,8 +161,7 @@ class _Helpers:
                 kept = (G.data_ptr(), N or 1, U.data_ptr(), N or 1)
             else:
                 kept = (None, 0, None, 0)
-            call(f_gated, M, N, K, *operand(X, M, K, dev), *operand(Wg, N, K, dev), *operand(Wu, N, K, dev), act, h, ldh, *kept,
-                 raw_stream(dev))
+            call(dev, f_gated, M, N, K, *operand(X, M, K, dev), *operand(Wg, N, K, dev), *operand(Wu, N, K, dev), act, h, ldh, *kept)
             return (H, G, U) if keep else H
 
         def grad(dY, Wd, G, U, activation):
@@ -163,9 +171,18 @@ class _Helpers:
             dev = dY.get_device()
             outs = [empty(M, N, dtype=bf16, device=dY.device) for _ in range(3)]
             places = [v for o in outs for v in (o.data_ptr(), N or 1)]
-            call(f_grad, M, N, K, *operand(dY, M, K, dev), *operand(Wd, K, N, dev), *operand(G, M, N, dev), *operand(U, M, N, dev), act,
-                 *places, raw_stream(dev))
+            call(dev, f_grad, M, N, K, *operand(dY, M, K, dev), *operand(Wd, K, N, dev), *operand(G, M, N, dev), *operand(U, M, N, dev), act,
+                 *places)
             return tuple(outs)
+
+        def bwd(dH, G, U, activation):
+            act = activation_code(activation)
+            M, N = matrix(dH)
+            dev = dH.get_device()
+            dG, dU = empty(M, N, dtype=bf16, device=dH.device), empty(M, N, dtype=bf16, device=dH.device)
+            call(dev, fns["ffn_gated_bwd_bf16"], M, N, *operand(dH, M, N, dev), *operand(G, M, N, dev), *operand(U, M, N, dev), act,
+                 dG.data_ptr(), N or 1, dU.data_ptr(), N or 1)
+            return dG, dU
 
         def input_gradient(dG, Wg, dU, Wu, out, out_dtype):
             M, K = matrix(dG)
@@ -173,8 +190,7 @@ class _Helpers:
             dev = dG.get_device()
             dtype = checked(out_dtype if out is None else out.dtype, bf16, dx)
             dX, p, ld = result(out, M, N, dtype, dG)
-            call(dx[dtype], M, N, K, *operand(dG, M, K, dev), *operand(Wg, K, N, dev), *operand(dU, M, K, dev), *operand(Wu, K, N, dev), p, ld,
-                 raw_stream(dev))
+            call(dev, dx[dtype], M, N, K, *operand(dG, M, K, dev), *operand(Wg, K, N, dev), *operand(dU, M, K, dev), *operand(Wu, K, N, dev), p, ld)
             return dX
 
         def both_dw(dG, dU, X, out_dtype):
@@ -183,8 +199,8 @@ class _Helpers:
             dev = dG.get_device()
             dtype = checked(out_dtype, f32, dw2)
             dWg, dWu = empty(M, N, dtype=dtype, device=dG.device), empty(M, N, dtype=dtype, device=dG.device)
-            call(dw2[dtype], M, N, K, *operand(dG, K, M, dev), *operand(dU, K, M, dev), *operand(X, K, N, dev), dWg.data_ptr(), N or 1,
-                 dWu.data_ptr(), N or 1, raw_stream(dev))
+            call(dev, dw2[dtype], M, N, K, *operand(dG, K, M, dev), *operand(dU, K, M, dev), *operand(X, K, N, dev), dWg.data_ptr(), N or 1,
+                 dWu.data_ptr(), N or 1)
             return dWg, dWu
 
         def one_dw(dY, X, out, out_dtype):
@@ -193,10 +209,10 @@ class _Helpers:
             dev = dY.get_device()
             dtype = checked(out_dtype if out is None else out.dtype, f32, dw1)
             dW, p, ld = result(out, M, N, dtype, dY)
-            call(dw1[dtype], M, N, K, *operand(dY, K, M, dev), *operand(X, K, N, dev), p, ld, raw_stream(dev))
+            call(dev, dw1[dtype], M, N, K, *operand(dY, K, M, dev), *operand(X, K, N, dev), p, ld)
             return dW
 
-        self.gated, self.grad, self.input_gradient, self.both_dw, self.one_dw = gated, grad, input_gradient, both_dw, one_dw
+        self.gated, self.grad, self.bwd, self.input_gradient, self.both_dw, self.one_dw = gated, grad, bwd, input_gradient, both_dw, one_dw
 
 
 _helpers = None
@@ -221,6 +237,11 @@ def gated_linear_grad(dY, Wd, G, U, activation="silu"):
     return (_helpers or _h()).grad(dY, Wd, G, U, activation)
 
 
+def gated_linear_bwd(dH, G, U, activation="silu"):
+    """(dG, dU) of the gradient dH of H itself and what the forward pass kept: dG = dH * U * act'(G), dU = dH * act(G)."""
+    return (_helpers or _h()).bwd(dH, G, U, activation)
+
+
 def gated_linear_dx(dG, Wg, dU, Wu, out=None, out_dtype=None):
     """dG . Wg + dU . Wu (M x N, bf16 unless out_dtype or out says float32): dG, dU M x K, Wg, Wu K x N."""
     return (_helpers or _h()).input_gradient(dG, Wg, dU, Wu, out, out_dtype)
@@ -237,22 +258,9 @@ def linear_dw(dY, X, out=None, out_dtype=None):
     return (_helpers or _h()).one_dw(dY, X, out, out_dtype)
 
 
-def linear_bf16(X, W):
-    """X . W^T rounded once to bf16 (M x N): X M x K, W N x K."""
-    import torch
-    M, K = X.shape
-    Y = torch.empty(M, W.shape[0], dtype=torch.bfloat16, device=X.device)
-    rc = _b.gemm_bf16_bf16_bt(M, W.shape[0], K, X.data_ptr(), _ld(X.stride(), M, K), W.data_ptr(), _ld(W.stride(), *W.shape), Y.data_ptr(),
-                              W.shape[0] or 1, torch._C._cuda_getCurrentRawStream(X.get_device()))
-    if rc != _b.GEMM_OK:
-        raise _b.GemmError(rc)
-    return Y
-
-
 def __getattr__(name):
-    # The module, which needs torch at its definition.
-    if name == "GatedFeedForward":
-        from .feedforward import GatedFeedForward
-        globals()[name] = GatedFeedForward
-        return GatedFeedForward
+    # The modules, which need torch at their definition.
+    if name in ("GatedLinear", "GatedFeedForward"):
+        from . import feedforward
+        return getattr(feedforward, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

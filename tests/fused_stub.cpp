@@ -4,6 +4,7 @@
 
 namespace gemm {
 int launch_fused(const FusedArgs &, FusedOp, const FusedPlan &, void *) { return LAUNCH_HIP_ERROR; }
+int launch_gated_bwd(const GatedBwdArgs &, void *) { return LAUNCH_HIP_ERROR; }
 int launch_adapters(const FusedArgs &, FusedOp, const FusedPlan &, const ShrinkArgs &, void *) { return LAUNCH_HIP_ERROR; }
 int launch_adapters_dw(const AdapterDwArgs &, void *) { return LAUNCH_HIP_ERROR; }
 }  // namespace gemm

@@ -1,0 +1,79 @@
+"""The feed-forward modules as torch modules, on the CPU: what autograd and the module see of them, with plain products
+standing in for the kernels."""
+import pytest
+import torch
+
+import fused_reference as ref
+from paper_2512_13282_amd import binding, feedforward as ff
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    def gated(x, wg, wu, name="silu", keep=False):
+        g, u = x.detach().double() @ wg.detach().double().t(), x.detach().double() @ wu.detach().double().t()
+        h = ref.act(name, g)[0] * u
+        return (h.to(BF16), g, u) if keep else h.to(BF16)
+
+    def bwd(dh, g, u, name="silu"):
+        a, s = ref.act(name, g)
+        return dh.double() * u * s, dh.double() * a
+
+    def grad(dy, wd, g, u, name="silu"):
+        return (*bwd(dy.double() @ wd.detach().double(), g, u, name), ref.act(name, g)[0] * u)
+
+    d = lambda t: t.detach().double()       # noqa: E731
+    stand_ins = {
+        "gated_linear": gated, "gated_linear_bwd": bwd, "gated_linear_grad": grad,
+        "gated_linear_dx": lambda dg, wg, du, wu: (d(dg) @ d(wg) + d(du) @ d(wu)).to(BF16),
+        "gated_linear_dw": lambda dg, du, x, out_dtype: (((d(dg)).t() @ d(x)).to(out_dtype), ((d(du)).t() @ d(x)).to(out_dtype)),
+        "linear_dw": lambda dy, x, out_dtype: (d(dy).t() @ d(x)).to(out_dtype),
+    }
+    for name, fn in stand_ins.items():
+        monkeypatch.setattr(binding, name, fn, raising=False)
+    monkeypatch.setattr(ff, "_linear", lambda x, W: (d(x) @ d(W).t()).to(BF16))
+
+
+def test_gradients_and_a_second_derivative(plain):
+    torch.manual_seed(0)
+    block = ff.GatedFeedForward(24, 40, 16, device="cpu")
+    x = torch.randn(6, 24).to(BF16).requires_grad_()
+    wanted = (x, block.gate, block.up, block.down)
+    once = torch.autograd.grad(block(x).float().pow(2).mean(), wanted)
+    kept = torch.autograd.grad(block(x).float().pow(2).mean(), wanted, create_graph=True)
+    for a, b in zip(once, kept):
+        assert torch.equal(a, b.detach()) and a.dtype == BF16
+    with pytest.raises(RuntimeError, match="first derivatives"):
+        kept[0].float().pow(2).sum().backward()
+    X, wg, wu, wd = (t.detach().double().requires_grad_() for t in wanted)
+    y = (torch.nn.functional.silu(X @ wg.t()) * (X @ wu.t())) @ wd.t()
+    for got, want in zip(once, torch.autograd.grad(y.pow(2).mean(), (X, wg, wu, wd))):
+        assert torch.allclose(got.double(), want, rtol=0.05, atol=0.05 * want.abs().max().item())
+    gated = ff.GatedLinear(24, 40, "relu", device="cpu")
+    g, = torch.autograd.grad(gated(x).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="first derivatives"):
+        g.float().pow(2).sum().backward()
+
+
+def test_what_learns_and_what_is_saved(tmp_path):
+    W = torch.randn(12, 20).to(BF16)
+    layer = ff.AdaptersLinear(W, 3, 4)
+    assert [n for n, _ in layer.named_parameters()] == ["A", "B"] and not layer.weight.requires_grad
+    assert layer.A.shape == (3, 4, 20) and layer.B.shape == (3, 12, 4) and torch.all(layer.B == 0)
+    path = tmp_path / "layer.pt"
+    torch.save(layer.state_dict(), path)
+    other = ff.AdaptersLinear(torch.zeros_like(W), 3, 4, scale=2.0)
+    other.load_state_dict(torch.load(path, weights_only=True))
+    assert torch.equal(other.weight, W) and torch.equal(other.A, layer.A) and torch.all(other.scale == 1)
+    block = ff.GatedFeedForward(20, 12, device="cpu")
+    assert sorted(block.state_dict()) == ["down", "gate", "up"] and block.down.shape == (20, 12)
+    assert {t.device.type for t in block.to("meta").state_dict().values()} == {"meta"}
+
+
+def test_modules_are_reached_beside_their_operators():
+    from paper_2512_13282_amd import adapters, ffn
+    assert ffn.GatedFeedForward is ff.GatedFeedForward and ffn.GatedLinear is ff.GatedLinear and adapters.AdaptersLinear is ff.AdaptersLinear
+    for module in (ffn, adapters):
+        with pytest.raises(AttributeError):
+            module.NoSuchModule

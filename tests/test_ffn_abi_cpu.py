@@ -60,6 +60,18 @@ def arguments(form, sizes=(M, N, K), act=0, change=None):
     return fn, args
 
 
+def test_the_gradients_from_that_of_h_refuse():
+    good = [M, N, AT[0], N, AT[1], N, AT[2], N, 0, AT[3], N, AT[4], N]
+    bad = [(0, -1), (1, -1), (0, 1 << 60), (8, 4), (8, -1)]
+    bad += [(i, v) for i in (2, 4, 6, 9, 11) for v in (0, good[i] + 1)] + [(i, v) for i in (3, 5, 7, 10, 12) for v in (N - 1, -N, 1 << 61)]
+    bad += [(o, AT[i]) for o in (9, 11) for i in range(3)] + [(11, AT[3] + 4)]
+    for i, v in bad:
+        args = list(good)
+        args[i] = v
+        assert ffn.ffn_gated_bwd_bf16(*args) == BAD, (i, v)
+    assert ffn.ffn_gated_bwd_bf16(0, N, *good[2:]) == b.GEMM_OK and ffn.ffn_gated_bwd_bf16(M, 0, *good[2:]) == b.GEMM_OK
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_refusals(form):
     fn, parts, operands = FORMS[form]

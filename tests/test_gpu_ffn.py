@@ -1,5 +1,7 @@
 """The gated feed-forward kernels against their definitions in 64 bits, within the bounds of their fp32 sums and their
 one rounding (fused_reference.py)."""
+import zlib
+
 import pytest
 import torch
 
@@ -24,7 +26,7 @@ def matrix(gen, rows, cols, scale=1.0, pad=0, offset=0):
 
 def generator(*key):
     gen = torch.Generator()
-    gen.manual_seed(hash(key) % (1 << 31))
+    gen.manual_seed(zlib.crc32(repr(key).encode()))
     return gen
 
 
@@ -235,3 +237,17 @@ def test_slices_give_the_same_bits_captured_and_on_every_stream(op):
         del graph
     torch.cuda.synchronize()
     assert b.gemm_release_workspace() == b.GEMM_OK
+
+
+@pytest.mark.parametrize("size", [(1, 8, 0), (3, 7, 1), (70, 133, 5), (300, 1000, 8)], **ids)
+@pytest.mark.parametrize("name", ref.ACTIVATIONS)
+def test_gradients_from_that_of_h(size, name):
+    M, N, pad = size
+    gen = generator("bwd", *size)
+    dh, g, u = matrix(gen, M, N, 1.0, pad, 0), matrix(gen, M, N, 2.0, pad, pad % 2), matrix(gen, M, N, 1.0, pad, 0)
+    d = dh.double()
+    a, s = ref.act(name, g.double())
+    dG, dU = b.gated_linear_bwd(dh, g, u, name)
+    for got, v, e in ((dG, d * u.double() * s, (d * u.double()).abs() * ref.SLOPE_ERROR * (1 + s.abs())),
+                      (dU, d * a, d.abs() * ref.ACT_ERROR * (1 + a.abs()))):
+        ref.assert_within(got, (v, ref.rounded(v, e + 2.0 ** -22 * v.abs(), BF16)))
