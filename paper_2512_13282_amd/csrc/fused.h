@@ -30,6 +30,7 @@ struct FusedArgs {
     int32_t act;                     // FFN_* of ffn_mi355x.h
     int32_t pairs;                   // DW: 1 or 2 matrices A
     int32_t whole;                   // workgroups with a tile and all of K, ahead of the rest
+    int32_t early;                   // of the lower tiles, that many come after the first 128 workgroups
     int32_t half;                    // DW: tile rows of the first matrix
     struct Tail {                    // the lower tiles, where the plan has some: from row `row` and column `col` on
         int64_t row, col;
@@ -74,7 +75,7 @@ FusedTail fused_tail(FusedOp op, int32_t pairs, int64_t M, int64_t N, const Fuse
 
 // The kernels for few rows of A, by rows: the one that takes its operands as they lie, and the one for operands on
 // 16-byte rows.
-constexpr int32_t kFusedDecode = 6, kFusedStream = 10;
+constexpr int32_t kFusedDecode = 7, kFusedStream = 11;
 inline bool fused_few_rows(int32_t config) { return config >= kFusedDecode; }
 inline bool fused_any_address(int32_t config) { return config >= kFusedDecode && config < kFusedStream; }
 

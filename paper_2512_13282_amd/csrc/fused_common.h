@@ -220,11 +220,16 @@ struct FusedWork {
     int slot, slice, slices;     // the tile's place among those in slices, this slice of it and how many there are
     bool low;                    // one of the lower tiles
 };
+constexpr int kEarlyFrom = 128;
 template <int BM, int LOW, int COLS>
 __device__ __forceinline__ FusedWork fused_work(const FusedArgs &a, int all) {
     const KernelArgs &g = a.g;
-    const bool rest = int(blockIdx.x) >= a.whole;
-    const int total = rest ? int(gridDim.x) - a.whole : a.whole, hw = rest ? int(blockIdx.x) - a.whole : int(blockIdx.x);
+    // GRAD: lower tiles also fill the second half of the first round, so that the compute units end their tiles, and read and
+    // write ten bytes for each of their elements, at different times from then on (2048 x 11008 x 4096: 8 %).
+    const int at = int(blockIdx.x), early = LOW > 0 ? a.early : 0;
+    const bool rest = (early > 0 && at >= kEarlyFrom && at < kEarlyFrom + early) || at >= a.whole + early;
+    const int total = rest ? int(gridDim.x) - a.whole : a.whole;
+    const int hw = early == 0 ? (rest ? at - a.whole : at) : rest ? (at < kEarlyFrom + early ? at - kEarlyFrom : at - a.whole) : at < kEarlyFrom ? at : at - early;
     const int per = total / 8, rem = total % 8, xcd = hw % 8, local = hw / 8;
     const int id = xcd < rem ? xcd * (per + 1) + local : rem * (per + 1) + (xcd - rem) * per + local;
     FusedWork w;

@@ -50,6 +50,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
         const FusedTail t = fused_tail(op, a.pairs, a.g.M, a.g.N, plan);
         a.tail = FusedArgs::Tail{t.row, t.col, int32_t(t.tiles_m), int32_t(t.tiles_n), op == FUSED_DW ? int32_t(t.half) : INT32_MAX};
         grid += t.tiles;
+        a.early = op == FUSED_GRAD && plan.whole > 128 ? int32_t(t.tiles < 128 ? t.tiles / 8 * 8 : 128) : 0;
     }
     a.g.tiles_m = int32_t(plan.tail_rows > 0 ? plan.tail_rows : tm);
     a.g.tiles_n = int32_t(plan.tail_cols > 0 ? plan.tail_cols : tn);
@@ -75,7 +76,14 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     // The kernels for few rows add h's planes up themselves; elsewhere and where the caller keeps h the slices meet in it.
     const bool sum_h = shrink != nullptr && shrink->slices > 1 && (shrink->h != nullptr || !fused_few_rows(plan.config));
     const bool own_h = shrink != nullptr && shrink->h == nullptr && sum_h;
-    const int64_t planes = shrink == nullptr || (shrink->h != nullptr && shrink->slices == 1) ? 0 : up16((shrink->slices + (own_h ? 1 : 0)) * shrink->plane * 4);
+    // The planes of h, or the slices' sums as registers hold them and h.
+    int64_t planes = 0, h_at = 0;
+    if (sum_h) {
+        h_at = int64_t(shrink->blocks) * shrink->groups * shrink->slices * shrink_mt(*shrink) * shrink_rt(*shrink) * 1024;
+        planes = h_at + (own_h ? up16(shrink->plane * 4) : 0);
+    } else if (shrink != nullptr && (shrink->h == nullptr || shrink->slices > 1)) {
+        planes = up16(shrink->slices * shrink->plane * 4);
+    }
     const int64_t counted = sliced, h_counted = sum_h ? int64_t(shrink->blocks) * shrink->groups : 0;
 
     WorkspaceHold hold;                  // over the copies, the adapters' first product and the product
@@ -105,7 +113,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
         ShrinkArgs s = *shrink;
         float *const own = reinterpret_cast<float *>(static_cast<uint8_t *>(a.g.workspace) + partial);
         s.out = planes > 0 ? own : s.h;
-        if (own_h) s.h = own + s.slices * s.plane;
+        if (own_h) s.h = own + h_at / 4;
         s.counters = sum_h ? a.g.counters + counted : nullptr;
         if ((s.qt ? queue_shrink<true>(s, stream) : queue_shrink<false>(s, stream)) != hipSuccess) return LAUNCH_HIP_ERROR;
         a.h = sum_h ? s.h : s.out;

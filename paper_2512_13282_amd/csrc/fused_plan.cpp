@@ -10,9 +10,10 @@ const FusedConfig kFusedConfigs[] = {
     {256, 256, 8, 1, 16, 0, "fused_pingpong_256x256"},
     {256, 256, 8, 1, 1, 192, "fused_pingpong_256x256_192"},
     {256, 256, 8, 1, 1, 128, "fused_pingpong_256x256_128"},
+    {128, 128, 8, 1, 4096, 0, "fused_128x128_4x2"},
     {16, 16, 8, 2, 1, 0, "fused_decode_16"},
-    {32, 16, 8, 2, 1, 0, "fused_decode_32"},
-    {48, 16, 8, 2, 1, 0, "fused_decode_48"},
+    {32, 16, 16, 1, 1, 0, "fused_decode_32"},
+    {48, 16, 16, 1, 1, 0, "fused_decode_48"},
     {64, 16, 8, 2, 1, 0, "fused_decode_64"},
     {16, 16, 8, 1, 1, 0, "fused_stream_16"},
     {32, 16, 8, 1, 1, 0, "fused_stream_32"},
@@ -37,11 +38,13 @@ constexpr FusedFigures kFigures[] = {
     {2.811, 0.670, 0.670, 4.436, 0.760},
     {4.102, 0.885, 0.885, 4.870, 0.556},
     {4.757, 1.104, 1.104, 4.369, 0.413},
+    {}, {},
+    {2.000, 0.500, 0.500, 4.000, 0.850},
 };
 // A stage's time by operator, over GATED's.
-constexpr double kPart[FUSED_OPS][4] = {
-    {1.000, 1.000, 1.000, 1.000}, {1.140, 1.184, 1.164, 1.190}, {1.000, 0.957, 0.906, 0.882},
-    {0.978, 1.071, 1.066, 1.102}, {0.932, 0.826, 0.827, 0.929}, {0.865, 0.779, 0.778, 0.797},
+constexpr double kPart[FUSED_OPS][7] = {
+    {1.000, 1.000, 1.000, 1.000, 0, 0, 1.000}, {1.140, 1.184, 1.164, 1.190, 0, 0, 1.184}, {1.000, 0.957, 0.906, 0.882, 0, 0, 0.957},
+    {0.978, 1.071, 1.066, 1.102, 0, 0, 1.071}, {0.932, 0.826, 0.827, 0.929, 0, 0, 0.826}, {0.865, 0.779, 0.778, 0.797, 0, 0, 0.779},
 };
 constexpr double kStore[FUSED_OPS] = {0.432, 0.376, 0.448, 0.090, 0.228, 0.471};   // a megabyte of results (GRAD: and of G and U)
 constexpr double kLaunch = 3.1, kRate = 4.0;                                       // megabytes in a microsecond

@@ -15,8 +15,9 @@ namespace gemm {
 // tokens are taken one after the other over all rows, of which the adapter's own are written; the others' results are
 // dropped.  `parts` workgroups share the adapters of the same tokens, in turn.
 //
-// Slices leave planes.  Where `counters` is set the one that arrives last adds them up in their order (mx_common.h says
-// how the accesses are ordered), else whoever reads h does.
+// Slices leave planes, which whoever reads h adds up.  Where `counters` is set they leave their sums as their registers
+// hold them (a run of 1 KiB per wave and store), and the one that arrives last adds them up in their order (mx_common.h says
+// how the accesses are ordered).
 // ---------------------------------------------------------------------------
 template <bool QT, int MT, int RT, int KW>
 __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) {
@@ -50,13 +51,11 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
         pending[m] = uint32_t(__ballot(has[m])) & 0xffffu;
         row[m] = static_cast<const uint16_t *>(s.P) + safe * s.ldp + l_begin + 32 * c0 + 8 * grp;
     }
-    auto store = [&](int m, int j, int64_t t, f32x4_t v) __attribute__((always_inline)) {
-        float *const dst = out + t * s.r + j;
-        if (s.counters != nullptr) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e < s.r) store_coherent(dst + e, v[e]);
-        } else if (j + 4 <= s.r) {
+    constexpr uint32_t TILES = MT * RT, SLICE = TILES * 1024;
+    const int area = block * int(gridDim.z) + int(blockIdx.z);
+    const __amdgpu_buffer_rsrc_t sums = make_rsrc(reinterpret_cast<uint8_t *>(s.out) + int64_t(area) * s.slices * SLICE, uint32_t(s.slices) * SLICE);
+    auto to_h = [&](float *dst, int j, f32x4_t v) __attribute__((always_inline)) {
+        if (j + 4 <= s.r) {
             *reinterpret_cast<f32x4_el_t *>(dst) = v;
         } else {
 #pragma unroll
@@ -64,12 +63,18 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
                 if (j + e < s.r) dst[e] = v[e];
         }
     };
+    // Tile k = RT m + rt: four ranks from j on of token t.
+    auto store = [&](int k, int64_t t, f32x4_t v) __attribute__((always_inline)) {
+        const int j = j0 + 16 * (k % RT) + 4 * grp;
+        if (s.counters != nullptr) mx_store_part(sums, uint32_t(blockIdx.y) * SLICE + uint32_t(k * 1024 + lane * 16), v);
+        else to_h(out + t * s.r + j, j, v);
+    };
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int64_t t = t0 + 16 * m + l16;
         if (zeros && t < s.M && !has[m] && wave == m % KW)       // none: zeros
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) store(m, j0 + 16 * rt + 4 * grp, t, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
+            for (int rt = 0; rt < RT; ++rt) store(m * RT + rt, t, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
     }
     for (;;) {
         int cur = -1;
@@ -192,7 +197,7 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
 #pragma unroll
             for (int v = 0; v < MT; ++v)
                 if (v == m) take = has[v] && own[v] == cur;
-            if (take) store(m, j0 + 16 * (k % RT) + 4 * grp, t0 + 16 * m + l16, sum * scale);
+            if (take) store(k, t0 + 16 * m + l16, sum * scale);
         }
         phase_barrier();
     }
@@ -200,23 +205,22 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
     // The last of the block's slices and parts adds the planes up.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    const int counter = block * int(gridDim.z) + int(blockIdx.z);
     if (threadIdx.x == 0)
-        flag = __hip_atomic_fetch_add(&s.counters[counter], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == unsigned(s.slices * s.parts - 1);
+        flag = __hip_atomic_fetch_add(&s.counters[area], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == unsigned(s.slices * s.parts - 1);
     __syncthreads();
     if (flag == 0) return;
-    const int rows = int(s.M - t0 < 16 * MT ? s.M - t0 : 16 * MT), ranks = s.r - j0 < 16 * RT ? s.r - j0 : 16 * RT;
-    for (int i = int(threadIdx.x); i < rows * ranks; i += 64 * KW) {
-        const int64_t at = (t0 + i / ranks) * s.r + j0 + i % ranks;
-        float v[8];
+    for (int k = wave; k < int(TILES); k += KW) {
+        const int64_t t = t0 + 16 * (k / RT) + l16;
+        f32x4_t v[8];                                            // past the last slice zeros
 #pragma unroll
-        for (int p = 0; p < 8; ++p) v[p] = p < s.slices ? load_coherent(s.out + p * s.plane + at) : 0.0f;
-        float sum = v[0];
+        for (int p = 0; p < 8; ++p) v[p] = mx_load_part(sums, t < s.M ? uint32_t(p) * SLICE + uint32_t(k * 1024 + lane * 16) : kOOB);
+        f32x4_t sum = v[0];
 #pragma unroll
         for (int p = 1; p < 8; ++p) sum += v[p];
-        s.h[at] = sum;
+        const int j = j0 + 16 * (k % RT) + 4 * grp;
+        if (t < s.M) to_h(s.h + t * s.r + j, j, sum);
     }
-    if (threadIdx.x == 0) __hip_atomic_store(&s.counters[counter], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) __hip_atomic_store(&s.counters[area], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // ---------------------------------------------------------------------------
@@ -300,18 +304,30 @@ __global__ __launch_bounds__(256) void adapters_dw_kernel(AdapterDwArgs a) {
         held -= 32;
     };
 
-    for (int64_t t0 = int64_t(wave) * 64; t0 < a.M; t0 += 64 * WAVES) {
-        const int64_t t = t0 + lane;
-        const bool mine = t < a.M && a.index[t] == cur;
-        const uint64_t mask = __ballot(mine);
-        if (mask == 0u) continue;
-        if (mine) {
-            const int before = __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0u));
-            list[wave][(head + held + before) & 127] = int(t);
+    constexpr int LOOKS = 8;                                     // looks at the index on the way at once
+    for (int64_t t0 = int64_t(wave) * 64; t0 < a.M; t0 += 64 * WAVES * LOOKS) {
+        int own[LOOKS];
+#pragma unroll
+        for (int k = 0; k < LOOKS; ++k) {
+            const int64_t t = t0 + 64 * WAVES * k + lane;
+            own[k] = t < a.M ? a.index[t] : -1;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        held += __builtin_popcountll(mask);                      // at most 31 + 64
-        while (held >= 32) step(32);
+#pragma unroll 1
+        for (int k = 0; k < LOOKS; ++k) {
+            const uint64_t mask = __ballot(own[0] == cur);
+            const int t = int(t0) + 64 * WAVES * k + lane;
+            const bool mine = own[0] == cur;
+#pragma unroll
+            for (int i = 0; i + 1 < LOOKS; ++i) own[i] = own[i + 1];
+            if (mask == 0u) continue;
+            if (mine) {
+                const int before = __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0u));
+                list[wave][(head + held + before) & 127] = t;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            held += __builtin_popcountll(mask);                  // at most 31 + 64
+            while (held >= 32) step(32);
+        }
     }
     if (held > 0) step(held);
 
