@@ -1,6 +1,8 @@
 // fused_plan.cpp -- how the fused products choose their tile and K slices (host).
 #include "fused.h"
 
+#include <math.h>
+
 namespace gemm {
 
 const FusedConfig kFusedConfigs[] = {
@@ -26,33 +28,39 @@ constexpr int kCUs = 256;
 constexpr int32_t kFused128 = 1, kFused192 = 2, kFused256 = 3;     // rows of kFusedConfigs that the lower tiles' plans use too
 
 // The model's figures: a least-squares fit of modelled_us to the logarithms of the times of every configuration and number
-// of slices at 840 drawn shapes (rows 1 to 4096, widths of 64 to 14336, every operator).  They are to be fitted again where a
-// kernel changes.
+// of slices at 970 drawn shapes (rows 1 to 4096, widths of 64 to 14336, every operator, cold weights).  They are to be
+// fitted again where a kernel changes.
 struct FusedFigures {
     // Microseconds: a workgroup's start and end, a stage of 64 k of its tile alone on its compute unit and with the unit
     // full, a last slice's sum and its share per 100 KB of partial sums.
     double start_us, part_us, part_full_us, sum_us, sum_slice_us;
 };
 constexpr FusedFigures kFigures[] = {
-    {1.115, 0.335, 0.602, 3.846, 0.941},
-    {2.811, 0.670, 0.670, 4.436, 0.760},
-    {4.102, 0.885, 0.885, 4.870, 0.556},
-    {4.757, 1.104, 1.104, 4.369, 0.413},
-    {}, {},
-    {2.000, 0.500, 0.500, 4.000, 0.850},
+    {1.341, 0.370, 0.619, 0.661, 0.000},
+    {2.935, 0.673, 0.673, 1.871, 0.528},
+    {4.314, 0.876, 0.876, 2.580, 0.411},
+    {5.138, 1.084, 1.084, 2.438, 0.377},
+    {}, {},                                          // with lower tiles: as the one without, and theirs
+    {1.643, 0.509, 0.509, 1.746, 0.295},
 };
 // A stage's time by operator, over GATED's.
 constexpr double kPart[FUSED_OPS][7] = {
-    {1.000, 1.000, 1.000, 1.000, 0, 0, 1.000}, {1.140, 1.184, 1.164, 1.190, 0, 0, 1.184}, {1.000, 0.957, 0.906, 0.882, 0, 0, 0.957},
-    {0.978, 1.071, 1.066, 1.102, 0, 0, 1.071}, {0.932, 0.826, 0.827, 0.929, 0, 0, 0.826}, {0.865, 0.779, 0.778, 0.797, 0, 0, 0.779},
+    {1.000, 1.000, 1.000, 1.000, 0, 0, 1.000},
+    {1.107, 1.167, 1.126, 1.133, 0, 0, 1.061},
+    {0.970, 0.947, 0.889, 0.903, 0, 0, 0.962},
+    {0.954, 0.988, 0.990, 1.062, 0, 0, 0.973},
+    {0.936, 0.817, 0.828, 0.932, 0, 0, 0.929},
+    {0.877, 0.824, 0.797, 0.831, 0, 0, 0.902},
 };
-constexpr double kStore[FUSED_OPS] = {0.432, 0.376, 0.448, 0.090, 0.228, 0.471};   // a megabyte of results (GRAD: and of G and U)
-constexpr double kLaunch = 3.1, kRate = 4.0;                                       // megabytes in a microsecond
-// The kernels for few rows: the start, a megabyte of weights and of A, 100 KB of both through one compute unit, 1000 k.
-struct FewFigures { double start_us, weights_us, x_us, own_us, k_us; };
+constexpr double kStore[FUSED_OPS] = {0.312, 0.377, 0.393, 0.040, 0.344, 0.303};   // a megabyte of results (GRAD: and of G and U)
+constexpr double kLaunch = 2.73, kRate = 4.85, kSlice = 0.51;                      // megabytes in a microsecond; each slice
+constexpr double kEarly = 0.92;                                                    // GRAD's lower tiles that begin early
+// The kernels for few rows: the start, a megabyte of weights and of A, 100 KB of both through one compute unit, 1000 k,
+// a round of workgroups.
+struct FewFigures { double start_us, weights_us, x_us, own_us, k_us, round_us; };
 constexpr FewFigures kFew[] = {
-    {4.195, 0.167, 0.066, 2.425, 0.000}, {3.644, 0.162, 0.128, 2.434, 0.251}, {3.559, 0.201, 0.107, 2.488, 0.423},
-    {3.455, 0.261, 0.073, 2.772, 0.474}, {4.959, 0.168, 0.000, 0.733, 0.000}, {4.742, 0.187, 0.039, 0.998, 0.000},
+    {3.809, 0.141, 0.108, 2.531, 0.000, 0.362}, {4.277, 0.188, 0.095, 2.733, 0.000, 0.006}, {3.256, 0.216, 0.075, 2.698, 0.213, 0.757},
+    {2.049, 0.216, 0.090, 2.505, 0.605, 1.200}, {4.024, 0.137, 0.026, 0.843, 0.000, 1.069}, {4.220, 0.168, 0.026, 0.971, 0.000, 0.720},
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -123,7 +131,8 @@ double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, c
         const double tokens = double(M < c.bm ? M : c.bm), weights = 2.0 * rows * double(K) / 1e6, x = groups * tokens * double(K) * 2 / 1e6;
         const double per_cu = double(ceil_div(int64_t(groups), kCUs)), own = per_cu * 2.0 * (16 + tokens) * double(K) / 1e5;
         const double all = f.weights_us * weights + f.x_us * x, one = f.own_us * own;
-        return f.start_us + (all > one ? all : one) + f.k_us * double(K) / 1e3 + copy;
+        const double rounds = double(ceil_div(int64_t(groups), kCUs * (p.config < kFusedStream ? 2 : 1)));
+        return f.start_us + (all > one ? all : one) + f.k_us * double(K) / 1e3 + f.round_us * rounds + copy;
     }
     const double stages = double(ceil_div(K, 64)) * (op == FUSED_DX ? 2 : 1), chunk = double(p.k_chunk) / 64;
     const int64_t tiles = ceil_div(M, c.bm) * pairs * ceil_div(N, op == FUSED_GATED ? c.bn / 2 : c.bn);
@@ -134,10 +143,12 @@ double modelled_us(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, c
         // The slices, the last one's sum, and every slice's partial sums out and back.
         const FusedFigures &f = kFigures[as];
         const double groups = double(tiles - p.whole) * p.split_k, rows = M < 8 ? 8 : M < c.bm ? double(M) : double(c.bm);
-        t += rounds_us(op, as, groups, chunk) + f.sum_us + f.sum_slice_us * p.split_k * rows * c.bn * 4 / 1e5 + groups * rows * c.bn * 8 / 4.5e6;
+        t += rounds_us(op, as, groups, chunk) + f.sum_us + kSlice * p.split_k + f.sum_slice_us * p.split_k * rows * c.bn * 4 / 1e5 + groups * rows * c.bn * 8 / 4.5e6;
     }
     const double memory = moved_mb(op, pairs, M, N, K) / kRate;
-    return kLaunch + (t > memory ? t : memory) + copy;
+    if (op == FUSED_GRAD && c.low > 0) t *= kEarly;
+    // Either hides the other in part only.
+    return kLaunch + cbrt(t * t * t + memory * memory * memory) + copy;
 }
 
 }  // namespace
@@ -174,6 +185,8 @@ bool fused_select(FusedOp op, int32_t pairs, int64_t M, int64_t N, int64_t K, in
     double best = 0;
     bool found = false;
     for (int32_t c = 0; c < kFusedNumConfigs; ++c) {
+        // Of the kernels for few rows at any address the first that holds them.
+        if (c > kFusedDecode && fused_any_address(c) && M <= kFusedConfigs[c - 1].bm) continue;
         int32_t seen = 0;
         for (const int32_t s : kSplits) {
             FusedPlan p;
