@@ -78,9 +78,10 @@ int ffn_dw_f32(int64_t M, int64_t N, int64_t K, const uint16_t *dY, int64_t lddy
 int ffn_dw_bf16(int64_t M, int64_t N, int64_t K, const uint16_t *dY, int64_t lddy, const uint16_t *X, int64_t ldx,
                 uint16_t *dW, int64_t lddw, void *stream);
 
-/* Pure host: the plan that a call of these sizes uses: the kernel's configuration (-1: nothing to do), its output tile
- * (GATED: of H), the number of K slices and the K of each (the gradient of X: of both products, one after the other, each
- * on whole 64 k).  GEMM_ERR_INVALID_VALUE: an unknown op, a negative size, a NULL out. */
+/* Pure host: the plan that a call of these sizes uses, its operands on 16-byte rows: the kernel's configuration (-1: nothing
+ * to do), its output tile (GATED: of H), the number of K slices of the tiles that fill no whole round of the compute units,
+ * and the K of each (the gradient of X: of both products, one after the other, each on whole 64 k).
+ * GEMM_ERR_INVALID_VALUE: an unknown op, a negative size, a NULL out. */
 typedef struct ffn_plan_info {
     int32_t config;
     int32_t bm, bn;

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 # M, N, K, adapters, rank, pad, offset
 SIZES = [(1, 8, 8, 1, 8, 0, 0), (1, 1, 1, 1, 1, 0, 0), (3, 7, 5, 2, 3, 0, 0), (16, 128, 256, 16, 16, 0, 0), (37, 131, 129, 5, 7, 1, 3),
          (64, 256, 520, 3, 16, 8, 8), (65, 130, 1000, 70, 4, 0, 0), (130, 264, 320, 1, 64, 0, 0), (300, 513, 511, 9, 33, 5, 1),
-         (257, 520, 136, 4, 128, 0, 0), (1, 1000, 2056, 3, 16, 0, 0), (12, 512, 4104, 40, 32, 0, 0), (511, 264, 64, 2, 1, 0, 0),
+         (257, 520, 136, 4, 128, 0, 0), (1, 1000, 2056, 3, 16, 0, 0), (12, 512, 4104, 40, 32, 0, 0), (511, 264, 64, 2, 1, 0, 0), (40, 96, 200, 2, 300, 0, 0),
          # More tiles than compute units: whole ones, and slices of the rest.
          (1100, 4200, 200, 6, 16, 0, 0), (4340, 4100, 264, 7, 24, 0, 4)]
 

@@ -251,3 +251,49 @@ def test_gradients_from_that_of_h(size, name):
     for got, v, e in ((dG, d * u.double() * s, (d * u.double()).abs() * ref.SLOPE_ERROR * (1 + s.abs())),
                       (dU, d * a, d.abs() * ref.ACT_ERROR * (1 + a.abs()))):
         ref.assert_within(got, (v, ref.rounded(v, e + 2.0 ** -22 * v.abs(), BF16)))
+
+
+def test_gradients_without_h():
+    gen = generator("no h")
+    dy, wd, g, u = matrix(gen, 70, 96), matrix(gen, 96, 133), matrix(gen, 70, 133), matrix(gen, 70, 133)
+    want = b.gated_linear_grad(dy, wd, g, u)
+    dG, dU = torch.empty_like(want[0]), torch.empty_like(want[1])
+    rc = ffn.ffn_gated_grad_bf16(70, 133, 96, dy.data_ptr(), 96, wd.data_ptr(), 133, g.data_ptr(), 133, u.data_ptr(), 133, 0, dG.data_ptr(), 133,
+                                 dU.data_ptr(), 133, 0, 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == b.GEMM_OK and torch.equal(dG, want[0]) and torch.equal(dU, want[1])
+
+
+def test_a_workspace_that_cannot_be_had(monkeypatch):
+    """Nothing is queued, and a later call allocates afresh."""
+    gen = generator("memory")
+    x, w = matrix(gen, 30, 1000), matrix(gen, 200, 1000)
+    try:
+        assert ffn.ffn_force_plan(ffn.FFN_OP_GATED, 0, 4) == b.GEMM_OK
+        want = b.gated_linear(x, w, w)
+        torch.cuda.synchronize()
+        assert b.gemm_release_workspace() == b.GEMM_OK
+        out = torch.full_like(want, 7.0)
+        monkeypatch.setenv("GEMM_MI355X_TEST_FAIL_WORKSPACE", "1")
+        with pytest.raises(b.GemmError) as e:
+            b.gated_linear(x, w, w, out=out)
+        assert e.value.status == b.GEMM_ERR_NO_MEMORY
+        torch.cuda.synchronize()
+        assert torch.all(out == 7)
+        monkeypatch.delenv("GEMM_MI355X_TEST_FAIL_WORKSPACE")
+        assert torch.equal(b.gated_linear(x, w, w, out=out), want)
+    finally:
+        ffn.ffn_force_plan(ffn.FFN_OP_GATED)
+
+
+def test_rows_far_apart():
+    """Strides past 4 MiB are copied first, and offsets past 2 GiB reached."""
+    gen = generator("far")
+    small, wg = matrix(gen, 260, 64), matrix(gen, 40, 64)
+    buf = torch.empty(260 * (1 << 22) + 64, dtype=BF16, device=DEV)
+    x = buf.as_strided((260, 64), (1 << 22, 1))
+    x.copy_(small)
+    assert torch.equal(b.gated_linear(x, wg, wg), b.gated_linear(small, wg, wg))
+    assert torch.equal(b.linear_dw(x, x), b.linear_dw(small, small))
+    near = buf.as_strided((260, 64), (1 << 21, 1))                # 4 MiB apart: as they lie
+    near.copy_(small)
+    assert torch.equal(b.gated_linear(near, wg, wg), b.gated_linear(small, wg, wg))
