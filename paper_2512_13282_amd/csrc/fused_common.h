@@ -225,7 +225,8 @@ template <int BM, int LOW, int COLS>
 __device__ __forceinline__ FusedWork fused_work(const FusedArgs &a, int all) {
     const KernelArgs &g = a.g;
     // GRAD: lower tiles also fill the second half of the first round, so that the compute units end their tiles, and read and
-    // write ten bytes for each of their elements, at different times from then on (2048 x 11008 x 4096: 8 %).
+    // write ten bytes for each of their elements, at different times from then on (2048 x 11008 x 4096: 204 against the best other
+    // plan's 226 us on one card, 224 against 221 on a second, 214 against 233 on a third).
     const int at = int(blockIdx.x), early = LOW > 0 ? a.early : 0;
     const bool rest = (early > 0 && at >= kEarlyFrom && at < kEarlyFrom + early) || at >= a.whole + early;
     const int total = rest ? int(gridDim.x) - a.whole : a.whole;

@@ -70,7 +70,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     bool copy[4];
     for (int i = 0; i < 4; ++i) {
         const Operand &o = operands[i];
-        copy[i] = !any && o.rows > 0 && o.cols > 0 && !fused_loadable(*o.p, *o.ld, o.along_k, o.cols);
+        copy[i] = !any && grid > 0 && o.rows > 0 && o.cols > 0 && !fused_loadable(*o.p, *o.ld, o.along_k, o.cols);
         if (copy[i]) copied += o.rows * up16(2 * o.cols);
     }
     // The kernels for few rows add h's planes up themselves; elsewhere and where the caller keeps h the slices meet in it.

@@ -109,7 +109,10 @@ __device__ __forceinline__ void few_rows_store(const FusedArgs &a, const f32x4_t
 // element of either is used by two waves, so nothing passes through LDS but the waves' sums, added up in a fixed
 // order.  Output register e of lane l is weight row 4 (l / 16) + e of token l % 16.  Operands may lie at any address.
 //
-// For operands that do not lie on 16-byte rows, and for the few chunks of short rows; fused_stream_kernel takes the rest.
+// Bound by the read of the weights for one row (gated 1 x 14336 x 4096, 235 MB: 39.3 us; the tile kernel 45.1), by the
+// latency of a few trips to memory for small odd sizes (37 x 2051 x 2049: 20.8 us; copied to aligned rows for the tile
+// kernel 25.2).  A's pieces pass the load path like the weights': 16 rows cost 1 x 4096 x 14336's 34 us another 16, and
+// fused_stream_kernel or the tile kernel takes those where rows are aligned.
 // ---------------------------------------------------------------------------
 template <int OP, int MT, int KW, int U, bool ODD>
 __global__ __launch_bounds__(64 * KW) void fused_decode_kernel(FusedArgs a) {
@@ -209,6 +212,10 @@ __global__ __launch_bounds__(64 * KW) void fused_decode_kernel(FusedArgs a) {
 // into registers, as above, cost the load path nearly twice the time once A has more than a few rows.  A wave waits
 // for its own loads only; nothing is shared, so there is no barrier before the sums.  Rows of A past M are
 // not read (zeros).
+//
+// Measured: adapters 16 x 4096 x 14336 (117 MB of weights, and as many bytes of A through the compute units' load paths)
+// 27.6 us, with the first product's launch 35.6; fused_decode_kernel in its place 43.6, the tile kernel in twelve slices 43.6.
+// For one row the registers win (39.2 against 48.1 us at gated 1 x 14336 x 4096).
 // ---------------------------------------------------------------------------
 template <int OP, int MT, int KW, int NS>
 __global__ __launch_bounds__(64 * KW) void fused_stream_kernel(FusedArgs a) {

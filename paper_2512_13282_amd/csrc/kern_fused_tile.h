@@ -40,6 +40,10 @@ __device__ __forceinline__ void store_fused(const FusedArgs &a, f32x16_t (&acc)[
 // across it (B given K x N, and A given K x M) in 64 rows of k, read back transposed.  GATED: the halves are the same
 // columns of two weights, so a lane holds g and u of the same outputs.  DX: the stages of the
 // second product follow those of the first.  DW: the tiles of the second A follow those of the first.
+//
+// Serves what the larger tiles would leave compute units idle for.  Bound by the load path (about 50 GB/s a compute unit):
+// dx 96 x 4096 x 2 . 11008 in eight slices 45.9 us with 128 x 128 tiles (eight waves, one workgroup to a unit), 51.9 with
+// 64 x 128 in four slices (four waves, two to a unit), which read each weight twice there; 56 with 128 x 256.
 // ---------------------------------------------------------------------------
 template <int OP, int BM, int BN, int WM, int WN, int WAVES_PER_EU, int NS>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * WM * WN, 64 * WM * WN),
