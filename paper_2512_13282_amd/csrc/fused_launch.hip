@@ -6,7 +6,48 @@
 
 namespace gemm {
 
+// Up to four operands of a product copied to aligned rows (mx_launch.h) in one launch.  Rows of bf16 may lie off dwords, where
+// 16-byte loads are slow: dwords put together (load8_any).
+struct FusedCopies {
+    MxCopy job[4];
+    int64_t end[4];                  // pieces of 16 bytes, this job's and those before it
+};
+__global__ __launch_bounds__(256) void fused_realign_kernel(FusedCopies c) {
+    const int64_t step = int64_t(gridDim.x) * 256;
+    for (int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x; id < c.end[3]; id += step) {
+        MxCopy j = c.job[0];
+        int64_t at = id;
+#pragma unroll
+        for (int k = 1; k < 4; ++k)
+            if (id >= c.end[k - 1]) {
+                j = c.job[k];
+                at = id - c.end[k - 1];
+            }
+        const int64_t pieces = j.pitch / 16;
+        const int64_t r = (at | pieces) >> 32 == 0 ? uint32_t(at) / uint32_t(pieces) : at / pieces, col = 8 * (at - r * pieces);
+        const uint16_t *const src = reinterpret_cast<const uint16_t *>(j.src + r * j.stride) + col;
+        const int64_t left = j.used / 2 - col;
+        *reinterpret_cast<u32x4_t *>(j.dst + r * j.pitch + 2 * col) = left >= 8 ? load8_any<true>(src) : load8_bf16(src, left);
+    }
+}
+
 namespace {
+
+bool realign(const MxCopy (&jobs)[4], int count, hipStream_t stream) {
+    if (count == 0) return true;
+    FusedCopies c{};
+    int64_t end = 0;
+    for (int k = 0; k < 4; ++k) {
+        if (k < count) {
+            c.job[k] = jobs[k];
+            end += jobs[k].rows * (jobs[k].pitch / 16);
+        }
+        c.end[k] = end;
+    }
+    const int64_t blocks = (end + 255) / 256;
+    hipLaunchKernelGGL(fused_realign_kernel, dim3(unsigned(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream, c);
+    return hipGetLastError() == hipSuccess;
+}
 
 int64_t up16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -106,8 +147,7 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
             *o.ld = jobs[n].pitch / 2;
             ++n;
         }
-        for (int i = 0; i < n; i += 2)
-            if (!mx_realign(jobs[i], i + 1 < n ? jobs[i + 1] : MxCopy{}, stream)) return LAUNCH_HIP_ERROR;
+        if (!realign(jobs, n, stream)) return LAUNCH_HIP_ERROR;
     }
     if (shrink != nullptr) {
         ShrinkArgs s = *shrink;

@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void mx_realign_kernel(MxCopy x, MxCopy y) {
     }
 }
 
-bool mx_realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
+static bool mx_realign(const MxCopy &x, const MxCopy &y, hipStream_t stream) {
     const int64_t n = (x.rows * (x.pitch / 16) + y.rows * (y.pitch / 16) + 255) / 256;
     hipLaunchKernelGGL(mx_realign_kernel, dim3(unsigned(n < 65536 ? n : 65536)), dim3(256), 0, stream, x, y);
     return hipGetLastError() == hipSuccess;

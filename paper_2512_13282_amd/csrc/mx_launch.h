@@ -19,7 +19,6 @@ struct MxCopy {
     uint8_t *dst;
     int64_t stride, used, pitch, rows;     // rows 0: nothing to copy
 };
-bool mx_realign(const MxCopy &x, const MxCopy &y, hipStream_t stream);
 
 template <typename K>
 hipError_t launch_mx(K kernel, const MxArgs &a, dim3 grid, int threads, size_t lds, hipStream_t s) {

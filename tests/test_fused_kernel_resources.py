@@ -13,7 +13,7 @@ def test_every_kernel_present(kernels):  # noqa: F811
     # Six operators; GATED and ADAPT have kernels for few rows too, at any address (four sizes, on and off dwords) and on
     # 16-byte rows (two).
     for stem, count in (("fused_tile_kernel", 12), ("fused_pingpong_kernel", 30), ("fused_decode_kernel", 16), ("fused_stream_kernel", 4),
-                        ("adapters_shrink_kernel", 17), ("adapters_dw_kernel", 3), ("gated_bwd_kernel", 1)):
+                        ("adapters_shrink_kernel", 17), ("adapters_dw_kernel", 3), ("gated_bwd_kernel", 1), ("fused_realign_kernel", 1)):
         assert sum(stem in n for n in names) == count, stem
 
 
