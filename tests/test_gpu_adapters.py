@@ -258,3 +258,30 @@ def test_rows_without_an_adapter_beside_one_of_nan(none):
         held = ad.Adapters(bad[:, :, :n_in], bad[:, :, :n_out].transpose(1, 2).contiguous())
         for plan, y in plans(op, lambda: fn(x, weight, held, index)):
             assert torch.all(torch.isfinite(y[rows])) and torch.all(torch.isnan(y[~rows])), plan
+
+
+def test_adapters_past_four_gib():
+    """Many adapters of a wide projection: the last one's matrices lie past 32-bit offsets."""
+    gen = generator("large")
+    n, r, N, K = 700, 64, 50000, 72
+    x, w = matrix(gen, 33, K), matrix(gen, N, K)
+    A = torch.zeros(n, r, K, dtype=BF16, device=DEV)
+    B = torch.zeros(n, N, r, dtype=BF16, device=DEV)               # 4.5 GB
+    A[-1].normal_(std=0.1)
+    B[-1].normal_(std=0.1)
+    index = torch.full((33,), n - 1, dtype=torch.int32)
+    index[5] = 3
+    at = index.to(DEV)
+    alone = ad.Adapters(A[-1:].clone(), B[-1:].clone())
+    one = torch.where(at == n - 1, 0, -1).to(torch.int32)
+    y, h = b.linear_adapters(x, w, ad.Adapters(A, B), at, keep=True)
+    y1, h1 = b.linear_adapters(x, w, alone, one, keep=True)
+    assert torch.equal(h, h1) and torch.equal(y, y1)
+    dA, dB = b.linear_adapters_dw(x, y, h, h, at, n)
+    dA1, dB1 = b.linear_adapters_dw(x, y, h, h, one, 1)
+    assert torch.equal(dA[-1], dA1[0]) and torch.equal(dB[-1], dB1[0]) and torch.all(dB[3] == 0) and torch.all(dB[n - 2] == 0)
+    v = matrix(gen, N, 24)                                          # input gradient over the same B, N outputs
+    A2 = matrix(gen, r, 24).view(1, r, 24).expand(n, r, 24).contiguous()
+    dx = b.linear_adapters_dx(y, v, ad.Adapters(A2, B), at, out_dtype=torch.float32)
+    dx1 = b.linear_adapters_dx(y, v, ad.Adapters(A2[:1].contiguous(), alone.B), one, out_dtype=torch.float32)
+    assert torch.equal(dx[index != 3], dx1[index != 3])

@@ -297,3 +297,21 @@ def test_rows_far_apart():
     near = buf.as_strided((260, 64), (1 << 21, 1))                # 4 MiB apart: as they lie
     near.copy_(small)
     assert torch.equal(b.gated_linear(near, wg, wg), b.gated_linear(small, wg, wg))
+
+
+def test_results_past_four_gib():
+    """Offsets of results and operands past 32 bits: the last rows are those of a call on them alone."""
+    gen = generator("large")
+    M, N, K = 70000, 33000, 40
+    wg = matrix(gen, N, K)
+    x = torch.randn(M, K, device=DEV).to(BF16)
+    H = b.gated_linear(x, wg, wg)
+    assert torch.equal(H[-300:], b.gated_linear(x[-300:].clone(), wg, wg)) and torch.equal(H[:300], b.gated_linear(x[:300].clone(), wg, wg))
+    # H as an operand along the sum and across it.
+    dX = b.gated_linear_dx(H, wg, H, wg, out_dtype=torch.float32)
+    ref.assert_within(dX[-40:], ref.dx(H[-40:], wg, H[-40:], wg, torch.float32))
+    dW = b.linear_dw(H, x)
+    ref.assert_within(dW[-8:], ref.dw(H[:, -8:], x, torch.float32))
+    dG, dU = b.gated_linear_bwd(H, H, H)
+    small = b.gated_linear_bwd(H[-5:].clone(), H[-5:].clone(), H[-5:].clone())
+    assert torch.equal(dG[-5:], small[0]) and torch.equal(dU[-5:], small[1])
