@@ -111,7 +111,7 @@ __device__ __forceinline__ void few_rows_store(const FusedArgs &a, const f32x4_t
 //
 // Bound by the read of the weights for one row (gated 1 x 14336 x 4096, 235 MB: 39.3 us; the tile kernel 45.1), by the
 // latency of a few trips to memory for small odd sizes (37 x 2051 x 2049: 20.8 us; copied to aligned rows for the tile
-// kernel 25.2).  A's pieces pass the load path like the weights': 16 rows cost 1 x 4096 x 14336's 34 us another 16, and
+// kernel 21.5).  A's pieces pass the load path like the weights': 16 rows cost 1 x 4096 x 14336's 34 us another 16, and
 // fused_stream_kernel or the tile kernel takes those where rows are aligned.
 // ---------------------------------------------------------------------------
 template <int OP, int MT, int KW, int U, bool ODD>
