@@ -39,9 +39,13 @@ def _gradients(gradients, *behind):
 
 def _linear(x, W):
     """x . W^T rounded once to bf16."""
-    (M, K), N = x.shape, W.shape[0]
-    if W.shape[1] != K:
+    if x.dtype != torch.bfloat16 or W.dtype != torch.bfloat16:
+        raise TypeError("expected bfloat16 operands")
+    if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
         raise ValueError("operand sizes do not fit")
+    if not x.is_cuda or not W.is_cuda or x.get_device() != W.get_device():
+        raise ValueError("operands must be on the same GPU")
+    (M, K), N = x.shape, W.shape[0]
     y = torch.empty(M, N, dtype=torch.bfloat16, device=x.device)
     with torch.cuda.device(x.device):
         rc = binding.gemm_bf16_bf16_bt(M, N, K, x.data_ptr(), _ld(x.stride(), M, K), W.data_ptr(), _ld(W.stride(), N, K), y.data_ptr(), N or 1,

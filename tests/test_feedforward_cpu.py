@@ -77,3 +77,37 @@ def test_modules_are_reached_beside_their_operators():
     for module in (ffn, adapters):
         with pytest.raises(AttributeError):
             module.NoSuchModule
+
+
+class _OnGpu:
+    """Stands for a matrix on a GPU: its address must not be taken."""
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=BF16, index=0):
+        self.shape, self.dtype, self.index, self.device = torch.Size(shape), dtype, index, torch.device("cuda", index)
+
+    def dim(self):
+        return len(self.shape)
+
+    def get_device(self):
+        return self.index
+
+    def data_ptr(self):
+        pytest.fail("the address of an operand that has to be refused was taken")
+
+
+@pytest.mark.parametrize("x,W,error", [
+    (torch.zeros(3, 8, dtype=BF16), torch.zeros(5, 8), TypeError),                       # an fp32 weight
+    (torch.zeros(3, 8), torch.zeros(5, 8, dtype=BF16), TypeError),
+    (_OnGpu(3, 8), torch.zeros(5, 8), TypeError),
+    (_OnGpu(3, 8), torch.zeros(5, 8, dtype=BF16), ValueError),                           # a weight that is not on the GPU
+    (_OnGpu(3, 8), _OnGpu(5, 8, index=1), ValueError),                                   # ... on another one
+    (torch.zeros(3, 8, dtype=BF16), torch.zeros(5, 8, dtype=BF16), ValueError),
+    (_OnGpu(3, 8), _OnGpu(5, 9), ValueError),
+    (_OnGpu(3, 8), _OnGpu(5, 8, 1), ValueError),
+    (_OnGpu(2, 3, 8), _OnGpu(5, 8), ValueError),
+], ids=lambda v: v.__name__ if isinstance(v, type) else f"{type(v).__name__}-{'x'.join(map(str, v.shape))}-{v.dtype}")
+def test_the_down_projection_refuses_what_is_not_a_bf16_matrix_on_its_gpu(x, W, error, monkeypatch):
+    monkeypatch.setattr(torch, "empty", lambda *_, **__: pytest.fail("a result was allocated for operands that have to be refused"))
+    with pytest.raises(error):
+        ff._linear(x, W)

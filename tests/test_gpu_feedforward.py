@@ -185,3 +185,13 @@ def test_the_example_trains_and_decodes():
     with torch.no_grad():
         x = torch.randn(2, 256, device=DEV).to(BF16)
         assert down(gated(x), torch.tensor([0, -1], device=DEV, dtype=torch.int32)).shape == (2, 256)
+
+
+@pytest.mark.parametrize("down,error", [(lambda w: w.float(), TypeError), (lambda w: w.cpu(), ValueError)], ids=["fp32", "on the CPU"])
+def test_a_down_projection_that_does_not_fit_is_refused(down, error):
+    block = ff.GatedFeedForward(64, 96, 40)
+    block.down = torch.nn.Parameter(down(block.down.detach()))
+    x = torch.randn(3, 64, device=DEV).to(BF16)
+    for mode in (torch.no_grad, torch.enable_grad):
+        with mode(), pytest.raises(error):
+            block(x)
