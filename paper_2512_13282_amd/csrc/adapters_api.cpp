@@ -23,7 +23,7 @@ Stack stack(const void *p, int64_t n, int64_t rows, int64_t cols, int64_t ld, in
     if (one.empty()) return {one, true};
     if (!one.valid() || n > gemm::kMaxSize || stride > gemm::kMaxSize) return {one, false};
     const int64_t span = int64_t(one.span());
-    if (n > 1 && (stride * size < span || stride * size > gemm::kMaxSize / n)) return {one, false};
+    if (n > 1 && (stride < 0 || stride * size < span || stride * size > gemm::kMaxSize / n)) return {one, false};
     return {Region{one.p, n, span, n > 1 ? stride * size : span, size}, true};
 }
 

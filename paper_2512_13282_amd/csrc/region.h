@@ -25,9 +25,9 @@ struct Region {
 };
 
 inline Region region(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t esize) {
-    // Strides past the limit are left as they are: valid() refuses them.
+    // Strides past the limit and negative ones, whose bytes may not fit 64 bits, become ones that valid() refuses.
     const bool big = ld > kMaxSize || cols > kMaxSize;
-    return Region{reinterpret_cast<uintptr_t>(p), rows, big ? kMaxSize : cols * esize, big ? kMaxSize + 1 : ld * esize, esize};
+    return Region{reinterpret_cast<uintptr_t>(p), rows, big ? kMaxSize : cols * esize, big ? kMaxSize + 1 : ld < 0 ? -1 : ld * esize, esize};
 }
 
 }  // namespace gemm

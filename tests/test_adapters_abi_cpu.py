@@ -109,3 +109,14 @@ def test_helpers_refuse_what_is_not_theirs():
         b.linear_adapters(x, w, held, index)             # not on a GPU
     with pytest.raises(ValueError):
         b.linear_adapters_dw(x, x, torch.zeros(4, 8), torch.zeros(4, 8), index, 3)
+
+
+def test_negative_strides_past_64_bits_of_bytes_are_refused():
+    """A stride whose bytes wrap round to a large positive number."""
+    far = lambda size: -(1 << 64) // size + (1 << 30)        # noqa: E731
+    for fn, forward, size in FORMS:
+        for k, v in (("ldx", far(2)), ("ldw", far(2)), ("lda", far(2)), ("ldb", far(2)), ("sa", far(2)), ("sb", far(2)), ("ldy", far(size))):
+            assert linear(fn, forward, **{k: v}) == BAD, (fn.__name__, k)
+    for fn, size in ((ad.adapters_dw_f32, 4), (ad.adapters_dw_bf16, 2)):
+        for k, v in (("ldx", far(2)), ("lddy", far(2)), ("ldda", far(size)), ("lddb", far(size)), ("sda", far(size)), ("sdb", far(size))):
+            assert gradients(fn, **{k: v}) == BAD, (fn.__name__, k)

@@ -166,3 +166,15 @@ def test_helpers_refuse_what_is_not_theirs():
                  lambda: b.gated_linear_dw(x, x, x), lambda: b.linear_dw(x, x)):
         with pytest.raises(ValueError):                  # not on a GPU
             call()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_negative_strides_past_64_bits_of_bytes_are_refused(form):
+    """A stride whose bytes wrap round to a large positive number."""
+    _, parts, _ = FORMS[form]
+    for i, (_, _, size) in enumerate(p for p in parts if p != "act"):
+        f, args = arguments(form, change=(i, None, -(1 << 64) // size + (1 << 30)))
+        assert f(*args) == BAD, i
+    good = [M, N, AT[0], N, AT[1], N, AT[2], N, 0, AT[3], N, AT[4], N]
+    for i in (3, 5, 7, 10, 12):
+        assert ffn.ffn_gated_bwd_bf16(*good[:i], -(1 << 63) + (1 << 30), *good[i + 1:]) == BAD, i

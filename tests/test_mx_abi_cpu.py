@@ -139,3 +139,12 @@ def test_plans_and_their_hook():
             assert mx.mx_force_plan(op) == b.GEMM_OK
     for bad in ((3, -1, 0), (-1, -1, 0), (0, 64, 0), (0, -2, 0), (0, -1, -1)):
         assert mx.mx_force_plan(*bad) == BAD
+
+
+def test_negative_strides_past_64_bits_of_bytes_are_refused():
+    """A stride whose bytes wrap round to a large positive number."""
+    far = -(1 << 63) + (1 << 30)
+    assert mx.mx_pack4(4, 64, X, far, Q, 64, S, 2) == BAD and mx.mx_unpack4(4, 64, Q, 64, S, 2, X, far) == BAD
+    for fn, a, bm, bits, size in FORMS:
+        for k, v in (("lda", far), ("ldc", -(1 << 64) // size + (1 << 30))):
+            assert fn(*{**_good(a, bm, bits), k: v}.values()) == BAD, (fn.__name__, k)
