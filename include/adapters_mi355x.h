@@ -13,7 +13,7 @@
  * adapter), the index 32-bit integers, all in DEVICE memory.  Products are exact and accumulated in fp32;
  * between the two products of an adapter nothing is rounded to fewer than 16 bits where the result is bf16, and to
  * fewer than 24 where it is fp32.  What a request's adapter holds, infinities and NaN included, reaches that
- * request's rows alone.  Results do not depend on the order in which workgroups run.
+ * request's rows alone, and is there what the formula makes of it.  Results do not depend on the order in which workgroups run.
  *
  * Ownership, workspaces, streams, capture, realigned operands and error codes are those of ffn_mi355x.h.  A captured
  * call reads the index, the scales and the adapters anew at each replay.  GEMM_ERR_INVALID_VALUE is returned for a

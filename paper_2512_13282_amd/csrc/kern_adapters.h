@@ -233,11 +233,12 @@ __global__ __launch_bounds__(64 * KW) void adapters_shrink_kernel(ShrinkArgs s) 
 // transposed; h keeps its fp32 value in bf16 parts (split_bf16).  The waves' sums meet in LDS in a fixed order, so
 // results do not depend on timing.  Rows of other adapters are never read.
 //
-// Measured: 2048 tokens of eight adapters of rank 16, x 4096 and dy 11008 wide, 22.2 us for 62 MB read (a look at the index at a
-// time instead of eight 2 us more).
+// Measured: 2048 tokens of eight adapters of rank 16, x 4096 and dy 11008 wide, 22 to 24 us for 62 MB read (a look at the index at a
+// time instead of eight 2 us more).  Registers are held to as many workgroups as LDS leaves room for on a compute unit, five at rank 16:
+// with the second walk's they would be four.
 // ---------------------------------------------------------------------------
 template <int RT>
-__global__ __launch_bounds__(256) void adapters_dw_kernel(AdapterDwArgs a) {
+__global__ __launch_bounds__(256, RT == 1 ? 5 : RT == 2 ? 3 : 2) void adapters_dw_kernel(AdapterDwArgs a) {
     constexpr int WAVES = 4, CT = 4;                             // column tiles of 16
     __shared__ __attribute__((aligned(1024))) uint8_t rows[WAVES][32 * 128];
     __shared__ int list[WAVES][128];
@@ -252,14 +253,10 @@ __global__ __launch_bounds__(256) void adapters_dw_kernel(AdapterDwArgs a) {
     const bool exact = !a.bf16_out;
 
     f32x4_t acc[RT][CT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[i][c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
     // A step over list entries [head, head + 32), the first `count` of them.
     int head = 0, held = 0;
-    auto step = [&](int count) __attribute__((always_inline)) {
+    auto step = [&](int count, auto strict_c) __attribute__((always_inline)) {
         u32x4_t zv[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                            // lane: row 8 i + lane / 8, 16 bytes lane % 8
@@ -300,8 +297,9 @@ __global__ __launch_bounds__(256) void adapters_dw_kernel(AdapterDwArgs a) {
             split_bf16(hv[i], h3);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                if (exact) acc[i][c] = mfma16_bf16(h3[2], zf[c], acc[i][c]);
-                acc[i][c] = mfma16_bf16(h3[1], zf[c], acc[i][c]);
+                const u32x4_t finite = decltype(strict_c)::value ? finite_bf16(zf[c]) : zf[c];
+                if (exact) acc[i][c] = mfma16_bf16(h3[2], finite, acc[i][c]);
+                acc[i][c] = mfma16_bf16(h3[1], finite, acc[i][c]);
                 acc[i][c] = mfma16_bf16(h3[0], zf[c], acc[i][c]);
             }
         }
@@ -311,31 +309,49 @@ __global__ __launch_bounds__(256) void adapters_dw_kernel(AdapterDwArgs a) {
     };
 
     constexpr int LOOKS = 8;                                     // looks at the index on the way at once
-    for (int64_t t0 = int64_t(wave) * 64; t0 < a.M; t0 += 64 * WAVES * LOOKS) {
-        int own[LOOKS];
+    auto walk = [&](auto strict_c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < LOOKS; ++k) {
-            const int64_t t = t0 + 64 * WAVES * k + lane;
-            own[k] = t < a.M ? a.index[t] : -1;
-        }
-#pragma unroll 1
-        for (int k = 0; k < LOOKS; ++k) {
-            const uint64_t mask = __ballot(own[0] == cur);
-            const int t = int(t0) + 64 * WAVES * k + lane;
-            const bool mine = own[0] == cur;
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-            for (int i = 0; i + 1 < LOOKS; ++i) own[i] = own[i + 1];
-            if (mask == 0u) continue;
-            if (mine) {
-                const int before = __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0u));
-                list[wave][(head + held + before) & 127] = t;
+            for (int c = 0; c < CT; ++c) acc[i][c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        head = held = 0;
+        for (int64_t t0 = int64_t(wave) * 64; t0 < a.M; t0 += 64 * WAVES * LOOKS) {
+            int own[LOOKS];
+#pragma unroll
+            for (int k = 0; k < LOOKS; ++k) {
+                const int64_t t = t0 + 64 * WAVES * k + lane;
+                own[k] = t < a.M ? a.index[t] : -1;
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            held += __builtin_popcountll(mask);                  // at most 31 + 64
-            while (held >= 32) step(32);
+#pragma unroll 1
+            for (int k = 0; k < LOOKS; ++k) {
+                const uint64_t mask = __ballot(own[0] == cur);
+                const int t = int(t0) + 64 * WAVES * k + lane;
+                const bool mine = own[0] == cur;
+#pragma unroll
+                for (int i = 0; i + 1 < LOOKS; ++i) own[i] = own[i + 1];
+                if (mask == 0u) continue;
+                if (mine) {
+                    const int before = __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0u));
+                    list[wave][(head + held + before) & 127] = t;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                held += __builtin_popcountll(mask);                  // at most 31 + 64
+                while (held >= 32) step(32, strict_c);
+            }
         }
-    }
-    if (held > 0) step(held);
+        if (held > 0) step(held, strict_c);
+    };
+    walk(std::false_type{});
+    // Sums that are not all finite are formed again, from rows without their infinities and NaN where a part of h may not
+    // meet them (finite_bf16).
+    float all = 0.0f;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) all = __builtin_fmaf(acc[i][c][e], 0.0f, all);
+    if (__ballot(all != all) != 0u) walk(std::true_type{});
 
     // The waves' sums, wave 0's first.
     if (wave > 0) {

@@ -285,3 +285,59 @@ def test_adapters_past_four_gib():
     dx = b.linear_adapters_dx(y, v, ad.Adapters(A2, B), at, out_dtype=torch.float32)
     dx1 = b.linear_adapters_dx(y, v, ad.Adapters(A2[:1].contiguous(), alone.B), one, out_dtype=torch.float32)
     assert torch.equal(dx[index != 3], dx1[index != 3])
+
+
+def matches(got, terms, what):
+    """What is not finite of the sums over terms' second axis (fp64, on the CPU), and nothing else."""
+    want = terms.sum(1)
+    got = got.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    assert torch.equal(got == float("inf"), want == float("inf")) and torch.equal(got == -float("inf"), want == -float("inf")), what
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("M", [12, 40, 300])
+@pytest.mark.parametrize("one", [True, False], ids=["one adapter", "several"])
+def test_infinities_are_what_the_formula_makes_of_them(M, one, dtype):
+    """An infinity times an h of either sign is one whatever the bits of h: exact in bf16 (every other token), to 24 bits, or 0."""
+    gen = generator("infinities", M, one)
+    N, K, n, r = 72, 64, 3, 5
+    index = torch.zeros(M, dtype=torch.int32) if one else torch.randint(0, n, (M,), generator=gen).to(torch.int32)
+    at = index.to(DEV)
+    x = matrix(gen, M, K)
+    x[::2] = 0
+    x[torch.arange(0, M, 2), torch.randint(0, K, ((M + 1) // 2,), generator=gen)] = 1.0
+    down = matrix(gen, n * r, K).view(n, r, K)
+    down[:, 2, :20] = 0                                             # an h of 0
+    up = matrix(gen, n * N, r).view(n, N, r)
+    for i in range(n):
+        up[i, 3 + i, 0] = float("inf")
+        up[i, 20, 1], up[i, 21, 2], up[i, 22, 3] = -float("inf"), float("inf"), float("nan")
+        up[i, 70, 0], up[i, 70, 4] = float("inf"), -float("inf")
+    w, v = matrix(gen, N, K), matrix(gen, K, N)
+    for op, call in ((0, lambda: b.linear_adapters(x, w, ad.Adapters(down, up), at, out_dtype=dtype, keep=True)),
+                     (1, lambda: b.linear_adapters_dx(x, v, ad.Adapters(up.transpose(1, 2).contiguous(), down.transpose(1, 2).contiguous()), at,
+                                                      out_dtype=dtype, keep=True))):
+        for plan, (y, h) in plans(op, call):
+            assert torch.all(torch.isfinite(h))
+            matches(y, h.double().cpu()[:, :, None] * up.double().cpu()[index.long()].transpose(1, 2), (op, plan))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("r", [5, 20, 70])
+def test_infinities_of_the_activations_in_the_weight_gradients(r, dtype):
+    gen = generator("infinities dw", r)
+    M, N, K, n = 150, 72, 100, 3
+    index = torch.randint(0, n, (M,), generator=gen).to(torch.int32)
+    x, dy = matrix(gen, M, K), matrix(gen, M, N)
+    h, dh = torch.randn(M, r, generator=gen), torch.randn(M, r, generator=gen)
+    h[::2], dh[::2] = h[::2].to(BF16).float(), dh[::2].to(BF16).float()
+    h[4, 1], dh[4, 1] = 0.0, 0.0
+    for z, cols in ((x, K), (dy, N)):
+        z[4, 7], z[5, 8], z[20, 9], z[21, cols - 1] = float("inf"), -float("inf"), float("nan"), float("inf")
+        z[30, 40], z[31, 40] = float("inf"), -float("inf")
+    dA, dB = b.linear_adapters_dw(x, dy, h.to(DEV), dh.to(DEV), index.to(DEV), n, out_dtype=dtype)
+    for i in range(n):
+        t = torch.nonzero(index == i)[:, 0]
+        matches(dA[i], dh.double()[t].t()[:, :, None] * x.double().cpu()[t][None], ("dA", i))
+        matches(dB[i].t(), h.double()[t].t()[:, :, None] * dy.double().cpu()[t][None], ("dB", i))
