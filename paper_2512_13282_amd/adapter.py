@@ -11,8 +11,15 @@ synthetic data and then decodes a token through it.
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
+
+
+def differentiated(*tensors) -> bool:
+    """Whether a call on these tensors may be asked for derivatives: it then takes its autograd function, which gives
+    gradients and refuses forward-mode tangents, where the helpers alone would drop them."""
+    return torch.is_grad_enabled() or any(forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 class _FirstDerivative(torch.autograd.Function):
@@ -95,8 +102,8 @@ class AdapterLinear(torch.nn.Module):
 
     def forward(self, x):
         """x: tokens x n_in, bf16 (one token to a batch of prompts).  First derivatives only: a gradient of a
-        gradient raises."""
-        if torch.is_grad_enabled():
+        gradient raises, and so does a forward-mode tangent."""
+        if differentiated(x, self.A, self.B):
             return _AdapterLinear.apply(x, self.weight, self.A, self.B)
         h = binding.mm_bf16_f32(x, self.A.t()).to(torch.bfloat16)
         y = binding.linear_mx4(x, self.weight, out_dtype=torch.float32)

@@ -6,7 +6,8 @@ behind autograd, as training and then decoding use them.
     AdaptersLinear:     y = x W^T + s_i (x A_i^T) B_i^T, token t of adapter i = index[t]
 
 The forward pass keeps G = x Wg^T and U = x Wu^T in bf16 for the backward pass, which forms h again from them.
-Inputs are matrices of tokens x n_in in bf16; gradients are first derivatives, a gradient of a gradient raises.
+Inputs are matrices of tokens x n_in in bf16; gradients are first derivatives; a gradient of a gradient raises, and so does a
+forward-mode tangent.
 ``python -m paper_2512_13282_amd.feedforward`` trains a block whose down projection has adapters of several jobs, on
 synthetic data, and then decodes a token of each.
 """
@@ -15,6 +16,7 @@ from __future__ import annotations
 import torch
 
 from . import binding
+from .adapter import differentiated
 from .mx import _ld
 
 
@@ -133,7 +135,7 @@ class GatedLinear(torch.nn.Module):
         self.activation = activation
 
     def forward(self, x):
-        if torch.is_grad_enabled():
+        if differentiated(x, self.gate, self.up):
             return _GatedLinear.apply(x, self.gate, self.up, self.activation)
         return binding.gated_linear(x, self.gate, self.up, self.activation)
 
@@ -146,7 +148,7 @@ class GatedFeedForward(GatedLinear):
         self.down = _weight(n_in if n_out is None else n_out, n_hidden, device=device)
 
     def forward(self, x):
-        if torch.is_grad_enabled():
+        if differentiated(x, self.gate, self.up, self.down):
             return _GatedFeedForward.apply(x, self.gate, self.up, self.down, self.activation)
         return _linear(binding.gated_linear(x, self.gate, self.up, self.activation), self.down)
 
@@ -164,7 +166,7 @@ class AdaptersLinear(torch.nn.Module):
         self.B = torch.nn.Parameter(torch.zeros(n, n_out, rank, device=weight.device, dtype=torch.bfloat16))
 
     def forward(self, x, index):
-        if torch.is_grad_enabled():
+        if differentiated(x, self.weight, self.A, self.B, self.scale):
             return _AdaptersLinear.apply(x, self.weight, self.A, self.B, self.scale, index)
         return binding.linear_adapters(x, self.weight, binding.Adapters(self.A, self.B, self.scale), index)
 

@@ -135,3 +135,18 @@ def test_only_the_adapter_learns():
     layer = adapter.AdapterLinear(base(), RANK)
     assert [n for n, _ in layer.named_parameters()] == ["A", "B"]
     assert not layer.weight.codes.requires_grad
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.enable_grad])
+def test_a_tangent_is_refused_and_not_dropped(plain, mode):
+    """Forward-mode derivatives, with and without a graph for the backward pass."""
+    from torch.autograd import forward_ad
+    layer, x = layer_and_input()
+    x = x.detach()
+    with mode(), forward_ad.dual_level():
+        assert layer(x).shape == (TOKENS, N_OUT)
+        with pytest.raises(RuntimeError, match="forward"):
+            layer(forward_ad.make_dual(x, torch.ones_like(x)))
+        for name, p in layer.named_parameters():
+            with pytest.raises(RuntimeError, match="forward"):
+                torch.func.functional_call(layer, {name: forward_ad.make_dual(p.detach(), torch.ones_like(p))}, (x,))

@@ -111,3 +111,23 @@ def test_the_down_projection_refuses_what_is_not_a_bf16_matrix_on_its_gpu(x, W, 
     monkeypatch.setattr(torch, "empty", lambda *_, **__: pytest.fail("a result was allocated for operands that have to be refused"))
     with pytest.raises(error):
         ff._linear(x, W)
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.enable_grad])
+def test_a_tangent_is_refused_and_not_dropped(plain, mode, monkeypatch):
+    """Forward-mode derivatives, of an input or of a parameter, with and without a graph for the backward pass."""
+    from torch.autograd import forward_ad
+    monkeypatch.setattr(binding, "linear_adapters", lambda x, W, held, index, keep=False:
+                        (x.detach() @ W.t(), x.detach() @ held.A[0].t()) if keep else x.detach() @ W.t(), raising=False)
+    x, index = torch.randn(6, 24).to(BF16), torch.zeros(6, dtype=torch.int32)
+    adapters = ff.AdaptersLinear(torch.randn(16, 24).to(BF16), 2, 4)
+    calls = [(ff.GatedLinear(24, 40, device="cpu"), ()), (ff.GatedFeedForward(24, 40, device="cpu"), ()), (adapters, (index,))]
+    for module, rest in calls:
+        with mode(), forward_ad.dual_level():
+            assert module(x, *rest).shape[0] == 6
+            with pytest.raises(RuntimeError, match="forward"):
+                module(forward_ad.make_dual(x, torch.ones_like(x)), *rest)
+            for name, p in [*module.named_parameters(), *module.named_buffers()]:
+                dual = forward_ad.make_dual(p.detach(), torch.ones_like(p))
+                with pytest.raises(RuntimeError, match="forward"):
+                    torch.func.functional_call(module, {name: dual}, (x, *rest))
