@@ -155,15 +155,23 @@ class GatedFeedForward(GatedLinear):
 
 class AdaptersLinear(torch.nn.Module):
     """A projection ``weight`` (n_out x n_in bf16, a buffer that does not learn) with ``n`` trainable adapters of rank ``rank``.
-    ``forward(x, index)``: index holds each token's adapter (int32), -1 for none."""
+    Its scales (a buffer) are fp32 and stay so where the module is converted to another type.  ``forward(x, index)``: index
+    holds each token's adapter (int32), -1 for none."""
 
     def __init__(self, weight, n: int, rank: int, scale: float = 1.0):
         super().__init__()
         n_out, n_in = weight.shape
         self.register_buffer("weight", weight)
-        self.register_buffer("scale", torch.full((n,), scale, device=weight.device))
+        self.register_buffer("scale", torch.full((n,), scale, device=weight.device, dtype=torch.float32))
         self.A = _weight(n, rank, n_in, device=weight.device)
         self.B = torch.nn.Parameter(torch.zeros(n, n_out, rank, device=weight.device, dtype=torch.bfloat16))
+
+    def _apply(self, fn, *args, **kwargs):
+        scale = self.scale
+        super()._apply(fn, *args, **kwargs)
+        if self.scale.dtype != torch.float32:       # a module that is converted keeps its fp32 scales
+            self.scale = scale.to(self.scale.device)
+        return self
 
     def forward(self, x, index):
         if differentiated(x, self.weight, self.A, self.B, self.scale):

@@ -131,3 +131,24 @@ def test_a_tangent_is_refused_and_not_dropped(plain, mode, monkeypatch):
                 dual = forward_ad.make_dual(p.detach(), torch.ones_like(p))
                 with pytest.raises(RuntimeError, match="forward"):
                     torch.func.functional_call(module, {name: dual}, (x, *rest))
+
+
+@pytest.mark.parametrize("default", [torch.float32, torch.float64, BF16])
+def test_scales_are_fp32_whatever_they_are_made_of_and_the_module_becomes(default):
+    torch.set_default_dtype(default)
+    try:
+        W = torch.randn(12, 20).to(BF16)
+        whole, third = ff.AdaptersLinear(W, 3, 4, scale=2), ff.AdaptersLinear(W, 3, 4, scale=0.3)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    want = torch.full((3,), 0.3, dtype=torch.float32)
+    assert whole.scale.dtype == torch.float32 and torch.all(whole.scale == 2) and torch.equal(third.scale, want)
+    # The usual conversions of a model, alone and inside another module, keep the value and not only the type.
+    for convert in (lambda m: m.to(BF16), lambda m: m.bfloat16(), lambda m: m.half().to(BF16), lambda m: m.double().to(BF16),
+                    lambda m: torch.nn.Sequential(m).to(torch.device("cpu"), BF16)[0]):
+        layer = convert(ff.AdaptersLinear(W, 3, 4, scale=0.3))
+        assert torch.equal(layer.scale, want) and layer.A.dtype == BF16 and layer.weight.dtype == BF16
+        assert "scale" in layer.state_dict() and "scale" in dict(layer.named_buffers())
+    layer = third.to("meta", BF16)
+    assert layer.scale.device.type == "meta" and layer.scale.dtype == torch.float32
+    assert layer.to_empty(device="cpu").scale.shape == (3,)
