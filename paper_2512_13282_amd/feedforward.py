@@ -104,6 +104,8 @@ class _GatedFeedForward(torch.autograd.Function):
 class _AdaptersLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, A, B, scale, index):
+        if ctx.needs_input_grad[4]:
+            raise RuntimeError("the adapters' scales have no gradient")
         y, h = binding.linear_adapters(x, W, binding.Adapters(A, B, scale), index, keep=True)
         ctx.save_for_backward(x, W, A, B, scale, index, h)
         return y
@@ -155,8 +157,8 @@ class GatedFeedForward(GatedLinear):
 
 class AdaptersLinear(torch.nn.Module):
     """A projection ``weight`` (n_out x n_in bf16, a buffer that does not learn) with ``n`` trainable adapters of rank ``rank``.
-    Its scales (a buffer) are fp32 and stay so where the module is converted to another type.  ``forward(x, index)``: index
-    holds each token's adapter (int32), -1 for none."""
+    Its scales (a buffer) are fp32, stay so where the module is converted to another type, and have no
+    gradient.  ``forward(x, index)``: index holds each token's adapter (int32), -1 for none."""
 
     def __init__(self, weight, n: int, rank: int, scale: float = 1.0):
         super().__init__()

@@ -152,3 +152,18 @@ def test_scales_are_fp32_whatever_they_are_made_of_and_the_module_becomes(defaul
     layer = third.to("meta", BF16)
     assert layer.scale.device.type == "meta" and layer.scale.dtype == torch.float32
     assert layer.to_empty(device="cpu").scale.shape == (3,)
+
+
+def test_scales_that_are_to_learn_are_refused(monkeypatch):
+    """They have no gradient: left out of the backward pass without a word they would never move."""
+    monkeypatch.setattr(binding, "linear_adapters", lambda x, W, held, index, keep=False:
+                        (x.detach() @ W.t(), x.detach() @ held.A[0].t()) if keep else x.detach() @ W.t(), raising=False)
+    layer = ff.AdaptersLinear(torch.randn(12, 20).to(BF16), 2, 4)
+    x, index = torch.randn(6, 20).to(BF16), torch.zeros(6, dtype=torch.int32)
+    layer.scale.requires_grad_()
+    with pytest.raises(RuntimeError, match="scales"):
+        layer(x, index)
+    with torch.no_grad():
+        assert layer(x, index).shape == (6, 12)
+    layer.scale.requires_grad_(False)
+    assert layer(x, index).requires_grad
