@@ -39,7 +39,8 @@ extern "C" {
 #endif
 
 /* act(g): g / (1 + e^-g); g P(g) with P the standard normal distribution; g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2;
- * max(g, 0).  A NaN stays one.  The derivative of the last at 0 is 0. */
+ * max(g, 0).  A NaN stays one.  The derivative of the last at 0 is 0.  Values of act and act' below 2^-100 may be taken
+ * for 0. */
 enum { FFN_SILU = 0, FFN_GELU = 1, FFN_GELU_TANH = 2, FFN_RELU = 3 };
 
 /* H (M x N) = act(X Wg^T) * (X Wu^T), X M x K, Wg and Wu N x K.  G and U (M x N each): where they are not NULL (both or

@@ -12,7 +12,8 @@ namespace gemm {
 // act(g) and act'(g) in fp32.  With p = 1 / (1 + e^-z) for silu (z = g) and the tanh form of gelu
 // (z = 2 sqrt(2 / pi) (g + 0.044715 g^3), as (1 + tanh(z / 2)) / 2 = p), and p the normal distribution for gelu
 // itself, act is g p.  e^x by the hardware's 2^x: the argument's rounding costs |x| 2^-24 of the
-// value, below the bf16 result's half step (2^-9) wherever the value is not negligible.
+// value, far below the bf16 result's half step (2^-8) down to where e^-z passes the range of fp32 and p becomes 0 (act below
+// 2^-100).
 // ---------------------------------------------------------------------------
 template <int ACT>
 __device__ __forceinline__ float act_value(float g) {

@@ -315,3 +315,101 @@ def test_results_past_four_gib():
     dG, dU = b.gated_linear_bwd(H, H, H)
     small = b.gated_linear_bwd(H[-5:].clone(), H[-5:].clone(), H[-5:].clone())
     assert torch.equal(dG[-5:], small[0]) and torch.equal(dU[-5:], small[1])
+
+
+def tail_bounds(name, g):
+    """act(g) and act'(g) in 64 bits, each with a bound that is relative to the terms it is the sum of.
+
+    With t = |z| for p = 1 / (1 + e^-z) (silu, gelu_tanh): z is off by four roundings, 2^-24 |z| each, and so the exponent; 2^x, 1 / x
+    and the products add single steps of 2^-23.  With t = g^2 for gelu: erfc of an argument that is off by 1.5 2^-24 of itself moves by g^2 + 1
+    times that, and erfc itself is taken to be good to 16 steps, 2^-19.  (1 + t) 2^-19 covers each.  A bf16 result adds 2^-8."""
+    if name == "relu":
+        a, s = ref.act(name, g)
+        return (a, 2.0 ** -8 * a), (s, 2.0 ** -8 * s)
+    if name == "gelu":
+        p, slope, t = 0.5 * torch.special.erfc(-g / 2 ** 0.5), torch.exp(-g * g / 2) / (2 * torch.pi) ** 0.5, g * g
+    else:
+        c = 2 * (2 / torch.pi) ** 0.5
+        z, dz = (g, 1.0) if name == "silu" else (c * (g + 0.044715 * g ** 3), c * (1 + 3 * 0.044715 * g * g))
+        p, slope, t = torch.sigmoid(z), torch.sigmoid(z) * torch.sigmoid(-z) * dz, z.abs()
+    a, s = g * p, p + g * slope
+    off = 2.0 ** -19 * (1 + t)
+    return (a, (2.0 ** -8 + off) * a.abs()), (s, 2.0 ** -8 * s.abs() + off * (p + g.abs() * slope))
+
+
+@pytest.mark.parametrize("name", ref.ACTIVATIONS)
+def test_activations_in_their_tails(name):
+    """Small values of act and act' keep their bits down to 2^-100; below that they may be 0."""
+    g = torch.unique(torch.cat((torch.linspace(-80, 80, 3201), torch.linspace(-14, 14, 2801), torch.linspace(-1.5, 1.5, 301))).to(BF16))
+    N = g.numel()
+    x, wg, wu = torch.zeros(2, 8, dtype=BF16), torch.zeros(N, 8, dtype=BF16), torch.zeros(N, 8, dtype=BF16)
+    x[:, 0], wg[:, 0], wu[:, 0] = 1, g, 1
+    x, wg, wu, wd = x.to(DEV), wg.to(DEV), wu.to(DEV), torch.zeros(8, N, dtype=BF16, device=DEV)
+    wd[0] = 1
+    (a, ea), (s, es) = tail_bounds(name, g.to(DEV).double())
+
+    def within(got, want, bound, what):
+        off, small = (got.double() - want).abs(), want.abs() < 2.0 ** -100
+        assert torch.all((off <= bound)[~small.expand_as(off)]), (what, (off / (bound + 1e-300))[~small.expand_as(off)].max().item())
+        assert torch.all(got.double().abs()[small.expand_as(off)] <= 2.0 ** -99), what
+
+    for plan in plans(ffn.FFN_OP_GATED, 2, N, 8, splits=(1,)):
+        H, G, U = b.gated_linear(x, wg, wu, name, keep=True)
+        within(H, a, ea, ("act", plan))
+    one = torch.ones_like(G)
+    for what, got in (("grad", b.gated_linear_grad(x, wd, G, U, name)), ("bwd", (*b.gated_linear_bwd(one, G, U, name), H))):
+        within(got[0], s, es, ("slope", what))
+        within(got[1], a, ea, ("act of the gradient", what))
+        within(got[2], a, ea, ("H again", what))
+
+
+# M, N, K of the result: whole rounds of 256 x 256 tiles leave more behind by columns than by rows, so the lower tiles take the rows
+# after them (of the second gradient, where there are two).
+ROW_TAILS = [(23040, 700, 72), (22950, 651, 40)]
+
+
+def leaves_rows(M, cols, pairs):
+    """Whether tiles of 256 rows and `cols` columns, walked in whole rounds of 256, end with lower tiles over rows."""
+    tm, tn = -(-M // 256) * pairs, -(-cols // 256)
+    full = tm * tn // 256 * 256
+    return 0 < full < tm * tn and full // tm * tm < full // tn * tn
+
+
+@pytest.mark.parametrize("config", [4, 5])
+@pytest.mark.parametrize("size", ROW_TAILS, **ids)
+def test_lower_tiles_over_the_last_rows(size, config):
+    M, N, K = size
+    gen = generator("row tails", *size)
+    x, w, v = matrix(gen, M, K), matrix(gen, N, K, K ** -0.5), matrix(gen, K, N, K ** -0.5)
+    half, u = N // 2, matrix(gen, M, N)
+    t, y = matrix(gen, K, M), matrix(gen, K, N)
+    first, second = matrix(gen, K, M // 2), matrix(gen, K, M // 2)
+    assert leaves_rows(M, N, 1) and leaves_rows(M // 2, N, 2) and leaves_rows(M, 2 * half, 1)
+    calls = {
+        ffn.FFN_OP_GATED: (lambda: b.gated_linear(x, w[:half], w[half:2 * half], "gelu", keep=True), lambda: ref.gated(x, w[:half], w[half:2 * half], "gelu")),
+        ffn.FFN_OP_GRAD: (lambda: b.gated_linear_grad(x, v, u, u, "silu"), lambda: ref.grad(x, v, u, u, "silu")),
+        ffn.FFN_OP_DX: (lambda: (b.gated_linear_dx(x, v, x, v),), lambda: (ref.dx(x, v, x, v, BF16),)),
+        ffn.FFN_OP_GATED_DW: (lambda: b.gated_linear_dw(first, second, y), lambda: (ref.dw(first, y, torch.float32), ref.dw(second, y, torch.float32))),
+        ffn.FFN_OP_DW: (lambda: (b.linear_dw(t, y),), lambda: (ref.dw(t, y, torch.float32),)),
+    }
+    for op, (call, want) in calls.items():
+        try:
+            assert ffn.ffn_force_plan(op, config, 1) == b.GEMM_OK
+            print(size, config, op, flush=True)
+            got = call()
+        finally:
+            ffn.ffn_force_plan(op)
+        for g, w64 in zip(got, want()):
+            ref.assert_within(g, w64, f"op {op}")
+
+
+@pytest.mark.parametrize("size", [(11008, 4096, 2048), (5504, 2048, 513)], **ids)
+def test_weight_gradients_of_a_training_step(size):
+    """Both gradients and one, by the library's plans for these sizes."""
+    M, N, K = size
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(M)
+    dg, du, x = (torch.randn(K, c, device=DEV, generator=gen).to(BF16) for c in (M, M, N))
+    print(ffn.ffn_plan(ffn.FFN_OP_GATED_DW, M, N, K), ffn.ffn_plan(ffn.FFN_OP_DW, M, N, K), flush=True)
+    for got, want in zip((*b.gated_linear_dw(dg, du, x), b.linear_dw(dg, x)), (dg, du, dg)):
+        ref.assert_within(got, ref.dw(want, x, torch.float32))
