@@ -6,7 +6,7 @@ import torch
 import fused_reference as ref
 from paper_2512_13282_amd import adapters as ad
 from paper_2512_13282_amd import binding as b
-from test_gpu_ffn import BF16, DEV, generator, ids, matrix
+from test_gpu_ffn import BF16, DEV, generator, ids, leaves_rows, matrix
 
 pytestmark = pytest.mark.gpu
 
@@ -341,3 +341,24 @@ def test_infinities_of_the_activations_in_the_weight_gradients(r, dtype):
         t = torch.nonzero(index == i)[:, 0]
         matches(dA[i], dh.double()[t].t()[:, :, None] * x.double().cpu()[t][None], ("dA", i))
         matches(dB[i].t(), h.double()[t].t()[:, :, None] * dy.double().cpu()[t][None], ("dB", i))
+
+
+@pytest.mark.parametrize("config", [4, 5])
+@pytest.mark.parametrize("op", [0, 1])
+def test_lower_tiles_over_the_last_rows(op, config):
+    """Whole rounds of 256 x 256 tiles over all columns, then lower tiles over the last rows, each row with its adapter."""
+    gen = generator("row tails", op)
+    M, N, K, n, r = 22950, 651, 40, 3, 5
+    n_out, n_in = (N, K) if op == 0 else (K, N)
+    x, w = matrix(gen, M, K), matrix(gen, n_out, n_in, K ** -0.5)
+    A, B = stacked(gen, n, r, n_in, K ** -0.5, 0, 0), stacked(gen, n, n_out, r, 1.0, 0, 0)
+    index = torch.randint(-1, n, (M,), generator=gen).to(torch.int32)
+    at = index.to(DEV)
+    assert leaves_rows(M, N, 1)
+    try:
+        assert ad.adapters_force_plan(op, config, 1) == b.GEMM_OK
+        y = (b.linear_adapters if op == 0 else b.linear_adapters_dx)(x, w, ad.Adapters(A, B), at)
+    finally:
+        ad.adapters_force_plan(op)
+    down, up = (A.transpose(1, 2), B.transpose(1, 2)) if op == 0 else (B, A)
+    ref.assert_within(y, ref.adapted(x, w.t() if op == 0 else w, down, up, None, index, BF16)[0])
