@@ -245,11 +245,10 @@ __device__ __forceinline__ FusedWork fused_work(const FusedArgs &a, int all) {
     const int width = g.group_m * tiles_n, first_m = t / width * g.group_m;
     const int rows = tiles_m - first_m < g.group_m ? tiles_m - first_m : g.group_m;
     const int tm = first_m + t % width % rows, tn = t % width / rows;
-    // DW: tile rows from `half` on are the second matrix's.  The lower tiles begin at a row of the matrix that the
-    // others leave off in, and at the first row of a matrix after it.
+    // DW: tile rows from `half` on are the second matrix's (lower tiles over the last rows: all are).
     const int half = w.low ? a.tail.half : a.half;
     w.which = tm >= half;
-    const int64_t row0 = w.low && !(w.which && half > 0) ? a.tail.row : 0;
+    const int64_t row0 = w.low ? a.tail.row : 0;
     w.m0 = row0 + int64_t(w.which ? tm - half : tm) * (w.low ? LOW : BM);
     w.n0 = (w.low ? a.tail.col : 0) + int64_t(tn) * COLS;
     const int chunk = int(g.k_chunk / 64);

@@ -104,7 +104,7 @@ __device__ __forceinline__ u32x4_t load8_any(const uint16_t *p) {
 // by zeros, so an infinity or a NaN in one request's adapter stays out of the others'.  h does not depend on the
 // adapter and is read once for every 16 ranks; the matrices of two to four adapters are on their way at once, for what
 // a batch of many requests waits for is their latency.  h keeps its fp32 value in two bf16 parts (2^-16 left
-// out, a bf16 result's half step being 2^-9), three and so all of it for an fp32 result.  Runs ahead of the
+// out, a bf16 result's half step being 2^-8), three and so all of it for an fp32 result.  Runs ahead of the
 // K loop, on sums that are 0, while the first stages are on their way.
 //
 // Sums that are not all finite are formed again, STRICT, from values without their infinities and NaN where a part of h may not

@@ -163,11 +163,11 @@ FusedTail fused_tail(FusedOp op, int32_t pairs, int64_t M, int64_t N, const Fuse
         t.tiles_m = t.half * pairs;
         t.tiles_n = tn - p.tail_cols;
     } else {
-        const bool second = p.tail_rows >= per;                  // the rows left are all the second matrix's
+        // Of two matrices the rows left are the second's: whole rounds have more than half of all tiles.
+        const bool second = pairs == 2;
         t.row = (second ? p.tail_rows - per : p.tail_rows) * c.bm;
-        const int64_t left = ceil_div(M - t.row, c.low);
-        t.half = second ? 0 : left;
-        t.tiles_m = second ? left : left + (pairs == 2 ? ceil_div(M, c.low) : 0);
+        t.tiles_m = ceil_div(M - t.row, c.low);
+        t.half = second ? 0 : t.tiles_m;
         t.tiles_n = tn;
     }
     t.tiles = t.tiles_m * t.tiles_n;
