@@ -18,7 +18,8 @@
  * Ownership, workspaces, streams, capture, realigned operands and error codes are those of ffn_mi355x.h.  A captured
  * call reads the index, the scales and the adapters anew at each replay.  GEMM_ERR_INVALID_VALUE is returned for a
  * NULL set, a negative n or r, and an adapter's matrix that overlaps the next one, too, and GEMM_ERR_UNSUPPORTED for a
- * rank above 1024.  A, B and the adapters' gradients may lie at any address and stride.
+ * rank above 1024, too; by adapters_linear_* for more than 2^26 tokens or 2^31 - 1 adapters, by adapters_dw_* for more than 65535
+ * adapters or N + K above 2^29.  A, B and the adapters' gradients may lie at any address and stride.
  */
 #ifndef ADAPTERS_MI355X_H
 #define ADAPTERS_MI355X_H

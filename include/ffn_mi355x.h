@@ -15,7 +15,7 @@
  * entry point throws or aborts, and workspaces (partial sums of K slices, realigned copies) are the
  * ones that gemm_release_workspace frees.  Reads are made in pieces of up to 16 bytes: an operand
  * whose rows lie on 16-byte addresses may have the bytes up to its row's next multiple of 16 read,
- * without being used.
+ * any other the rest of the aligned four bytes that hold a row's first and last element, without being used.
  * GEMM_ERR_INVALID_VALUE is returned for a negative size, a stride that is too small, a NULL pointer
  * whose operand is non-empty, a pointer that is not aligned to its element size, an unknown
  * activation, and a result that overlaps an operand or another result; GEMM_ERR_UNSUPPORTED for a size

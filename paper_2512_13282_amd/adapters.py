@@ -11,8 +11,8 @@ addresses.  The torch helpers read addresses, strides and the current stream and
 * ``linear_adapters_dw(x, dy, h, dh, index, n)``: every adapter's gradients, from what the two above leave with
   ``keep=True``.
 
-``Adapters`` holds n adapters of one rank; one of a lower rank has zeros behind its own.  ``AdaptersLinear``
-(feedforward.py) is the projection as a module.
+``Adapters`` holds n adapters of one rank; one of a lower rank has zeros behind its own.  Ranks go up to 1024, a call's tokens to 2^26;
+gradients are had of at most 65535 adapters at a time.  ``AdaptersLinear`` (feedforward.py) is the projection as a module.
 """
 from __future__ import annotations
 
