@@ -87,7 +87,7 @@ def adapters_force_plan(op, config=-1, split_k=0) -> int:
 def _stack(x, n, rows, cols):
     """Row stride and stride from matrix to matrix of n matrices of rows x cols."""
     per, ld, step = x.stride()
-    return _ld((ld, step), rows, cols), per if n > 1 and rows and cols else rows * cols or 1
+    return _ld((ld, step), rows if n else 0, cols), per if n > 1 and rows and cols else rows * cols or 1
 
 
 class _Helpers:

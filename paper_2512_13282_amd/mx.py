@@ -107,7 +107,7 @@ def _ld(stride, rows, cols):
     single row or an empty matrix has no meaningful stride).  The entry points refuse one that is
     shorter than a row: an expanded tensor's, say, which holds fewer elements than the matrix."""
     ld, step = stride
-    if step != 1 and cols > 1:
+    if step != 1 and cols > 1 and rows:
         raise ValueError("rows must be contiguous")
     return ld if rows > 1 and cols else cols or 1
 

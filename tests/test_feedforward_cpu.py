@@ -167,3 +167,16 @@ def test_scales_that_are_to_learn_are_refused(monkeypatch):
         assert layer(x, index).shape == (6, 12)
     layer.scale.requires_grad_(False)
     assert layer(x, index).requires_grad
+
+
+def test_an_empty_matrix_has_no_strides_that_matter():
+    """The gradient of a sum over no tokens is an expanded matrix without rows, and contiguous() leaves its strides of 0."""
+    from paper_2512_13282_amd import adapters, mx
+    x = torch.zeros(1).expand(0, 96).contiguous()
+    assert x.stride() == (0, 0)
+    assert mx._ld(x.stride(), *x.shape) == 96
+    for stride in ((0, 0), (1, 5), (96, 1)):
+        assert mx._ld(stride, 0, 96) == 96 and mx._ld(stride, 5, 0) == 1
+    with pytest.raises(ValueError):
+        mx._ld((0, 0), 1, 96)
+    assert adapters._stack(torch.zeros(1).expand(0, 8, 96), 0, 8, 96)[0] == 96

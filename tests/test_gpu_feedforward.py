@@ -195,3 +195,19 @@ def test_a_down_projection_that_does_not_fit_is_refused(down, error):
     for mode in (torch.no_grad, torch.enable_grad):
         with mode(), pytest.raises(error):
             block(x)
+
+
+def test_a_batch_without_tokens():
+    """Outputs without rows, and gradients of 0 for what learns."""
+    gated, block = ff.GatedLinear(64, 96), ff.GatedFeedForward(64, 96, 40)
+    down = ff.AdaptersLinear(torch.randn(40, 96, device=DEV).to(BF16), 2, 4)
+    index = torch.empty(0, dtype=torch.int32, device=DEV)
+    for module, call in ((gated, gated), (block, block), (down, lambda x: down(gated(x), index))):
+        x = torch.empty(0, 64, dtype=BF16, device=DEV, requires_grad=True)
+        with torch.no_grad():
+            assert call(x).shape[0] == 0
+        y = call(x)
+        y.sum().backward()
+        assert x.grad.shape == (0, 64)
+        for p in module.parameters():
+            assert p.grad.shape == p.shape and torch.all(p.grad == 0)
