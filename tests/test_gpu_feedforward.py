@@ -211,3 +211,83 @@ def test_a_batch_without_tokens():
         assert x.grad.shape == (0, 64)
         for p in module.parameters():
             assert p.grad.shape == p.shape and torch.all(p.grad == 0)
+
+
+def whole(*shape):
+    """Whole numbers of -1 to 1: sums of their products are exact in any order, so that plans do not matter to the bits."""
+    return torch.randint(-1, 2, shape, device=DEV).to(BF16)
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 0), (3, 1), (8, 8)])
+@pytest.mark.parametrize("tokens", [1, 2, 70])
+def test_inputs_and_gradients_that_are_slices(tokens, pad, offset):
+    """Rows at any stride and address give the bits of their copies, forward and backward."""
+    torch.manual_seed(tokens)
+    n_in, n_hidden, n_out = 48, 72, 40
+    gated, block = ff.GatedLinear(n_in, n_hidden, "relu"), ff.GatedFeedForward(n_in, n_hidden, n_out, "relu")
+    down = ff.AdaptersLinear(whole(n_out, n_hidden + pad + offset)[:, offset:n_hidden + offset], 3, 5)
+    with torch.no_grad():
+        for p in (*gated.parameters(), *block.parameters(), *down.parameters()):
+            p.copy_(whole(*p.shape))
+    index = torch.randint(-1, 3, (tokens,), device=DEV, dtype=torch.int32)
+    wide_x, wide_dy = whole(tokens, offset + n_in + pad), whole(tokens, offset + n_out + pad)
+    for call, leaves in ((lambda x: down(gated(x), index), (*gated.parameters(), *down.parameters())), (block, tuple(block.parameters()))):
+        results = []
+        for slices in (True, False):
+            x, dy = wide_x[:, offset:offset + n_in], wide_dy[:, offset:offset + n_out]
+            x, dy = (x, dy) if slices else (x.contiguous().clone(), dy.contiguous().clone())
+            x = x.detach().requires_grad_()
+            y = call(x)
+            results.append((y, *torch.autograd.grad(y, (x, *leaves), dy)))
+        assert all(torch.equal(a, c) for a, c in zip(*results))
+
+
+@pytest.mark.parametrize("n,rank", [(0, 4), (2, 0), (1, 1), (3, 1024)])
+def test_projections_without_adapters_and_of_the_largest_rank(n, rank):
+    torch.manual_seed(rank)
+    down = ff.AdaptersLinear(whole(24, 40), n, rank)
+    with torch.no_grad():
+        down.A.copy_(whole(n, rank, 40))
+        down.B.copy_(whole(n, 24, rank))
+    x = whole(9, 40).requires_grad_()
+    dy = whole(9, 24)
+    index = torch.randint(-1, n, (9,), device=DEV, dtype=torch.int32) if n else torch.zeros(9, dtype=torch.int32, device=DEV)
+    y = down(x, index)
+    grads = torch.autograd.grad(y, (x, down.A, down.B), dy)
+    X, W, A, B = (t.detach().double() for t in (x, down.weight, down.A, down.B))
+    want, dx, dA, dB = X @ W.t(), dy.double() @ W, torch.zeros_like(A), torch.zeros_like(B)
+    for t, i in enumerate(index.tolist()):
+        if n and i >= 0:
+            h, dh = X[t] @ A[i].t(), dy[t].double() @ B[i]
+            want[t] += h @ B[i].t()
+            dx[t] += dh @ A[i]
+            dA[i] += torch.outer(dh, X[t])
+            dB[i] += torch.outer(dy[t].double(), h)
+    for got, v in zip((y.detach(), *grads), (want, dx, dA, dB)):
+        assert torch.equal(got, v.to(BF16))
+
+
+def test_one_leaf_at_a_time():
+    """Whatever learns alone gets the gradient that it gets among the others."""
+    torch.manual_seed(9)
+    gated, block = ff.GatedLinear(48, 72), ff.GatedFeedForward(48, 72)
+    down = ff.AdaptersLinear(torch.randn(40, 72, device=DEV).to(BF16), 3, 5)
+    with torch.no_grad():
+        down.B.normal_()
+    index = torch.randint(-1, 3, (33,), device=DEV, dtype=torch.int32)
+    x = torch.randn(33, 48, device=DEV).to(BF16)
+    for call, modules in ((lambda: down(gated(x), index), (gated, down)), (lambda: block(x), (block,))):
+        leaves = [x, *(p for m in modules for p in m.parameters())]
+        for t in leaves:
+            t.requires_grad_()
+        y = call()
+        dy = torch.randn_like(y)
+        want = torch.autograd.grad(y, leaves, dy, retain_graph=True)
+        kept = torch.autograd.grad(y, leaves, dy, create_graph=True)
+        assert all(torch.equal(a, c) for a, c in zip(kept, want))
+        for i in range(len(leaves)):
+            for j, t in enumerate(leaves):
+                t.requires_grad_(i == j)
+            y2 = call()
+            assert torch.equal(y2, y) and torch.equal(torch.autograd.grad(y2, leaves[i], dy)[0], want[i])
+        x.requires_grad_(False)
